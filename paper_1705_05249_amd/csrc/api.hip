@@ -9,6 +9,7 @@
 
 #include <string>
 
+#include "../../include/mg_experts.h"
 #include "internal.h"
 #include "select.h"
 #include "lds_layout.h"
@@ -1329,6 +1330,10 @@ const char *mg_status_string(mg_status status)
         case MG_ERR_SIDE: return "invalid side";
         case MG_ERR_UPLO: return "invalid uplo";
         case MG_ERR_DIAG: return "invalid diag";
+        case MG_ERR_TYPE: return "unknown element type";
+        case MG_ERR_BLOCK: return "unknown block form or kind of scales";
+        case MG_ERR_GROUPS: return "number of groups, experts or choices out of range";
+        case MG_ERR_SCALES: return "leading dimension of scales too small";
         default: return "unknown status";
     }
 }

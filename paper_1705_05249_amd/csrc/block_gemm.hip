@@ -1,0 +1,191 @@
+// Host side of the 8-bit products (which kernel, how many slices), the kernel for operands at any address, the kernel for few rows, and the
+// launch that adds slices.
+#include "internal.h"
+#include "block_gemm_kernel.h"
+
+namespace mg {
+namespace {
+
+// ---- operands at any address: 128 x 128 tiles, staged through registers.  LDS rows of 128 bytes as in lds_layout.h (16-row fragments).
+template <int MODE, int SUMS> __global__ __launch_bounds__(256) void block_any_kernel(const BlockArgs args)
+{
+    constexpr int BM = 128, BN = 128, FM = 4, FN = 4;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds_a[BM * 128], lds_b[BN * 128];
+    __shared__ __attribute__((aligned(16))) float scale_a[BM], scale_b[BN];
+    BlockTile tile;
+    if (!block_tile<MODE, 7, BN>(args, &tile)) return;
+    const int t = threadIdx.x, lane = t % 64, wave = t / 64, wm = wave % 2, wn = wave / 2;
+    const uint8_t *const B = args.B + (MODE == BLOCK_ROWS ? tile.group * args.stride_b : 0);
+    const float *const SB = args.SB + (MODE == BLOCK_ROWS ? tile.group * args.stride_sb : 0);
+
+    // this thread's piece of four rows of each operand; rows that do not exist: the tile's first, whose products nobody stores
+    const int piece = t % 8;
+    const uint8_t *from_a[4], *from_b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = t / 8 + 32 * i;
+        const int64_t row = tile.m0 + r < tile.m_end ? tile.m0 + r : tile.m0;
+        from_a[i] = args.A + (MODE == BLOCK_ROWS ? source_row(args.groups, row) : row) * args.lda + tile.column + 16 * piece;
+        from_b[i] = B + (tile.n0 + r < args.n ? tile.n0 + r : tile.n0) * args.ldb + tile.column + 16 * piece;
+    }
+    const float *from_s;
+    {
+        const int r = t % 128;
+        if (t < 128) {
+            const int64_t row = tile.m0 + r < tile.m_end ? tile.m0 + r : tile.m0;
+            from_s = args.SA + ((MODE == BLOCK_ROWS ? source_row(args.groups, row) : row) >> args.a_shift) * args.ldsa;
+        } else {
+            from_s = SB + ((tile.n0 + r < args.n ? tile.n0 + r : tile.n0) >> args.b_shift) * args.ldsb;
+        }
+        from_s += tile.column / SCALE_BLOCK;
+    }
+
+    floatx4 acc[FN][FM];
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) acc[j][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    u32x4 next_a[4], next_b[4];
+    float next_s = 0.f;
+    auto fetch = [&](int b) {
+        const int64_t at = static_cast<int64_t>(b) * SCALE_BLOCK;
+        const int64_t left = tile.k - at - 16 * piece;
+        const int valid = static_cast<int>(left < 16 ? left : 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            next_a[i] = load_bytes16(from_a[i] + at, valid);
+            next_b[i] = load_bytes16(from_b[i] + at, valid);
+        }
+        next_s = from_s[b];
+    };
+    if (tile.b0 < tile.b_end) fetch(tile.b0);
+    for (int b = tile.b0; b < tile.b_end; ++b) {
+        __syncthreads();                                   // the block before has been read
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = ldsmap::kcontig_slot<16>(t / 8 + 32 * i, piece);
+            *reinterpret_cast<u32x4 *>(lds_a + at) = next_a[i];
+            *reinterpret_cast<u32x4 *>(lds_b + at) = next_b[i];
+        }
+        (t < 128 ? scale_a : scale_b)[t % 128] = next_s;
+        __syncthreads();
+        if (b + 1 < tile.b_end) fetch(b + 1);
+        typename FragmentOf<SUMS>::type fa[FM], fb;
+        float sa[FM];
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int row = 64 * wm + 16 * i + lane % 16;
+            fa[i].set(join(*reinterpret_cast<const u32x4 *>(lds_a + ldsmap::kcontig_slot<16>(row, lane / 16)),
+                           *reinterpret_cast<const u32x4 *>(lds_a + ldsmap::kcontig_slot<16>(row, lane / 16 + 4))));
+            sa[i] = scale_a[row];
+        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int row = 64 * wn + 16 * j + lane % 16;
+            fb.set(join(*reinterpret_cast<const u32x4 *>(lds_b + ldsmap::kcontig_slot<16>(row, lane / 16)),
+                        *reinterpret_cast<const u32x4 *>(lds_b + ldsmap::kcontig_slot<16>(row, lane / 16 + 4))));
+            if constexpr (SUMS == SUMS_POW2) {
+                const int sb = scale_bits(scale_b[row]);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) add_block_pow2(acc[j][i], fb, fa[i], sb, scale_bits(sa[i]));
+            } else {
+                const floatx4 sb = *reinterpret_cast<const floatx4 *>(scale_b + 64 * wn + 16 * j + 4 * (lane / 16));
+#pragma unroll
+                for (int i = 0; i < FM; ++i) add_block(acc[j][i], fb, fa[i], sb, sa[i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int64_t row = tile.m0 + 64 * wm + 16 * i + lane % 16;
+        if (row < tile.m_end) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) write_block(args, tile.group, row, tile.n0 + 64 * wn + 16 * j + 4 * (lane / 16), acc[j][i]);
+        }
+    }
+}
+
+// ---- C = alpha * (sum of the slices) + beta * C
+__global__ __launch_bounds__(256) void block_add_slices_kernel(const BlockArgs args)
+{
+    const int64_t quads = (args.n + 3) / 4;
+    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t row = id / quads, col = id % quads * 4;
+    if (row >= args.partial_rows) return;
+    if (!args.each_own_c && args.groups.offsets != nullptr && row >= args.groups.offsets[args.groups.count]) return;      // belongs to no expert
+    const int valid = static_cast<int>(args.n - col < 4 ? args.n - col : 4);
+    floatx4 sum{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < args.slices; ++s) {
+        float v[4];
+        load_piece<float, 4>(args.partial + (s * args.partial_rows + row) * args.n + col, valid, v);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum[r] += v[r];
+    }
+    BlockArgs whole = args;
+    whole.partial = nullptr;
+    const bool many = args.each_own_c;
+    write_block(whole, many ? static_cast<int>(row / args.m) : 0, many ? row % args.m : row, col, sum);
+}
+
+struct Plan {
+    int tiles_m, tiles_n, slices;
+};
+
+int64_t output_rows(int mode, int groups, int64_t m) { return mode == BLOCK_SUM ? groups * m : m; }
+
+// Slices of the sum: where the tiles leave most of the chip idle, and no more than leaves four blocks to each
+Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, size_t workspace)
+{
+    Plan p{};
+    p.tiles_m = static_cast<int>(ceil_div(m, 128) + (mode == BLOCK_ROWS ? groups : 0));
+    p.tiles_n = static_cast<int>(ceil_div(n, 128));
+    const int64_t tiles = (mode == BLOCK_ROWS ? ceil_div(m, 128) : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * (mode == BLOCK_SUM ? groups : 1);
+    const int64_t blocks = ceil_div(k, SCALE_BLOCK) / (mode == BLOCK_SUM ? groups : 1);
+    const size_t one = static_cast<size_t>(output_rows(mode, groups, m)) * n * 4;
+    int64_t s = 1;
+    while (s < 16 && tiles * s * 2 <= 256 && blocks / (s * 2) >= 4 && one * s * 2 <= workspace) s *= 2;
+    p.slices = static_cast<int>(s);
+    return p;
+}
+
+template <int MODE> hipError_t launch_mode(const BlockProblem &p, const BlockArgs &args)
+{
+    const dim3 grid(static_cast<uint32_t>(args.tiles_m) * args.tiles_n, args.slices, MODE == BLOCK_SUM ? p.groups.count : 1);
+    if (p.fp32_sums) block_any_kernel<MODE, SUMS_FP32><<<grid, 256, 0, p.stream>>>(args);
+    else if (p.pow2) block_any_kernel<MODE, SUMS_POW2><<<grid, 256, 0, p.stream>>>(args);
+    else block_any_kernel<MODE, SUMS_ANY><<<grid, 256, 0, p.stream>>>(args);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t block_gemm_workspace(int mode, int groups, int64_t m, int64_t n, int64_t k)
+{
+    const Plan p = plan(mode, groups, m, n, k, SIZE_MAX);
+    return p.slices > 1 ? static_cast<size_t>(output_rows(mode, groups, m)) * n * 4 * p.slices : 0;
+}
+
+hipError_t launch_block_gemm(const BlockProblem &p)
+{
+    const Plan how = plan(p.mode, p.groups.count, p.m, p.n, p.k, p.workspace == nullptr ? 0 : p.workspace_bytes);
+    BlockArgs args{};
+    args.A = p.A; args.lda = p.lda; args.SA = p.SA; args.ldsa = p.ldsa; args.a_shift = p.a_square ? 7 : 0;
+    args.B = p.B; args.ldb = p.ldb; args.SB = p.SB; args.ldsb = p.ldsb; args.b_shift = p.b_square ? 7 : 0;
+    args.stride_b = p.stride_b; args.stride_sb = p.stride_sb;
+    args.C = p.C; args.ldc = p.ldc; args.c_type = p.c_type; args.stride_c = p.stride_c; args.each_own_c = p.mode == BLOCK_SUM;
+    args.groups = p.groups;
+    args.m = static_cast<int>(p.m); args.n = static_cast<int>(p.n); args.k = p.alpha == 0.f ? 0 : static_cast<int>(p.k);
+    args.alpha = p.alpha; args.beta = p.beta;
+    args.tiles_m = how.tiles_m; args.tiles_n = how.tiles_n; args.slices = how.slices;
+    args.partial = how.slices > 1 ? static_cast<float *>(p.workspace) : nullptr;
+    args.partial_rows = output_rows(p.mode, p.groups.count, p.m);
+    const hipError_t e = p.mode == BLOCK_DENSE ? launch_mode<BLOCK_DENSE>(p, args)
+                         : p.mode == BLOCK_ROWS ? launch_mode<BLOCK_ROWS>(p, args) : launch_mode<BLOCK_SUM>(p, args);
+    if (e != hipSuccess || how.slices == 1) return e;
+    const int64_t quads = args.partial_rows * ceil_div(p.n, 4);
+    block_add_slices_kernel<<<static_cast<uint32_t>(ceil_div(quads, 256)), 256, 0, p.stream>>>(args);
+    return hipGetLastError();
+}
+
+}  // namespace mg

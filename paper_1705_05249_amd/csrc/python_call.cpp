@@ -1,4 +1,4 @@
-// The calls of gemm.py without ctypes: one C function per entry point that takes the Python arguments as they are (tensors, addresses,
+// The calls of gemm.py and experts.py without ctypes: one C function per entry point that takes the Python arguments as they are (tensors, addresses,
 // None), asks tensors for their addresses and torch for its current stream, and calls the library with the interpreter's lock released.
 // In ctypes and Python these conversions were 4 us of the 7.6 that the host took for a small product, 0.9 of 3.8 now: calls one behind the other,
 // FP32 256^3 7.6 -> 4.8 us, which is the kernel's own time, FP16 64 x 64 x 64 7.6 -> 3.8.
@@ -18,6 +18,7 @@
 #include <utility>
 
 #include "../../include/mg_gemm.h"
+#include "../../include/mg_experts.h"
 
 namespace {
 
@@ -166,7 +167,9 @@ PyObject *invoke(const char *name, mg_status (*fn)(P...), PyObject *const *args,
 #define MG_ENTRIES(X)                                                                                                       \
     X(mg_sgemm) X(mg_hgemm) X(mg_sgemm_static) X(mg_sgemv) X(mg_hgemv) X(mg_ssymm) X(mg_hsymm) X(mg_ssyrk) X(mg_hsyrk)      \
     X(mg_strmm) X(mg_htrmm) X(mg_sgemm_batched) X(mg_hgemm_batched) X(mg_sgemm_strided_batched) X(mg_hgemm_strided_batched) \
-    X(mg_sim2col) X(mg_him2col) X(mg_sconv2d) X(mg_hconv2d)
+    X(mg_sim2col) X(mg_him2col) X(mg_sconv2d) X(mg_hconv2d)                                                                 \
+    X(mg_block_quantize) X(mg_block_quantize_batched) X(mg_block_quantize_grouped) X(mg_block_gemm) X(mg_block_gemm_grouped) \
+    X(mg_block_gemm_grouped_sum) X(mg_expert_sort) X(mg_expert_gather) X(mg_expert_combine) X(mg_expert_combine_grad)
 
 #define X(name)                                                                                 \
     decltype(&::name) bound_##name;                                                             \
