@@ -128,32 +128,57 @@ __global__ __launch_bounds__(256) void block_add_slices_kernel(const BlockArgs a
     write_block(whole, many ? static_cast<int>(row / args.m) : 0, many ? row % args.m : row, col, sum);
 }
 
+constexpr int TILE_ANY = -1;                   // the kernel for operands at any address, 128 x 128
+
 struct Plan {
+    int tile;                                 // BlockDmaTile or TILE_ANY
     int tiles_m, tiles_n, slices;
 };
 
 int64_t output_rows(int mode, int groups, int64_t m) { return mode == BLOCK_SUM ? groups * m : m; }
 
-// Slices of the sum: where the tiles leave most of the chip idle, and no more than leaves four blocks to each
-Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, size_t workspace)
+// Which kernel and how many slices of the sum.  Slices: where the tiles leave most of the chip idle, and no more than leaves four blocks to each.
+Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums, bool aligned, size_t workspace)
 {
     Plan p{};
-    p.tiles_m = static_cast<int>(ceil_div(m, 128) + (mode == BLOCK_ROWS ? groups : 0));
-    p.tiles_n = static_cast<int>(ceil_div(n, 128));
-    const int64_t tiles = (mode == BLOCK_ROWS ? ceil_div(m, 128) : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * (mode == BLOCK_SUM ? groups : 1);
-    const int64_t blocks = ceil_div(k, SCALE_BLOCK) / (mode == BLOCK_SUM ? groups : 1);
+    const int64_t batch = mode == BLOCK_SUM ? groups : 1;
+    auto tiles = [&](int tile) {
+        const int64_t bm = tile == TILE_ANY ? 128 : block_dma_rows(tile), bn = tile == TILE_ANY ? 128 : block_dma_cols(tile, sums);
+        p.tiles_m = static_cast<int>(ceil_div(m, bm) + (mode == BLOCK_ROWS ? groups : 0));
+        p.tiles_n = static_cast<int>(ceil_div(n, bn));
+        return (mode == BLOCK_ROWS ? ceil_div(m, bm) : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * batch;
+    };
+    p.tile = !aligned ? TILE_ANY : tiles(DMA_256) >= 160 ? DMA_256 : DMA_128;
+    const int64_t count = tiles(p.tile);
+    const int64_t blocks = ceil_div(k, SCALE_BLOCK) / batch;
     const size_t one = static_cast<size_t>(output_rows(mode, groups, m)) * n * 4;
     int64_t s = 1;
-    while (s < 16 && tiles * s * 2 <= 256 && blocks / (s * 2) >= 4 && one * s * 2 <= workspace) s *= 2;
+    while (s < 16 && count * s * 2 <= 256 && blocks / (s * 2) >= 4 && one * s * 2 <= workspace) s *= 2;
     p.slices = static_cast<int>(s);
     return p;
 }
 
-template <int MODE> hipError_t launch_mode(const BlockProblem &p, const BlockArgs &args)
+// Rows on 16 bytes, and 32-bit offsets: inside a tile of 256 rows, or from the first row of A where rows are indexed
+bool dma_operands(const BlockProblem &p)
 {
+    auto on16 = [](const void *x, int64_t a, int64_t b) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && a % 16 == 0 && b % 16 == 0; };
+    if (!on16(p.A, p.lda, 0) || !on16(p.B, p.ldb, p.mode == BLOCK_ROWS ? p.stride_b : 0)) return false;
+    const __int128 rows_a = p.mode == BLOCK_ROWS && p.groups.source != nullptr ? p.m : 256, most = (__int128(1) << 31) - (1 << 20);
+    const __int128 along = p.mode == BLOCK_SUM ? p.lda : p.k;
+    return rows_a * p.lda + along < most && __int128(256) * p.ldb + along < most && (rows_a * p.ldsa + along / 128) * 4 < most &&
+           (__int128(256) * p.ldsb + along / 128) * 4 < most;
+}
+
+template <int MODE> hipError_t launch_mode(const BlockProblem &p, const BlockArgs &args, int sums, int tile)
+{
+    if (tile != TILE_ANY) {
+        if constexpr (MODE == BLOCK_DENSE) return launch_block_dma_dense(args, sums, tile, p.stream);
+        else if constexpr (MODE == BLOCK_ROWS) return launch_block_dma_rows(args, sums, tile, p.stream);
+        else return launch_block_dma_sum(args, sums, tile, p.stream);
+    }
     const dim3 grid(static_cast<uint32_t>(args.tiles_m) * args.tiles_n, args.slices, MODE == BLOCK_SUM ? p.groups.count : 1);
-    if (p.fp32_sums) block_any_kernel<MODE, SUMS_FP32><<<grid, 256, 0, p.stream>>>(args);
-    else if (p.pow2) block_any_kernel<MODE, SUMS_POW2><<<grid, 256, 0, p.stream>>>(args);
+    if (sums_fp32(sums)) block_any_kernel<MODE, SUMS_FP32><<<grid, 256, 0, p.stream>>>(args);
+    else if (sums == SUMS_POW2) block_any_kernel<MODE, SUMS_POW2><<<grid, 256, 0, p.stream>>>(args);
     else block_any_kernel<MODE, SUMS_ANY><<<grid, 256, 0, p.stream>>>(args);
     return hipGetLastError();
 }
@@ -162,13 +187,19 @@ template <int MODE> hipError_t launch_mode(const BlockProblem &p, const BlockArg
 
 size_t block_gemm_workspace(int mode, int groups, int64_t m, int64_t n, int64_t k)
 {
-    const Plan p = plan(mode, groups, m, n, k, SIZE_MAX);
-    return p.slices > 1 ? static_cast<size_t>(output_rows(mode, groups, m)) * n * 4 * p.slices : 0;
+    int slices = 1;
+    for (const int sums : {SUMS_POW2, SUMS_FP32})
+        for (const bool aligned : {false, true}) {
+            const Plan p = plan(mode, groups, m, n, k, sums, aligned, SIZE_MAX);
+            slices = slices > p.slices ? slices : p.slices;
+        }
+    return slices > 1 ? static_cast<size_t>(output_rows(mode, groups, m)) * n * 4 * slices : 0;
 }
 
 hipError_t launch_block_gemm(const BlockProblem &p)
 {
-    const Plan how = plan(p.mode, p.groups.count, p.m, p.n, p.k, p.workspace == nullptr ? 0 : p.workspace_bytes);
+    const int sums = p.fp32_sums ? (p.pow2 ? SUMS_FP32_POW2 : SUMS_FP32) : p.pow2 ? SUMS_POW2 : p.b_square ? SUMS_SQUARE : SUMS_ANY;
+    const Plan how = plan(p.mode, p.groups.count, p.m, p.n, p.k, sums, dma_operands(p), p.workspace == nullptr ? 0 : p.workspace_bytes);
     BlockArgs args{};
     args.A = p.A; args.lda = p.lda; args.SA = p.SA; args.ldsa = p.ldsa; args.a_shift = p.a_square ? 7 : 0;
     args.B = p.B; args.ldb = p.ldb; args.SB = p.SB; args.ldsb = p.ldsb; args.b_shift = p.b_square ? 7 : 0;
@@ -180,8 +211,8 @@ hipError_t launch_block_gemm(const BlockProblem &p)
     args.tiles_m = how.tiles_m; args.tiles_n = how.tiles_n; args.slices = how.slices;
     args.partial = how.slices > 1 ? static_cast<float *>(p.workspace) : nullptr;
     args.partial_rows = output_rows(p.mode, p.groups.count, p.m);
-    const hipError_t e = p.mode == BLOCK_DENSE ? launch_mode<BLOCK_DENSE>(p, args)
-                         : p.mode == BLOCK_ROWS ? launch_mode<BLOCK_ROWS>(p, args) : launch_mode<BLOCK_SUM>(p, args);
+    const hipError_t e = p.mode == BLOCK_DENSE ? launch_mode<BLOCK_DENSE>(p, args, sums, how.tile)
+                         : p.mode == BLOCK_ROWS ? launch_mode<BLOCK_ROWS>(p, args, sums, how.tile) : launch_mode<BLOCK_SUM>(p, args, sums, how.tile);
     if (e != hipSuccess || how.slices == 1) return e;
     const int64_t quads = args.partial_rows * ceil_div(p.n, 4);
     block_add_slices_kernel<<<static_cast<uint32_t>(ceil_div(quads, 256)), 256, 0, p.stream>>>(args);

@@ -7,8 +7,8 @@
 // adds eight products at a time on a grid of 2^-13 of the largest of them (measured: a product 2^-13 of another in its group of eight bytes counts, one
 // of 2^-14 does not, towards zero for either sign; groups and the running sum add up in FP32).  That leaves 1.5e-5 of the result for normal data and
 // 5e-5 with outliers, for any length: a fiftieth of bfloat16's rounding, a quarter of FP16's.  So these pipes serve results of 16 bits.
-// Results in FP32, and calls that ask for it, take the FP16 pipes: both operands are widened in registers, which is exact, and
-// v_mfma_f32_16x16x32_f16 adds on a grid of 2^-24, at half the rate.
+// Results in FP32, and calls that ask for it, take the FP16 or bfloat16 pipes: both operands are widened in registers, which is exact, and
+// v_mfma_f32_16x16x32 adds on a grid of 2^-24, at half the rate.
 //
 // The lanes of the instruction's first operand are rows of B, those of the second rows of A: a lane then holds four consecutive
 // columns of one row of C, and with square blocks of B (weights) the scale of B is one number for all of a fragment.
@@ -20,6 +20,7 @@
 namespace mg {
 
 typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bfloatx8 __attribute__((ext_vector_type(8)));
 
 struct BlockArgs {
     const uint8_t *A, *B;
@@ -62,9 +63,9 @@ template <int MODE, int LOG_BM, int BN> __device__ inline bool block_tile(const 
     if constexpr (MODE == BLOCK_ROWS) {
         RowTile r;
         if (!find_row_tile<LOG_BM>(args.groups, tm, &r)) return false;
-        t->group = r.group;
-        t->m0 = r.first;
-        t->m_end = r.end;
+        t->group = __builtin_amdgcn_readfirstlane(r.group);
+        t->m0 = __builtin_amdgcn_readfirstlane(static_cast<int>(r.first));
+        t->m_end = __builtin_amdgcn_readfirstlane(static_cast<int>(r.end));
     }
     if constexpr (MODE == BLOCK_SUM) {
         t->group = blockIdx.z;
@@ -83,8 +84,19 @@ template <int MODE, int LOG_BM, int BN> __device__ inline bool block_tile(const 
     return true;
 }
 
-// How a kernel sums: on the FP8 pipes with scales that are powers of two or any, or on the FP16 pipes
-enum BlockSums { SUMS_POW2 = 0, SUMS_ANY = 1, SUMS_FP32 = 2 };
+// How a kernel sums: on the FP8 pipes with scales that are powers of two or any (SUMS_SQUARE: any, and square blocks of B, so that all of a
+// fragment's rows of B have one), on the FP16 pipes with any scales, or on the bfloat16 pipes, whose operands take scales that are powers of two
+// into their exponents while they are widened
+enum BlockSums { SUMS_POW2 = 0, SUMS_ANY = 1, SUMS_FP32 = 2, SUMS_SQUARE = 3, SUMS_FP32_POW2 = 4 };
+constexpr bool sums_fp32(int sums) { return sums == SUMS_FP32 || sums == SUMS_FP32_POW2; }
+
+// Kernels for operands whose rows start on 16 bytes (block_dma_kernel.h), by their tile
+enum BlockDmaTile { DMA_256 = 0, DMA_128 = 1 };
+constexpr int block_dma_rows(int tile) { return tile == DMA_256 ? 256 : 128; }
+constexpr int block_dma_cols(int tile, int sums) { return tile == DMA_256 && !sums_fp32(sums) ? 256 : 128; }
+hipError_t launch_block_dma_dense(const BlockArgs &args, int sums, int tile, hipStream_t stream);
+hipError_t launch_block_dma_rows(const BlockArgs &args, int sums, int tile, hipStream_t stream);
+hipError_t launch_block_dma_sum(const BlockArgs &args, int sums, int tile, hipStream_t stream);
 
 // The scale of a power of two as the matrix instruction takes it: the exponent's eight bits
 __device__ inline int scale_bits(float s) { return static_cast<int>(__builtin_bit_cast(uint32_t, s) >> 23); }
@@ -108,8 +120,28 @@ struct Fp16Fragment {
         }
     }
 };
+// scaled: the lane's row of the operand has the scale `s`, a power of two
+struct Bf16Fragment {
+    bfloatx8 v[4];
+    template <int Q> __device__ inline void quarter(uint32_t lo, uint32_t hi, float s)
+    {
+        using Pair = decltype(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(0, 1.f, false));
+        const Pair two[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true),
+                             __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true)};
+        __builtin_memcpy(&v[Q], two, 16);
+    }
+    template <int Q> __device__ inline void quarter(const u32x4 (&x)[2], float s) { quarter<Q>(x[Q / 2][Q % 2 * 2], x[Q / 2][Q % 2 * 2 + 1], s); }
+    __device__ inline void set(const u32x4 (&x)[2], float s)
+    {
+        quarter<0>(x, s);
+        quarter<1>(x, s);
+        quarter<2>(x, s);
+        quarter<3>(x, s);
+    }
+};
 template <int SUMS> struct FragmentOf { using type = Fp8Fragment; };
 template <> struct FragmentOf<SUMS_FP32> { using type = Fp16Fragment; };
+template <> struct FragmentOf<SUMS_FP32_POW2> { using type = Bf16Fragment; };
 
 // acc += the block's sum times its scales; sb: the scales of the lane's four rows of B
 __device__ inline floatx4 block_sum(const Fp8Fragment &b, const Fp8Fragment &a)
@@ -128,6 +160,12 @@ template <typename F> __device__ inline void add_block(floatx4 &acc, const F &b,
     const floatx4 d = block_sum(b, a);
 #pragma unroll
     for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(d[r], sb[r] * sa, acc[r]);
+}
+// acc += d times the scales, s alone or with the four rows' of B
+template <bool ALONE> __device__ inline void scale_add(floatx4 &acc, const floatx4 &d, float s, std::integral_constant<bool, ALONE>, const u32x4 &sb)
+{
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(d[r], ALONE ? s : s * __builtin_bit_cast(floatx4, sb)[r], acc[r]);
 }
 // the same with exponents, of the lane's row of either operand
 __device__ inline void add_block_pow2(floatx4 &acc, const Fp8Fragment &b, const Fp8Fragment &a, int sb, int sa)
@@ -164,6 +202,87 @@ __device__ inline void write_block(const BlockArgs &args, int group, int64_t row
     if (args.c_type == MG_F32) write_c(static_cast<float *>(args.C) + at, valid, acc, args.alpha, args.beta);
     else if (args.c_type == MG_F16) write_c(static_cast<_Float16 *>(args.C) + at, valid, acc, args.alpha, args.beta);
     else write_c(static_cast<bfloat *>(args.C) + at, valid, acc, args.alpha, args.beta);
+}
+
+// A wavefront's FM x FN fragments to C by way of LDS: as the matrix instructions leave them, a store would reach 32 bytes of 16 rows; from LDS
+// every row's WIDTH columns leave together.  16-bit results that need no old C are rounded on the way in, others stay FP32 until they leave.  With 16
+// bytes between the rows in LDS no bank is asked twice, in either direction.  `region` is the wavefront's own.  4096 x 4096 in bfloat16 behind
+// one K-tile: 29 us stored straight from registers, 18 with FP32 in LDS and every store checked for the ends of C, 11.6 as it is (32 MB alone: 6.9).
+template <typename T, bool OLD, int FN> struct StoreRegion {
+    using Held = std::conditional_t<sizeof(T) == 2 && !OLD, T, float>;
+    static constexpr int WIDTH = FN * 16, PITCH = WIDTH * static_cast<int>(sizeof(Held)) + 16;
+    static constexpr int FRAGMENTS = 9216 / (16 * PITCH) >= 4 ? 4 : 9216 / (16 * PITCH) >= 2 ? 2 : 1;        // at a time
+};
+constexpr int STORE_REGION = 9216;
+template <typename T, bool OLD, bool WHOLE, int FM, int FN>
+__device__ __forceinline__ void store_fragments(T *c, int64_t ld, const floatx4 (&acc)[FN][FM], char *region, int64_t rows, int64_t cols, float alpha, float beta, int lane)
+{
+    using R = StoreRegion<T, OLD, FN>;
+    using Held = typename R::Held;
+    constexpr int STEP = R::FRAGMENTS < FM ? R::FRAGMENTS : FM, ROWS = STEP * 16, N = 16 / sizeof(T), ACROSS = R::WIDTH / N, DOWN = 64 / ACROSS;
+    static_assert(FM % STEP == 0 && ROWS % DOWN == 0 && ROWS * R::PITCH <= STORE_REGION, "whole passes");
+    const int col = lane % ACROSS * N;
+    const int valid = WHOLE ? N : static_cast<int>(cols - col < N ? cols - col : N);
+    T *at = c + lane / ACROSS * ld + col;
+    const int64_t step = DOWN * ld;
+#pragma unroll
+    for (int i0 = 0; i0 < FM; i0 += STEP) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < STEP; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                Piece<Held, 4> x;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x.v[r] = static_cast<Held>(alpha * acc[j][i0 + i][r]);
+                __builtin_memcpy(__builtin_assume_aligned(region + (i * 16 + lane % 16) * R::PITCH + (j * 16 + lane / 16 * 4) * sizeof(Held), 4 * sizeof(Held)), &x, sizeof(x));
+            }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r0 = 0; r0 < ROWS; r0 += DOWN, at += step) {
+            const int row = r0 + lane / ACROSS;
+            if (!WHOLE && (valid <= 0 || i0 * 16 + row >= rows)) continue;
+            Piece<Held, N> x;
+            __builtin_memcpy(&x, __builtin_assume_aligned(region + row * R::PITCH + col * sizeof(Held), 16), sizeof(x));
+            if constexpr (sizeof(T) == sizeof(Held) && !OLD) {
+                if (WHOLE || valid >= N) {
+                    *reinterpret_cast<Piece<Held, N> *>(at) = x;
+                } else {
+#pragma unroll
+                    for (int q = 0; q < N; ++q)
+                        if (q < valid) at[q] = x.v[q];
+                }
+            } else {
+                float v[N], old[N];
+                load_piece<T, N>(at, valid, old);
+#pragma unroll
+                for (int q = 0; q < N; ++q) v[q] = __builtin_fmaf(beta, old[q], x.v[q]);
+                store_piece<T, N>(at, valid, v);
+            }
+        }
+    }
+}
+template <typename T, int FM, int FN>
+__device__ __forceinline__ void store_as(T *c, int64_t ld, const floatx4 (&acc)[FN][FM], char *region, int64_t rows, int64_t cols, float alpha, float beta, int lane)
+{
+    if (beta != 0.f) store_fragments<T, true, false>(c, ld, acc, region, rows, cols, alpha, beta, lane);
+    else if (rows >= FM * 16 && cols >= FN * 16) store_fragments<T, false, true>(c, ld, acc, region, rows, cols, alpha, beta, lane);
+    else store_fragments<T, false, false>(c, ld, acc, region, rows, cols, alpha, beta, lane);
+}
+template <int FM, int FN>
+__device__ __forceinline__ void store_tile(const BlockArgs &args, const BlockTile &tile, const floatx4 (&acc)[FN][FM], char *region, int64_t row0, int64_t col0, int lane)
+{
+    const int64_t rows = tile.m_end - row0, cols = args.n - col0;
+    if (rows <= 0 || cols <= 0) return;
+    if (args.partial != nullptr) {
+        const int64_t first = static_cast<int64_t>(blockIdx.y) * args.partial_rows + (args.each_own_c ? tile.group * static_cast<int64_t>(args.m) : 0) + row0;
+        store_as(args.partial + first * args.n + col0, args.n, acc, region, rows, cols, 1.f, 0.f, lane);
+        return;
+    }
+    const int64_t at = tile.group * args.stride_c + row0 * args.ldc + col0;
+    if (args.c_type == MG_F32) store_as(static_cast<float *>(args.C) + at, args.ldc, acc, region, rows, cols, args.alpha, args.beta, lane);
+    else if (args.c_type == MG_F16) store_as(static_cast<_Float16 *>(args.C) + at, args.ldc, acc, region, rows, cols, args.alpha, args.beta, lane);
+    else store_as(static_cast<bfloat *>(args.C) + at, args.ldc, acc, region, rows, cols, args.alpha, args.beta, lane);
 }
 
 // 16 bytes of a row at any address, those from `valid` on zero and not read

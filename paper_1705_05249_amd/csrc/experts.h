@@ -184,7 +184,7 @@ template <int LOG> __device__ inline bool find_row_tile(const Groups &g, int til
             const int o = __shfl_up(sum, d);
             if (lane >= d) sum += o;
         }
-        const int total = __shfl(sum, 63);
+        const int total = __builtin_amdgcn_readfirstlane(__shfl(sum, 63));          // (the compiler has to know that all lanes go the same way)
         if (tile < before + total) {
             const uint64_t behind = __ballot(before + sum > tile);
             const int at = __ffsll(static_cast<unsigned long long>(behind)) - 1;
