@@ -395,6 +395,12 @@ template <int MODE> hipError_t launch_block_dma(const BlockArgs &args, int sums,
         if (sums == SUMS_FP32_POW2) return launch_block_dma_as<MODE, SUMS_FP32_POW2, 256, 128, 4, 2, 2>(args, stream);
         return launch_block_dma_as<MODE, SUMS_FP32, 256, 128, 4, 2, 2>(args, stream);
     }
+    if (tile == DMA_64) {
+        if (sums == SUMS_POW2) return launch_block_dma_as<MODE, SUMS_POW2, 64, 64, 2, 2, 4>(args, stream);
+        if (sums == SUMS_FP32_POW2) return launch_block_dma_as<MODE, SUMS_FP32_POW2, 64, 64, 2, 2, 4>(args, stream);
+        if (sums == SUMS_FP32) return launch_block_dma_as<MODE, SUMS_FP32, 64, 64, 2, 2, 4>(args, stream);
+        return launch_block_dma_as<MODE, SUMS_ANY, 64, 64, 2, 2, 4>(args, stream);
+    }
     if (sums == SUMS_POW2) return launch_block_dma_as<MODE, SUMS_POW2, 128, 128, 2, 2, 2>(args, stream);
     if (sums == SUMS_FP32_POW2) return launch_block_dma_as<MODE, SUMS_FP32_POW2, 128, 128, 2, 2, 2>(args, stream);
     if (sums == SUMS_FP32) return launch_block_dma_as<MODE, SUMS_FP32, 128, 128, 2, 2, 2>(args, stream);

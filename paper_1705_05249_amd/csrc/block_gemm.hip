@@ -129,10 +129,13 @@ __global__ __launch_bounds__(256) void block_add_slices_kernel(const BlockArgs a
 }
 
 constexpr int TILE_ANY = -1;                   // the kernel for operands at any address, 128 x 128
+constexpr int TILE_FEW = -2;                   // the kernel for few rows in one operand
 
 struct Plan {
-    int tile;                                 // BlockDmaTile or TILE_ANY
+    int tile;                                 // BlockDmaTile, TILE_ANY or TILE_FEW
     int tiles_m, tiles_n, slices;
+    int fragments;                            // TILE_FEW
+    bool few_b;
 };
 
 int64_t output_rows(int mode, int groups, int64_t m) { return mode == BLOCK_SUM ? groups * m : m; }
@@ -141,6 +144,14 @@ int64_t output_rows(int mode, int groups, int64_t m) { return mode == BLOCK_SUM 
 Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums, bool aligned, size_t workspace)
 {
     Plan p{};
+    p.slices = 1;
+    const int64_t few = mode == BLOCK_ROWS ? ceil_div(m, groups) : m < n ? m : n;       // rows of A (for an expert), or of the smaller operand
+    if (mode != BLOCK_SUM && few <= 32) {
+        p.tile = TILE_FEW;
+        p.few_b = mode == BLOCK_DENSE && n < m;
+        p.fragments = few <= 16 ? 1 : 2;
+        return p;
+    }
     const int64_t batch = mode == BLOCK_SUM ? groups : 1;
     auto tiles = [&](int tile) {
         const int64_t bm = tile == TILE_ANY ? 128 : block_dma_rows(tile), bn = tile == TILE_ANY ? 128 : block_dma_cols(tile, sums);
@@ -148,7 +159,7 @@ Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums, bool 
         p.tiles_n = static_cast<int>(ceil_div(n, bn));
         return (mode == BLOCK_ROWS ? ceil_div(m, bm) : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * batch;
     };
-    p.tile = !aligned ? TILE_ANY : tiles(DMA_256) >= 160 ? DMA_256 : DMA_128;
+    p.tile = !aligned ? TILE_ANY : tiles(DMA_256) >= 160 ? DMA_256 : tiles(DMA_128) >= 160 ? DMA_128 : DMA_64;
     const int64_t count = tiles(p.tile);
     const int64_t blocks = ceil_div(k, SCALE_BLOCK) / batch;
     const size_t one = static_cast<size_t>(output_rows(mode, groups, m)) * n * 4;
@@ -211,6 +222,7 @@ hipError_t launch_block_gemm(const BlockProblem &p)
     args.tiles_m = how.tiles_m; args.tiles_n = how.tiles_n; args.slices = how.slices;
     args.partial = how.slices > 1 ? static_cast<float *>(p.workspace) : nullptr;
     args.partial_rows = output_rows(p.mode, p.groups.count, p.m);
+    if (how.tile == TILE_FEW) return launch_block_few(args, p.mode, how.few_b, how.fragments, p.stream);
     const hipError_t e = p.mode == BLOCK_DENSE ? launch_mode<BLOCK_DENSE>(p, args, sums, how.tile)
                          : p.mode == BLOCK_ROWS ? launch_mode<BLOCK_ROWS>(p, args, sums, how.tile) : launch_mode<BLOCK_SUM>(p, args, sums, how.tile);
     if (e != hipSuccess || how.slices == 1) return e;

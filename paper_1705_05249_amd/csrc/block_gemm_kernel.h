@@ -91,12 +91,14 @@ enum BlockSums { SUMS_POW2 = 0, SUMS_ANY = 1, SUMS_FP32 = 2, SUMS_SQUARE = 3, SU
 constexpr bool sums_fp32(int sums) { return sums == SUMS_FP32 || sums == SUMS_FP32_POW2; }
 
 // Kernels for operands whose rows start on 16 bytes (block_dma_kernel.h), by their tile
-enum BlockDmaTile { DMA_256 = 0, DMA_128 = 1 };
-constexpr int block_dma_rows(int tile) { return tile == DMA_256 ? 256 : 128; }
-constexpr int block_dma_cols(int tile, int sums) { return tile == DMA_256 && !sums_fp32(sums) ? 256 : 128; }
+enum BlockDmaTile { DMA_256 = 0, DMA_128 = 1, DMA_64 = 2 };
+constexpr int block_dma_rows(int tile) { return tile == DMA_256 ? 256 : tile == DMA_128 ? 128 : 64; }
+constexpr int block_dma_cols(int tile, int sums) { return tile == DMA_256 && sums_fp32(sums) ? 128 : block_dma_rows(tile); }
 hipError_t launch_block_dma_dense(const BlockArgs &args, int sums, int tile, hipStream_t stream);
 hipError_t launch_block_dma_rows(const BlockArgs &args, int sums, int tile, hipStream_t stream);
 hipError_t launch_block_dma_sum(const BlockArgs &args, int sums, int tile, hipStream_t stream);
+// Few rows of A (few_b: of B), 16 * fragments for a work-group: BLOCK_DENSE or (of A) BLOCK_ROWS (block_few.hip)
+hipError_t launch_block_few(const BlockArgs &args, int mode, bool few_b, int fragments, hipStream_t stream);
 
 // The scale of a power of two as the matrix instruction takes it: the exponent's eight bits
 __device__ inline int scale_bits(float s) { return static_cast<int>(__builtin_bit_cast(uint32_t, s) >> 23); }
