@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/mg_experts.h"
 
 namespace mg {
@@ -131,12 +133,6 @@ __device__ inline uint32_t max_over_16_lanes(uint32_t v)
     return v;
 }
 
-// Magnitude of a finite number as its bits (ordered as the numbers are), 0 of others
-__device__ inline uint32_t finite_magnitude(float x)
-{
-    const uint32_t u = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
-    return u < 0x7f800000u ? u : 0u;
-}
 // The scale 2^e of a block whose largest magnitude has the bits `largest`: e is the least with largest / 2^e <= 448 = 1.75 * 2^8, -126 at least.
 // Adding 0x1fffff to the bits carries into the exponent exactly where the mantissa is above 1.75.
 __device__ inline int scale_exponent(uint32_t largest)
@@ -146,16 +142,6 @@ __device__ inline int scale_exponent(uint32_t largest)
     return e < -126 ? -126 : e;
 }
 __device__ inline float power_of_two(int e) { return __builtin_bit_cast(float, static_cast<uint32_t>(e + 127) << 23); }
-// x / 2^e to 8 bits, two at a time: the product with 2^-e is exact but for results far below e4m3's smallest step
-__device__ inline float scaled_or_nan(float x, float inverse)
-{
-    return finite_magnitude(x) == (__builtin_bit_cast(uint32_t, x) & 0x7fffffffu) ? x * inverse : __builtin_nanf("");
-}
-__device__ inline uint32_t four_e4m3(float a, float b, float c, float d)
-{
-    int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true));
-}
 
 // A tile of up to 2^LOG rows that belong to one expert
 struct RowTile {
