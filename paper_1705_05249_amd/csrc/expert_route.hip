@@ -137,94 +137,170 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(int64_t slots,
 // ---- rows --------------------------------------------------------------------------------------------------------------
 template <typename T> struct RowPiece { static constexpr int N = 16 / sizeof(T); };            // elements of 16 bytes
 
-// one thread for 16 bytes of a row
-template <typename T>
-__global__ __launch_bounds__(256) void gather_kernel(int64_t rows, int fan, int64_t cols, const T *X, int64_t ldx, const int32_t *source,
-                                                     const float *weights, T *Y, int64_t ldy, uint32_t pieces)
+// Threads of a work-group on rows of `pieces` 16-byte pieces: 2^log of them beside each other on a row, the rest on the rows behind it, and as many
+// work-groups beside each other as the row takes
+struct RowShape {
+    int log;
+    uint32_t beside;
+};
+inline RowShape row_shape(int64_t pieces)
 {
-    constexpr int N = RowPiece<T>::N;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t row = id / pieces, col = id % pieces * N;
-    if (row >= rows) return;
+    int log = 0;
+    while (log < 8 && (1 << log) < pieces) ++log;
+    return {log, static_cast<uint32_t>(ceil_div(pieces, int64_t(1) << log))};
+}
+
+// GATHER_ROWS pieces a thread, so that as many loads are in flight; without weights the bytes are moved as they are
+constexpr int GATHER_ROWS = 4;
+template <typename T, bool WEIGHTED>
+__global__ __launch_bounds__(256) void gather_kernel(int rows, int fan, int64_t cols, const T *X, int64_t ldx, const int32_t *source, const float *weights,
+                                                     T *Y, int64_t ldy, int log, uint32_t beside)
+{
+    constexpr int N = RowPiece<T>::N, U = GATHER_ROWS;
+    const int64_t col = (static_cast<int64_t>(blockIdx.x % beside << log) + (threadIdx.x & ((1 << log) - 1))) * N;
+    if (col >= cols) return;
     const int valid = static_cast<int>(cols - col < N ? cols - col : N);
-    const int slot = source[row];
-    float v[N];
+    const int per_pass = 256 >> log, first = static_cast<int>(blockIdx.x / beside) * per_pass * U + static_cast<int>(threadIdx.x >> log);
+    int slot[U];
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = 0.f;
-    if (slot >= 0 && slot < rows) {
-        load_piece<T, N>(X + slot / fan * ldx + col, valid, v);
-        if (weights != nullptr) {
-            const float w = weights[slot];
+    for (int u = 0; u < U; ++u) {
+        const int row = first + u * per_pass;
+        slot[u] = row < rows ? source[row] : -1;
+        if (slot[u] >= rows) slot[u] = -1;
+    }
+    if (valid == N && !WEIGHTED) {
+        Piece<T, N> x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            x[u] = Piece<T, N>{};
+            if (slot[u] >= 0) x[u] = *reinterpret_cast<const Piece<T, N> *>(X + slot[u] / fan * ldx + col);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = first + u * per_pass;
+            if (row < rows) *reinterpret_cast<Piece<T, N> *>(Y + row * ldy + col) = x[u];
+        }
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t row = first + u * per_pass;
+        if (row >= rows) continue;
+        float v[N];
+        load_piece<T, N>(X + (slot[u] >= 0 ? slot[u] / fan * ldx + col : 0), slot[u] >= 0 ? valid : 0, v);
+        if (WEIGHTED && slot[u] >= 0) {
+            const float w = weights[slot[u]];
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] *= w;
         }
+        store_piece<T, N>(Y + row * ldy + col, valid, v);
     }
-    store_piece<T, N>(Y + row * ldy + col, valid, v);
 }
 
+// One piece of a token's row a thread; the rows of COMBINE_SLOTS choices are on their way at a time
+constexpr int COMBINE_SLOTS = 4;
 template <typename T>
 __global__ __launch_bounds__(256) void combine_kernel(int64_t tokens, int fan, int64_t cols, const T *Y, int64_t ldy, const int32_t *position,
-                                                      const float *weights, T *O, int64_t ldo, uint32_t pieces)
+                                                      const float *weights, T *O, int64_t ldo, int log, uint32_t beside)
 {
-    constexpr int N = RowPiece<T>::N;
-    const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t token = id / pieces, col = id % pieces * N;
-    if (token >= tokens) return;
+    constexpr int N = RowPiece<T>::N, U = COMBINE_SLOTS;
+    const int64_t col = (static_cast<int64_t>(blockIdx.x % beside << log) + (threadIdx.x & ((1 << log) - 1))) * N;
+    const int64_t token = static_cast<int64_t>(blockIdx.x / beside) * (256 >> log) + (threadIdx.x >> log);
+    if (col >= cols || token >= tokens) return;
     const int valid = static_cast<int>(cols - col < N ? cols - col : N);
+    const int rows = static_cast<int>(tokens) * fan;
+    const int32_t *at = position + token * fan;
+    const float *of = weights == nullptr ? nullptr : weights + token * fan;
     float sum[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] = 0.f;
-    for (int j = 0; j < fan; ++j) {
-        const int64_t slot = token * fan + j;
-        const int row = position[slot];
-        if (row < 0 || row >= tokens * fan) continue;
-        const float w = weights != nullptr ? weights[slot] : 1.f;
-        float v[N];
-        load_piece<T, N>(Y + row * ldy + col, valid, v);
+    for (int j0 = 0; j0 < fan; j0 += U) {
+        float v[U][N], w[U];
+        int row[U];
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] = __builtin_fmaf(w, v[i], sum[i]);
+        for (int u = 0; u < U; ++u) {
+            row[u] = j0 + u < fan ? at[j0 + u] : -1;
+            if (row[u] >= rows) row[u] = -1;
+            w[u] = j0 + u < fan && of != nullptr ? of[j0 + u] : 1.f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_piece<T, N>(Y + (row[u] >= 0 ? row[u] * ldy + col : 0), row[u] >= 0 ? valid : 0, v[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (row[u] >= 0) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] = __builtin_fmaf(w[u], v[u][i], sum[i]);
+            }
     }
     store_piece<T, N>(O + token * ldo + col, valid, sum);
 }
 
-// A work-group takes a token: its row of dO is read once for all of its slots.
-template <typename T>
+// WAVES wavefronts take a token (one for short rows, so that a work-group takes four): for GRAD_SLOTS of its choices at a time they walk the row, with dO's
+// piece read once for all of them, and add up the weights' gradients in registers.
+constexpr int GRAD_SLOTS = 4;
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void combine_grad_kernel(int64_t tokens, int fan, int64_t cols, const T *dO, int64_t lddo, const T *Y, int64_t ldy,
                                                            const int32_t *position, const float *weights, T *dY, int64_t lddy, float *dweights)
 {
-    constexpr int N = RowPiece<T>::N;
-    __shared__ float part[4];
-    const int64_t token = blockIdx.x;
-    for (int j = 0; j < fan; ++j) {
-        const int64_t slot = token * fan + j;
-        const int row = position[slot];
-        const bool kept = row >= 0 && row < tokens * fan;                 // (the same in all threads)
-        float dot = 0.f;
-        if (kept) {
-            const float w = weights != nullptr ? weights[slot] : 1.f;
-            for (int64_t col = threadIdx.x * N; col < cols; col += 256 * N) {
-                const int valid = static_cast<int>(cols - col < N ? cols - col : N);
-                float g[N], y[N];
-                load_piece<T, N>(dO + token * lddo + col, valid, g);
-                if (dweights != nullptr) {
-                    load_piece<T, N>(Y + row * ldy + col, valid, y);
+    constexpr int N = RowPiece<T>::N, U = GRAD_SLOTS, THREADS = WAVES * 64;
+    __shared__ float part[4][U];
+    const int wave = threadIdx.x / 64, me = threadIdx.x % THREADS;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * (4 / WAVES) + wave / WAVES;
+    if (WAVES == 1 && token >= tokens) return;
+    const int rows = static_cast<int>(tokens) * fan;
+    for (int j0 = 0; j0 < fan; j0 += U) {
+        int row[U];
+        float w[U], dot[U];
 #pragma unroll
-                    for (int i = 0; i < N; ++i) dot = __builtin_fmaf(g[i], y[i], dot);
+        for (int u = 0; u < U; ++u) {
+            row[u] = j0 + u < fan ? position[token * fan + j0 + u] : -1;
+            if (row[u] >= rows) row[u] = -1;
+            w[u] = j0 + u < fan && weights != nullptr ? weights[token * fan + j0 + u] : 1.f;
+            dot[u] = 0.f;
+        }
+        for (int64_t col = me * N; col < cols; col += THREADS * N) {
+            const int valid = static_cast<int>(cols - col < N ? cols - col : N);
+            float g[N], y[U][N];
+            load_piece<T, N>(dO + token * lddo + col, valid, g);
+            if (dweights != nullptr) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) load_piece<T, N>(Y + (row[u] >= 0 ? row[u] * ldy + col : 0), row[u] >= 0 ? valid : 0, y[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (row[u] < 0) continue;
+                if (dweights != nullptr) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) dot[u] = __builtin_fmaf(g[i], y[u][i], dot[u]);
                 }
                 if (dY != nullptr) {
+                    float d[N];
 #pragma unroll
-                    for (int i = 0; i < N; ++i) g[i] *= w;
-                    store_piece<T, N>(dY + row * lddy + col, valid, g);
+                    for (int i = 0; i < N; ++i) d[i] = w[u] * g[i];
+                    store_piece<T, N>(dY + row[u] * lddy + col, valid, d);
                 }
             }
         }
         if (dweights == nullptr) continue;
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
-        if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = dot;
-        __syncthreads();
-        if (threadIdx.x == 0) dweights[slot] = (part[0] + part[1]) + (part[2] + part[3]);
-        __syncthreads();
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) dot[u] += __shfl_xor(dot[u], d);
+        if constexpr (WAVES > 1) {
+            if (threadIdx.x % 64 == 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) part[wave][u] = dot[u];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < U; ++u) dot[u] = (part[0][u] + part[1][u]) + (part[2][u] + part[3][u]);
+            __syncthreads();
+        }
+        if (me == 0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (j0 + u < fan) dweights[token * fan + j0 + u] = dot[u];
+        }
     }
 }
 
@@ -237,8 +313,7 @@ template <typename F> hipError_t with_type(int dtype, F &&f)
     return hipGetLastError();
 }
 
-template <typename T> uint32_t row_pieces(int64_t cols) { return static_cast<uint32_t>(ceil_div(cols, RowPiece<T>::N)); }
-uint32_t groups_of_256(int64_t threads) { return static_cast<uint32_t>(ceil_div(threads, 256)); }
+template <typename T> int64_t row_pieces(int64_t cols) { return ceil_div(cols, RowPiece<T>::N); }
 
 }  // namespace
 
@@ -276,9 +351,13 @@ hipError_t launch_expert_gather(int dtype, int64_t tokens, int fan, int64_t cols
 {
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
-        const uint32_t pieces = row_pieces<T>(cols);
-        gather_kernel<T><<<groups_of_256(tokens * fan * pieces), 256, 0, stream>>>(tokens * fan, fan, cols, static_cast<const T *>(X), ldx, source, weights,
-                                                                                   static_cast<T *>(Y), ldy, pieces);
+        const RowShape s = row_shape(row_pieces<T>(cols));
+        const int rows = static_cast<int>(tokens * fan);
+        const uint32_t grid = static_cast<uint32_t>(ceil_div(rows, (256 >> s.log) * GATHER_ROWS)) * s.beside;
+        if (weights != nullptr)
+            gather_kernel<T, true><<<grid, 256, 0, stream>>>(rows, fan, cols, static_cast<const T *>(X), ldx, source, weights, static_cast<T *>(Y), ldy, s.log, s.beside);
+        else
+            gather_kernel<T, false><<<grid, 256, 0, stream>>>(rows, fan, cols, static_cast<const T *>(X), ldx, source, weights, static_cast<T *>(Y), ldy, s.log, s.beside);
     });
 }
 
@@ -287,9 +366,9 @@ hipError_t launch_expert_combine(int dtype, int64_t tokens, int fan, int64_t col
 {
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
-        const uint32_t pieces = row_pieces<T>(cols);
-        combine_kernel<T><<<groups_of_256(tokens * pieces), 256, 0, stream>>>(tokens, fan, cols, static_cast<const T *>(Y), ldy, position, weights,
-                                                                              static_cast<T *>(O), ldo, pieces);
+        const RowShape s = row_shape(row_pieces<T>(cols));
+        combine_kernel<T><<<static_cast<uint32_t>(ceil_div(tokens, 256 >> s.log)) * s.beside, 256, 0, stream>>>(tokens, fan, cols, static_cast<const T *>(Y), ldy, position, weights,
+                                                                                                              static_cast<T *>(O), ldo, s.log, s.beside);
     });
 }
 
@@ -298,9 +377,13 @@ hipError_t launch_expert_combine_grad(int dtype, int64_t tokens, int fan, int64_
 {
     return with_type(dtype, [&](auto zero) {
         using T = decltype(zero);
-        combine_grad_kernel<T><<<static_cast<uint32_t>(tokens), 256, 0, stream>>>(tokens, fan, cols, static_cast<const T *>(dO), lddo,
-                                                                                  static_cast<const T *>(Y), ldy, position, weights, static_cast<T *>(dY),
-                                                                                  lddy, dweights);
+        // one wavefront for a token where it holds the row in two pieces a lane
+        if (row_pieces<T>(cols) <= 128)
+            combine_grad_kernel<T, 1><<<static_cast<uint32_t>(ceil_div(tokens, 4)), 256, 0, stream>>>(tokens, fan, cols, static_cast<const T *>(dO), lddo, static_cast<const T *>(Y),
+                                                                                                     ldy, position, weights, static_cast<T *>(dY), lddy, dweights);
+        else
+            combine_grad_kernel<T, 4><<<static_cast<uint32_t>(tokens), 256, 0, stream>>>(tokens, fan, cols, static_cast<const T *>(dO), lddo, static_cast<const T *>(Y), ldy, position,
+                                                                                         weights, static_cast<T *>(dY), lddy, dweights);
     });
 }
 
