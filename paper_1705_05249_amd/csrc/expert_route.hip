@@ -10,8 +10,9 @@ namespace mg {
 namespace {
 
 // ---- sort --------------------------------------------------------------------------------------------------------------
-constexpr int SORT_THREADS = 1024, SORT_WAVES = 16;
-constexpr int SORT_CHUNK = 8192;                 // slots of a work-group: 512 for each wavefront
+constexpr int SORT_KEYS = 4;                     // slots of a lane, 64 apart
+constexpr int SORT_WAVES = 16;
+constexpr int SORT_CHUNK = SORT_WAVES * 64 * SORT_KEYS;          // slots of a work-group
 constexpr int SORT_ROW = MG_MOST_GROUPS + 1;     // experts and, behind them, the dropped slots
 
 // Lanes with the same key, as a mask (keys below 2^bits; all 64 lanes take part)
@@ -28,7 +29,7 @@ __device__ inline uint64_t same_key(int key, int bits)
 // Sum over a work-group's threads in front of this one; `total`: over all of them
 __device__ inline int sum_before(int v, int *scratch, int *total)
 {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
     int sum = v;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -38,7 +39,7 @@ __device__ inline int sum_before(int v, int *scratch, int *total)
     if (lane == 63) scratch[wave] = sum;
     __syncthreads();
     int before = 0, all = 0;
-    for (int w = 0; w < SORT_WAVES; ++w) {
+    for (int w = 0; w < waves; ++w) {
         if (w < wave) before += scratch[w];
         all += scratch[w];
     }
@@ -56,54 +57,62 @@ __device__ inline int slot_key(const int32_t *ids, int64_t i, int64_t end, int e
 }
 
 // counts[chunk][key] of a chunk of slots
-__global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(int64_t slots, int experts, const int32_t *ids, int32_t *counts)
+__global__ __launch_bounds__(SORT_WAVES * 64) void sort_count_kernel(int64_t slots, int experts, const int32_t *ids, int32_t *counts)
 {
-    __shared__ int count[SORT_ROW];
-    for (int e = threadIdx.x; e <= experts; e += SORT_THREADS) count[e] = 0;
+    __shared__ int count[SORT_ROW + 1];
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * SORT_CHUNK + threadIdx.x;
+    int key[SORT_KEYS];
+#pragma unroll
+    for (int q = 0; q < SORT_KEYS; ++q) key[q] = slot_key(ids, first + q * (SORT_WAVES * 64), slots, experts);
+    for (int e = threadIdx.x; e <= experts; e += SORT_WAVES * 64) count[e] = 0;
     __syncthreads();
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * SORT_CHUNK, end = first + SORT_CHUNK < slots ? first + SORT_CHUNK : slots;
-    for (int64_t i = first + threadIdx.x; i < end; i += SORT_THREADS) atomicAdd(&count[slot_key(ids, i, end, experts)], 1);     // (whole numbers: any order)
+#pragma unroll
+    for (int q = 0; q < SORT_KEYS; ++q) atomicAdd(&count[key[q]], 1);               // (whole numbers: any order)
     __syncthreads();
-    for (int e = threadIdx.x; e <= experts; e += SORT_THREADS) counts[static_cast<int64_t>(blockIdx.x) * (experts + 1) + e] = count[e];
+    for (int e = threadIdx.x; e <= experts; e += SORT_WAVES * 64) counts[static_cast<int64_t>(blockIdx.x) * (experts + 1) + e] = count[e];
 }
 
-// Rows of a chunk's slots.  counts null: the call's only chunk, counted here.
-__global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(int64_t slots, int experts, const int32_t *ids, const int32_t *counts, int chunks,
-                                                                  int32_t *offsets, int32_t *position, int32_t *source)
+// Rows of a chunk's slots; a wavefront has 64 SORT_KEYS of them in a row.  counts null: the call's only chunk, counted here.
+__global__ __launch_bounds__(SORT_WAVES * 64) void sort_place_kernel(int64_t slots, int experts, const int32_t *ids, const int32_t *counts, int chunks,
+                                                                     int32_t *offsets, int32_t *position, int32_t *source)
 {
-    extern __shared__ int next[];                 // [wave][key]: the row of the wavefront's next slot of that key
+    extern __shared__ int next[];                 // [wave][key]: how many slots of that key the wavefront has, then the row of its first one
     __shared__ int scratch[SORT_WAVES];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, keys = experts + 1;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64, keys = experts + 1;
     const int bits = 32 - __builtin_clz(experts + 1);
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * SORT_CHUNK;
-    const int64_t end = first + SORT_CHUNK < slots ? first + SORT_CHUNK : slots;
-    const int64_t each = ((end - first + SORT_WAVES - 1) / SORT_WAVES + 63) / 64 * 64;
-    const int64_t mine = first + wave * each, mine_end = mine + each < end ? mine + each : end;
+    const int64_t mine = static_cast<int64_t>(blockIdx.x) * SORT_CHUNK + wave * (64 * SORT_KEYS) + lane;
     const uint64_t below = (uint64_t(1) << lane) - 1;
 
-    for (int i = threadIdx.x; i < SORT_WAVES * keys; i += SORT_THREADS) next[i] = 0;
+    int key[SORT_KEYS], rank[SORT_KEYS];
+#pragma unroll
+    for (int q = 0; q < SORT_KEYS; ++q) key[q] = slot_key(ids, mine + 64 * q, slots, experts);
+    for (int i = threadIdx.x; i < waves * keys; i += blockDim.x) next[i] = 0;
     __syncthreads();
-    for (int64_t i = mine; i < mine_end; i += 64) {
-        const int key = slot_key(ids, i + lane, mine_end, experts);
-        const uint64_t same = same_key(key, bits);
-        if (key < keys && (same & below) == 0) next[wave * keys + key] += __popcll(same);        // (one lane for each key)
+#pragma unroll
+    for (int q = 0; q < SORT_KEYS; ++q) {
+        const uint64_t same = same_key(key[q], bits);
+        const int earlier = key[q] < keys ? next[wave * keys + key[q]] : 0;
+        __builtin_amdgcn_wave_barrier();
+        rank[q] = earlier + __popcll(same & below);
+        if (key[q] < keys && (same & below) == 0) next[wave * keys + key[q]] = earlier + __popcll(same);       // (one lane for each key)
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
-    // thread e: rows in front of key e's, and of this chunk's share of them; MG_MOST_GROUPS + 1 keys take two rounds
+    // thread e: rows in front of key e's, and of this chunk's share of them
     int carried = 0;
-    for (int base = 0; base < keys; base += SORT_THREADS) {
+    for (int base = 0; base < keys; base += blockDim.x) {
         const int e = base + threadIdx.x;
         int all = 0, earlier = 0;
         if (e < keys) {
             if (counts != nullptr) {
+#pragma unroll 8
                 for (int c = 0; c < chunks; ++c) {
                     const int v = counts[static_cast<int64_t>(c) * keys + e];
                     all += v;
-                    if (c < static_cast<int>(blockIdx.x)) earlier += v;
+                    earlier += c < static_cast<int>(blockIdx.x) ? v : 0;
                 }
             } else {
-                for (int w = 0; w < SORT_WAVES; ++w) all += next[w * keys + e];
+                for (int w = 0; w < waves; ++w) all += next[w * keys + e];
             }
         }
         int total;
@@ -111,7 +120,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(int64_t slots,
         carried += total;
         if (e < keys) {
             int at = before + earlier;
-            for (int w = 0; w < SORT_WAVES; ++w) {
+            for (int w = 0; w < waves; ++w) {
                 const int v = next[w * keys + e];
                 next[w * keys + e] = at;
                 at += v;
@@ -120,17 +129,13 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_place_kernel(int64_t slots,
         }
     }
     __syncthreads();
-    for (int64_t i = mine; i < mine_end; i += 64) {
-        const int key = slot_key(ids, i + lane, mine_end, experts);
-        const uint64_t same = same_key(key, bits);
-        const int row = key < keys ? next[wave * keys + key] + __popcll(same & below) : 0;
-        __builtin_amdgcn_wave_barrier();
-        if (key < keys && (same & below) == 0) next[wave * keys + key] = row + __popcll(same);
-        __builtin_amdgcn_wave_barrier();
-        if (key < keys) {
-            position[i + lane] = key < experts ? row : -1;
-            source[row] = key < experts ? static_cast<int32_t>(i + lane) : -1;
-        }
+#pragma unroll
+    for (int q = 0; q < SORT_KEYS; ++q) {
+        if (key[q] >= keys) continue;
+        const int row = next[wave * keys + key[q]] + rank[q];
+        const bool kept = key[q] < experts;
+        position[mine + 64 * q] = kept ? row : -1;
+        source[row] = kept ? static_cast<int32_t>(mine + 64 * q) : -1;
     }
 }
 
@@ -148,6 +153,15 @@ inline RowShape row_shape(int64_t pieces)
     int log = 0;
     while (log < 8 && (1 << log) < pieces) ++log;
     return {log, static_cast<uint32_t>(ceil_div(pieces, int64_t(1) << log))};
+}
+
+// 16 bytes that nobody reads soon
+template <typename T, int N> __device__ inline void store_streaming(T *p, const Piece<T, N> &x)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+    words w;
+    __builtin_memcpy(&w, &x, 16);
+    __builtin_nontemporal_store(w, reinterpret_cast<words *>(p));
 }
 
 // GATHER_ROWS pieces a thread, so that as many loads are in flight; without weights the bytes are moved as they are
@@ -178,7 +192,7 @@ __global__ __launch_bounds__(256) void gather_kernel(int rows, int fan, int64_t 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = first + u * per_pass;
-            if (row < rows) *reinterpret_cast<Piece<T, N> *>(Y + row * ldy + col) = x[u];
+            if (row < rows) store_streaming(Y + row * ldy + col, x[u]);
         }
         return;
     }
@@ -330,11 +344,14 @@ hipError_t launch_expert_sort(int64_t tokens, int fan, int experts, const int32_
     const int chunks = static_cast<int>(ceil_div(slots, SORT_CHUNK));
     int32_t *counts = chunks > 1 ? static_cast<int32_t *>(workspace) : nullptr;
     if (counts != nullptr) {
-        sort_count_kernel<<<chunks, SORT_THREADS, 0, stream>>>(slots, experts, ids, counts);
+        sort_count_kernel<<<chunks, SORT_WAVES * 64, 0, stream>>>(slots, experts, ids, counts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const size_t lds = static_cast<size_t>(SORT_WAVES) * (experts + 1) * sizeof(int);
+    // a short call in as few wavefronts as its slots and its experts keep busy
+    const int64_t wanted = ceil_div(slots, 64 * SORT_KEYS) > ceil_div(experts + 1, 256) ? ceil_div(slots, 64 * SORT_KEYS) : ceil_div(experts + 1, 256);
+    const int waves = static_cast<int>(wanted < SORT_WAVES ? wanted : SORT_WAVES);
+    const size_t lds = static_cast<size_t>(waves) * (experts + 1) * sizeof(int);
     static bool raised = false;                   // raising the limit twice is harmless
     if (lds > 48 * 1024 && !raised) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(sort_place_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -342,7 +359,7 @@ hipError_t launch_expert_sort(int64_t tokens, int fan, int experts, const int32_
         if (e != hipSuccess) return e;
         raised = true;
     }
-    sort_place_kernel<<<chunks > 0 ? chunks : 1, SORT_THREADS, lds, stream>>>(slots, experts, ids, counts, chunks, offsets, position, source);
+    sort_place_kernel<<<chunks > 0 ? chunks : 1, waves * 64, lds, stream>>>(slots, experts, ids, counts, chunks, offsets, position, source);
     return hipGetLastError();
 }
 
