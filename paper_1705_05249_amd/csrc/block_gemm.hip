@@ -6,23 +6,23 @@
 namespace mg {
 namespace {
 
-// ---- operands at any address: 128 x 128 tiles, staged through registers.  LDS rows of 128 bytes as in lds_layout.h (16-row fragments).
-template <int MODE, int SUMS> __global__ __launch_bounds__(256) void block_any_kernel(const BlockArgs args)
+// ---- operands at any address: SIZE x SIZE tiles (128, or 64 where those would leave compute units idle), staged through registers.  LDS rows of 128 bytes as in lds_layout.h (16-row fragments).
+template <int MODE, int SUMS, int SIZE> __global__ __launch_bounds__(256) void block_any_kernel(const BlockArgs args)
 {
-    constexpr int BM = 128, BN = 128, FM = 4, FN = 4;
+    constexpr int BM = SIZE, BN = SIZE, HALF = SIZE / 2, FM = HALF / 16, FN = HALF / 16, PIECES = SIZE / 32;
     __shared__ __attribute__((aligned(1024))) uint8_t lds_a[BM * 128], lds_b[BN * 128];
     __shared__ __attribute__((aligned(16))) float scale_a[BM], scale_b[BN];
     BlockTile tile;
-    if (!block_tile<MODE, 7, BN>(args, &tile)) return;
+    if (!block_tile<MODE, SIZE == 128 ? 7 : 6, BN>(args, &tile)) return;
     const int t = threadIdx.x, lane = t % 64, wave = t / 64, wm = wave % 2, wn = wave / 2;
     const uint8_t *const B = args.B + (MODE == BLOCK_ROWS ? tile.group * args.stride_b : 0);
     const float *const SB = args.SB + (MODE == BLOCK_ROWS ? tile.group * args.stride_sb : 0);
 
-    // this thread's piece of four rows of each operand; rows that do not exist: the tile's first, whose products nobody stores
+    // this thread's piece of PIECES rows of each operand; rows that do not exist: the tile's first, whose products nobody stores
     const int piece = t % 8;
-    const uint8_t *from_a[4], *from_b[4];
+    const uint8_t *from_a[PIECES], *from_b[PIECES];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < PIECES; ++i) {
         const int r = t / 8 + 32 * i;
         const int64_t row = tile.m0 + r < tile.m_end ? tile.m0 + r : tile.m0;
         from_a[i] = args.A + (MODE == BLOCK_ROWS ? source_row(args.groups, row) : row) * args.lda + tile.column + 16 * piece;
@@ -30,8 +30,8 @@ template <int MODE, int SUMS> __global__ __launch_bounds__(256) void block_any_k
     }
     const float *from_s;
     {
-        const int r = t % 128;
-        if (t < 128) {
+        const int r = t % SIZE;                    // (of 64 x 64 tiles the upper two wavefronts repeat the lower ones)
+        if (t / SIZE % 2 == 0) {
             const int64_t row = tile.m0 + r < tile.m_end ? tile.m0 + r : tile.m0;
             from_s = args.SA + ((MODE == BLOCK_ROWS ? source_row(args.groups, row) : row) >> args.a_shift) * args.ldsa;
         } else {
@@ -46,14 +46,14 @@ template <int MODE, int SUMS> __global__ __launch_bounds__(256) void block_any_k
 #pragma unroll
         for (int i = 0; i < FM; ++i) acc[j][i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    u32x4 next_a[4], next_b[4];
+    u32x4 next_a[PIECES], next_b[PIECES];
     float next_s = 0.f;
     auto fetch = [&](int b) {
         const int64_t at = static_cast<int64_t>(b) * SCALE_BLOCK;
         const int64_t left = tile.k - at - 16 * piece;
         const int valid = static_cast<int>(left < 16 ? left : 16);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < PIECES; ++i) {
             next_a[i] = load_bytes16(from_a[i] + at, valid);
             next_b[i] = load_bytes16(from_b[i] + at, valid);
         }
@@ -63,26 +63,26 @@ template <int MODE, int SUMS> __global__ __launch_bounds__(256) void block_any_k
     for (int b = tile.b0; b < tile.b_end; ++b) {
         __syncthreads();                                   // the block before has been read
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < PIECES; ++i) {
             const int at = ldsmap::kcontig_slot<16>(t / 8 + 32 * i, piece);
             *reinterpret_cast<u32x4 *>(lds_a + at) = next_a[i];
             *reinterpret_cast<u32x4 *>(lds_b + at) = next_b[i];
         }
-        (t < 128 ? scale_a : scale_b)[t % 128] = next_s;
+        (t / SIZE % 2 == 0 ? scale_a : scale_b)[t % SIZE] = next_s;
         __syncthreads();
         if (b + 1 < tile.b_end) fetch(b + 1);
         typename FragmentOf<SUMS>::type fa[FM], fb;
         float sa[FM];
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const int row = 64 * wm + 16 * i + lane % 16;
+            const int row = HALF * wm + 16 * i + lane % 16;
             fa[i].set(join(*reinterpret_cast<const u32x4 *>(lds_a + ldsmap::kcontig_slot<16>(row, lane / 16)),
                            *reinterpret_cast<const u32x4 *>(lds_a + ldsmap::kcontig_slot<16>(row, lane / 16 + 4))));
             sa[i] = scale_a[row];
         }
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-            const int row = 64 * wn + 16 * j + lane % 16;
+            const int row = HALF * wn + 16 * j + lane % 16;
             fb.set(join(*reinterpret_cast<const u32x4 *>(lds_b + ldsmap::kcontig_slot<16>(row, lane / 16)),
                         *reinterpret_cast<const u32x4 *>(lds_b + ldsmap::kcontig_slot<16>(row, lane / 16 + 4))));
             if constexpr (SUMS == SUMS_POW2) {
@@ -90,7 +90,7 @@ template <int MODE, int SUMS> __global__ __launch_bounds__(256) void block_any_k
 #pragma unroll
                 for (int i = 0; i < FM; ++i) add_block_pow2(acc[j][i], fb, fa[i], sb, scale_bits(sa[i]));
             } else {
-                const floatx4 sb = *reinterpret_cast<const floatx4 *>(scale_b + 64 * wn + 16 * j + 4 * (lane / 16));
+                const floatx4 sb = *reinterpret_cast<const floatx4 *>(scale_b + HALF * wn + 16 * j + 4 * (lane / 16));
 #pragma unroll
                 for (int i = 0; i < FM; ++i) add_block(acc[j][i], fb, fa[i], sb, sa[i]);
             }
@@ -98,10 +98,10 @@ template <int MODE, int SUMS> __global__ __launch_bounds__(256) void block_any_k
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-        const int64_t row = tile.m0 + 64 * wm + 16 * i + lane % 16;
+        const int64_t row = tile.m0 + HALF * wm + 16 * i + lane % 16;
         if (row < tile.m_end) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) write_block(args, tile.group, row, tile.n0 + 64 * wn + 16 * j + 4 * (lane / 16), acc[j][i]);
+            for (int j = 0; j < FN; ++j) write_block(args, tile.group, row, tile.n0 + HALF * wn + 16 * j + 4 * (lane / 16), acc[j][i]);
         }
     }
 }
@@ -128,11 +128,11 @@ __global__ __launch_bounds__(256) void block_add_slices_kernel(const BlockArgs a
     write_block(whole, many ? static_cast<int>(row / args.m) : 0, many ? row % args.m : row, col, sum);
 }
 
-constexpr int TILE_ANY = -1;                   // the kernel for operands at any address, 128 x 128
-constexpr int TILE_FEW = -2;                   // the kernel for few rows in one operand
+constexpr int TILE_ANY = -1, TILE_ANY_64 = -2; // the kernel for operands at any address
+constexpr int TILE_FEW = -3;                   // the kernel for few rows in one operand
 
 struct Plan {
-    int tile;                                 // BlockDmaTile, TILE_ANY or TILE_FEW
+    int tile;                                 // BlockDmaTile or one of those
     int tiles_m, tiles_n, slices;
     int fragments;                            // TILE_FEW
     bool few_b;
@@ -154,12 +154,12 @@ Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums, bool 
     }
     const int64_t batch = mode == BLOCK_SUM ? groups : 1;
     auto tiles = [&](int tile) {
-        const int64_t bm = tile == TILE_ANY ? 128 : block_dma_rows(tile), bn = tile == TILE_ANY ? 128 : block_dma_cols(tile, sums);
+        const int64_t any = tile == TILE_ANY ? 128 : 64, bm = tile < 0 ? any : block_dma_rows(tile), bn = tile < 0 ? any : block_dma_cols(tile, sums);
         p.tiles_m = static_cast<int>(ceil_div(m, bm) + (mode == BLOCK_ROWS ? groups : 0));
         p.tiles_n = static_cast<int>(ceil_div(n, bn));
         return (mode == BLOCK_ROWS ? ceil_div(m, bm) : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * batch;
     };
-    p.tile = !aligned ? TILE_ANY : tiles(DMA_256) >= 160 ? DMA_256 : tiles(DMA_128) >= 160 ? DMA_128 : DMA_64;
+    p.tile = !aligned ? (tiles(TILE_ANY) >= 160 ? TILE_ANY : TILE_ANY_64) : tiles(DMA_256) >= 160 ? DMA_256 : tiles(DMA_128) >= 160 ? DMA_128 : DMA_64;
     const int64_t count = tiles(p.tile);
     const int64_t blocks = ceil_div(k, SCALE_BLOCK) / batch;
     const size_t one = static_cast<size_t>(output_rows(mode, groups, m)) * n * 4;
@@ -182,15 +182,20 @@ bool dma_operands(const BlockProblem &p)
 
 template <int MODE> hipError_t launch_mode(const BlockProblem &p, const BlockArgs &args, int sums, int tile)
 {
-    if (tile != TILE_ANY) {
+    if (tile >= 0) {
         if constexpr (MODE == BLOCK_DENSE) return launch_block_dma_dense(args, sums, tile, p.stream);
         else if constexpr (MODE == BLOCK_ROWS) return launch_block_dma_rows(args, sums, tile, p.stream);
         else return launch_block_dma_sum(args, sums, tile, p.stream);
     }
     const dim3 grid(static_cast<uint32_t>(args.tiles_m) * args.tiles_n, args.slices, MODE == BLOCK_SUM ? p.groups.count : 1);
-    if (sums_fp32(sums)) block_any_kernel<MODE, SUMS_FP32><<<grid, 256, 0, p.stream>>>(args);
-    else if (sums == SUMS_POW2) block_any_kernel<MODE, SUMS_POW2><<<grid, 256, 0, p.stream>>>(args);
-    else block_any_kernel<MODE, SUMS_ANY><<<grid, 256, 0, p.stream>>>(args);
+    auto launch = [&](auto size) {
+        constexpr int SIZE = decltype(size)::value;
+        if (sums_fp32(sums)) block_any_kernel<MODE, SUMS_FP32, SIZE><<<grid, 256, 0, p.stream>>>(args);
+        else if (sums == SUMS_POW2) block_any_kernel<MODE, SUMS_POW2, SIZE><<<grid, 256, 0, p.stream>>>(args);
+        else block_any_kernel<MODE, SUMS_ANY, SIZE><<<grid, 256, 0, p.stream>>>(args);
+    };
+    if (tile == TILE_ANY) launch(std::integral_constant<int, 128>{});
+    else launch(std::integral_constant<int, 64>{});
     return hipGetLastError();
 }
 
