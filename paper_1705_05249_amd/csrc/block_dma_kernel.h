@@ -328,7 +328,7 @@ __global__ __launch_bounds__(WM *WN * 64) void block_dma_kernel(const BlockArgs 
             const bool of_a = p < BM * 8;
             const int r = p / 8 - (of_a ? 0 : BM), piece = p % 8;
             const uint8_t *from = of_a ? args.A + (first_a + row_a(r)) * args.lda : B + (tile.n0 + (r < rows_b ? r : rows_b - 1)) * args.ldb;
-            *reinterpret_cast<u32x4 *>(lds + (of_a ? 0 : B_AT) + ldsmap::kcontig_slot<16>(r, piece)) = load_bytes16(from + tile.column + at + 16 * piece, left - 16 * piece);
+            *reinterpret_cast<u32x4 *>(lds + (of_a ? 0 : B_AT) + ldsmap::kcontig_slot<16>(r, piece)) = load_aligned16(from + tile.column + at + 16 * piece, left - 16 * piece);
         }
         float *const scales = reinterpret_cast<float *>(lds + S_AT);
         for (int r = threadIdx.x; r < BM + BN; r += W * 64) {

@@ -10,7 +10,9 @@ namespace {
 template <int MODE, int SUMS, int SIZE> __global__ __launch_bounds__(256) void block_any_kernel(const BlockArgs args)
 {
     constexpr int BM = SIZE, BN = SIZE, HALF = SIZE / 2, FM = HALF / 16, FN = HALF / 16, PIECES = SIZE / 32;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds_a[BM * 128], lds_b[BN * 128];
+    constexpr int OPERANDS = (BM + BN) * 128, STORES = 4 * STORE_REGION;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds_a[OPERANDS > STORES ? OPERANDS : STORES];
+    uint8_t *const lds_b = lds_a + BM * 128;
     __shared__ __attribute__((aligned(16))) float scale_a[BM], scale_b[BN];
     BlockTile tile;
     if (!block_tile<MODE, SIZE == 128 ? 7 : 6, BN>(args, &tile)) return;
@@ -46,31 +48,34 @@ template <int MODE, int SUMS, int SIZE> __global__ __launch_bounds__(256) void b
 #pragma unroll
         for (int i = 0; i < FM; ++i) acc[j][i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    u32x4 next_a[PIECES], next_b[PIECES];
-    float next_s = 0.f;
-    auto fetch = [&](int b) {
+    // K-tiles on their way in registers, one more in LDS.  (Two of 128 x 128 take the registers of a second work-group: 57 -> 66 us for 2000 x 3001 x 1999.)
+    constexpr int SETS = SIZE == 128 ? 1 : 2;
+    struct Fetched {
+        u32x4 a[PIECES], b[PIECES];
+        float s;
+    } fetched[SETS];
+    auto fetch = [&](int b, Fetched &next) {
         const int64_t at = static_cast<int64_t>(b) * SCALE_BLOCK;
         const int64_t left = tile.k - at - 16 * piece;
         const int valid = static_cast<int>(left < 16 ? left : 16);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            next_a[i] = load_bytes16(from_a[i] + at, valid);
-            next_b[i] = load_bytes16(from_b[i] + at, valid);
+            next.a[i] = load_bytes16(from_a[i] + at, valid);
+            next.b[i] = load_bytes16(from_b[i] + at, valid);
         }
-        next_s = from_s[b];
+        next.s = from_s[b];
     };
-    if (tile.b0 < tile.b_end) fetch(tile.b0);
-    for (int b = tile.b0; b < tile.b_end; ++b) {
+    auto multiply = [&](int b, Fetched &next) {
         __syncthreads();                                   // the block before has been read
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int at = ldsmap::kcontig_slot<16>(t / 8 + 32 * i, piece);
-            *reinterpret_cast<u32x4 *>(lds_a + at) = next_a[i];
-            *reinterpret_cast<u32x4 *>(lds_b + at) = next_b[i];
+            *reinterpret_cast<u32x4 *>(lds_a + at) = next.a[i];
+            *reinterpret_cast<u32x4 *>(lds_b + at) = next.b[i];
         }
-        (t / SIZE % 2 == 0 ? scale_a : scale_b)[t % SIZE] = next_s;
+        (t / SIZE % 2 == 0 ? scale_a : scale_b)[t % SIZE] = next.s;
         __syncthreads();
-        if (b + 1 < tile.b_end) fetch(b + 1);
+        if (b + SETS < tile.b_end) fetch(b + SETS, next);
         typename FragmentOf<SUMS>::type fa[FM], fb;
         float sa[FM];
 #pragma unroll
@@ -95,15 +100,16 @@ template <int MODE, int SUMS, int SIZE> __global__ __launch_bounds__(256) void b
                 for (int i = 0; i < FM; ++i) add_block(acc[j][i], fb, fa[i], sb, sa[i]);
             }
         }
-    }
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int64_t row = tile.m0 + HALF * wm + 16 * i + lane % 16;
-        if (row < tile.m_end) {
-#pragma unroll
-            for (int j = 0; j < FN; ++j) write_block(args, tile.group, row, tile.n0 + HALF * wn + 16 * j + 4 * (lane / 16), acc[j][i]);
-        }
-    }
+    };
+    static_for<SETS>([&](auto S) {
+        if (tile.b0 + decltype(S)::value < tile.b_end) fetch(tile.b0 + decltype(S)::value, fetched[decltype(S)::value]);
+    });
+    for (int b = tile.b0; b < tile.b_end; b += SETS)
+        static_for<SETS>([&](auto S) {
+            if (b + decltype(S)::value < tile.b_end) multiply(b + decltype(S)::value, fetched[decltype(S)::value]);
+        });
+    __syncthreads();
+    store_tile(args, tile, acc, reinterpret_cast<char *>(lds_a) + wave * STORE_REGION, tile.m0 + HALF * wm, tile.n0 + HALF * wn, lane);
 }
 
 // ---- C = alpha * (sum of the slices) + beta * C

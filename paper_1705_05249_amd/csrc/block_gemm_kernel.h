@@ -287,15 +287,36 @@ __device__ __forceinline__ void store_tile(const BlockArgs &args, const BlockTil
     else store_as(static_cast<bfloat *>(args.C) + at, args.ldc, acc, region, rows, cols, args.alpha, args.beta, lane);
 }
 
-// 16 bytes of a row at any address, those from `valid` on zero and not read
+// The first `valid` of 16 bytes, zeros behind them
+__device__ inline u32x4 first_bytes(u32x4 x, int valid)
+{
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const int bits = (valid - 4 * d) * 8;                    // of this word, from its low end
+        x[d] &= bits <= 0 ? 0u : bits >= 32 ? ~0u : (1u << bits) - 1;
+    }
+    return x;
+}
+// 16 bytes of a row at any address, those from `valid` on zero.  A row's last piece is read word by word, each word on four bytes and with a byte of the row in it.
 __device__ inline u32x4 load_bytes16(const uint8_t *p, int valid)
 {
     if (valid >= 16) return __builtin_bit_cast(u32x4, *reinterpret_cast<const Piece<uint8_t, 16> *>(p));
-    u32x4 r{0u, 0u, 0u, 0u};
+    if (valid <= 0) return u32x4{0u, 0u, 0u, 0u};
+    const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 3);
+    const uint32_t *words = reinterpret_cast<const uint32_t *>(p - skew);
+    uint32_t w[5];
 #pragma unroll
-    for (int i = 0; i < 15; ++i)
-        if (i < valid) r[i / 4] |= static_cast<uint32_t>(p[i]) << (8 * (i % 4));
-    return r;
+    for (int d = 0; d < 5; ++d) w[d] = 4 * d < skew + valid ? words[d] : 0u;
+    u32x4 r;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) r[d] = __builtin_amdgcn_alignbyte(w[d + 1], w[d], skew);
+    return first_bytes(r, valid);
+}
+// The same from an address on 16 bytes, where a piece with a byte of the row in it may be read whole
+__device__ inline u32x4 load_aligned16(const uint8_t *p, int valid)
+{
+    if (valid <= 0) return u32x4{0u, 0u, 0u, 0u};
+    return first_bytes(*reinterpret_cast<const u32x4 *>(p), valid);
 }
 
 }  // namespace mg
