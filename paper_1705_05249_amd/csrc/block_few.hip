@@ -1,8 +1,8 @@
 // Products with few rows in one operand (the tokens that are being generated): the other operand, the weights, is read once and little else counts.
 //
 // A work-group takes 16 rows of the weights and up to 16 TF of the few; its eight wavefronts share the sum, each every eighth block
-// of 128, straight from memory into registers (a fragment of 16 x 128 bytes is 32 bytes for each lane, four lanes to a row's 128), the next block's
-// loads in flight during the instructions of this one.  The wavefronts' sums meet in LDS and are added in their order.  Memory leaves the matrix pipes
+// of 128, straight from memory into registers (a fragment of 16 x 128 bytes is 32 bytes for each lane, four lanes to a row's 128): four blocks of the
+// weights on their way at a time, 128 KB for a compute unit, and two of the few, which come from the caches.  The wavefronts' sums meet in LDS and are added in their order.  Memory leaves the matrix pipes
 // nine tenths idle, so the sums are always FP32's (operands widened to FP16).
 #include "internal.h"
 #include "block_gemm_kernel.h"
@@ -32,7 +32,7 @@ template <typename T> __device__ inline void write_one(T *c, float v, float alph
     *c = static_cast<T>(v);
 }
 
-template <int MODE, int TF> __global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(const FewArgs args)
+template <int MODE, int TF, typename FRAGMENT> __global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(const FewArgs args)
 {
     constexpr int FEW = 16 * TF, PITCH = 20;                              // floats between the rows of a sum in LDS
     __shared__ __attribute__((aligned(16))) float sums[FEW_WAVES][FEW * PITCH];
@@ -40,7 +40,7 @@ template <int MODE, int TF> __global__ __launch_bounds__(FEW_WAVES * 64) void bl
     int64_t first = static_cast<int64_t>(blockIdx.y) * FEW, end = args.rows_few, group = 0;
     if constexpr (MODE == BLOCK_ROWS) {
         RowTile tile;
-        if (!find_row_tile<TF == 1 ? 4 : TF == 2 ? 5 : 6>(args.groups, blockIdx.y, &tile)) return;
+        if (!find_row_tile<TF == 1 ? 4 : 5>(args.groups, blockIdx.y, &tile)) return;
         first = __builtin_amdgcn_readfirstlane(static_cast<int>(tile.first));
         end = __builtin_amdgcn_readfirstlane(static_cast<int>(tile.end));
         group = __builtin_amdgcn_readfirstlane(tile.group);
@@ -69,55 +69,67 @@ template <int MODE, int TF> __global__ __launch_bounds__(FEW_WAVES * 64) void bl
     floatx4 acc[TF];
 #pragma unroll
     for (int f = 0; f < TF; ++f) acc[f] = floatx4{0.f, 0.f, 0.f, 0.f};
-    struct Block {
-        u32x4 many[2], few[TF][2];
-        float s_many[4], s_few[TF];
+    struct Many {
+        u32x4 x[2];
+        float s[4];
     };
-    auto fetch = [&](int b, Block &x) {
+    struct Few {
+        u32x4 x[TF][2];
+        float s[TF];
+    };
+    // block b of either operand; WHOLE: not the end of a sum that is no multiple of 128
+    auto fetch_many = [&](int b, Many &m, auto whole) {
         const int64_t at = static_cast<int64_t>(b) * SCALE_BLOCK;
-        const int64_t left = args.k - at - lane / 16 * 16;
-        if (args.k - at >= SCALE_BLOCK) {                                 // (the same in all lanes)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                x.many[h] = load_bytes16(at_many + at + 64 * h, 16);
+        for (int h = 0; h < 2; ++h) m.x[h] = load_bytes16(at_many + at + 64 * h, decltype(whole)::value ? 16 : static_cast<int>(args.k - at) - lane / 16 * 16 - 64 * h);
+        m.s[0] = s_many[0][b];
 #pragma unroll
-                for (int f = 0; f < TF; ++f) x.few[f][h] = load_bytes16(at_few[f] + at + 64 * h, 16);
-            }
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int valid = static_cast<int>(left - 64 * h < 16 ? left - 64 * h : 16);
-                x.many[h] = load_bytes16(at_many + at + 64 * h, valid);
-#pragma unroll
-                for (int f = 0; f < TF; ++f) x.few[f][h] = load_bytes16(at_few[f] + at + 64 * h, valid);
-            }
-        }
-        x.s_many[0] = s_many[0][b];
-#pragma unroll
-        for (int r = 1; r < 4; ++r) x.s_many[r] = args.shift_many != 0 ? x.s_many[0] : s_many[r][b];       // (16 rows lie in one square block)
-#pragma unroll
-        for (int f = 0; f < TF; ++f) x.s_few[f] = s_few[f][b];
+        for (int r = 1; r < 4; ++r) m.s[r] = args.shift_many != 0 ? m.s[0] : s_many[r][b];       // (16 rows lie in one square block)
     };
-    auto multiply = [&](const Block &x) {
-        Fp16Fragment many, few;
-        many.set(join(x.many[0], x.many[1]));
-        const floatx4 s{x.s_many[0], x.s_many[1], x.s_many[2], x.s_many[3]};
+    auto fetch_few = [&](int b, Few &x, auto whole) {
+        const int64_t at = static_cast<int64_t>(b) * SCALE_BLOCK;
 #pragma unroll
         for (int f = 0; f < TF; ++f) {
-            few.set(join(x.few[f][0], x.few[f][1]));
-            add_block(acc[f], many, few, s, x.s_few[f]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x.x[f][h] = load_bytes16(at_few[f] + at + 64 * h, decltype(whole)::value ? 16 : static_cast<int>(args.k - at) - lane / 16 * 16 - 64 * h);
+            x.s[f] = s_few[f][b];
         }
     };
-    Block x[2];
-    int b = wave;
-    if (b < blocks) fetch(b, x[0]);
-    for (; b + FEW_WAVES < blocks; b += 2 * FEW_WAVES) {
-        fetch(b + FEW_WAVES, x[1]);
-        multiply(x[0]);
-        if (b + 2 * FEW_WAVES < blocks) fetch(b + 2 * FEW_WAVES, x[0]);
-        multiply(x[1]);
+    auto multiply = [&](const Many &m, const Few &x) {
+        FRAGMENT many, few;
+        many.set(join(m.x[0], m.x[1]));
+        const floatx4 s{m.s[0], m.s[1], m.s[2], m.s[3]};
+#pragma unroll
+        for (int f = 0; f < TF; ++f) {
+            few.set(join(x.x[f][0], x.x[f][1]));
+            add_block(acc[f], many, few, s, x.s[f]);
+        }
+    };
+    using Whole = std::true_type;
+    constexpr int AHEAD = 2;
+    const int whole_blocks = args.k / SCALE_BLOCK;
+    Many many[AHEAD];
+    Few few[2];
+    static_for<AHEAD>([&](auto U) {
+        constexpr int u = decltype(U)::value;
+        if (wave + u * FEW_WAVES < whole_blocks) fetch_many(wave + u * FEW_WAVES, many[u], Whole{});
+    });
+    if (wave < whole_blocks) fetch_few(wave, few[0], Whole{});
+    for (int b0 = wave; b0 < whole_blocks; b0 += AHEAD * FEW_WAVES)
+        static_for<AHEAD>([&](auto U) {
+            constexpr int u = decltype(U)::value;
+            const int b = b0 + u * FEW_WAVES;
+            if (b < whole_blocks) {
+                if (b + FEW_WAVES < whole_blocks) fetch_few(b + FEW_WAVES, few[(u + 1) % 2], Whole{});
+                multiply(many[u], few[u % 2]);
+                if (b + AHEAD * FEW_WAVES < whole_blocks) fetch_many(b + AHEAD * FEW_WAVES, many[u], Whole{});
+            }
+        });
+    if (whole_blocks < blocks && wave == whole_blocks % FEW_WAVES) {
+        fetch_many(whole_blocks, many[0], std::false_type{});
+        fetch_few(whole_blocks, few[0], std::false_type{});
+        multiply(many[0], few[0]);
     }
-    if (b < blocks) multiply(x[0]);
 
 #pragma unroll
     for (int f = 0; f < TF; ++f) *reinterpret_cast<floatx4 *>(&sums[wave][(16 * f + lane % 16) * PITCH + lane / 16 * 4]) = acc[f];
@@ -135,19 +147,23 @@ template <int MODE, int TF> __global__ __launch_bounds__(FEW_WAVES * 64) void bl
     }
 }
 
-template <int MODE> hipError_t launch_as(const FewArgs &args, int fragments, hipStream_t stream)
+template <int MODE> hipError_t launch_as(const FewArgs &args, int fragments, bool fp32, hipStream_t stream)
 {
     const int64_t tiles = ceil_div(args.rows_few, 16 * fragments) + (MODE == BLOCK_ROWS ? args.groups.count : 0);
     const dim3 grid(static_cast<uint32_t>(ceil_div(args.rows_many, 16)), static_cast<uint32_t>(tiles));
-    if (fragments == 1) block_few_kernel<MODE, 1><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
-    else if (fragments == 2) block_few_kernel<MODE, 2><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
-    else block_few_kernel<MODE, 4><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
+    if (fragments == 1) {
+        if (fp32) block_few_kernel<MODE, 1, Fp16Fragment><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
+        else block_few_kernel<MODE, 1, Fp8Fragment><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
+    } else {
+        if (fp32) block_few_kernel<MODE, 2, Fp16Fragment><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
+        else block_few_kernel<MODE, 2, Fp8Fragment><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_block_few(const BlockArgs &a, int mode, bool few_b, int fragments, hipStream_t stream)
+hipError_t launch_block_few(const BlockArgs &a, int mode, bool few_b, int fragments, bool fp32, hipStream_t stream)
 {
     FewArgs f{};
     f.groups = a.groups;
@@ -164,7 +180,7 @@ hipError_t launch_block_few(const BlockArgs &a, int mode, bool few_b, int fragme
         f.few = a.A; f.s_few = a.SA; f.ld_few = a.lda; f.lds_few = a.ldsa; f.shift_few = a.a_shift; f.rows_few = a.m; f.c_few = a.ldc;
         f.stride_many = a.stride_b; f.stride_s_many = a.stride_sb;
     }
-    return mode == BLOCK_DENSE ? launch_as<BLOCK_DENSE>(f, fragments, stream) : launch_as<BLOCK_ROWS>(f, fragments, stream);
+    return mode == BLOCK_DENSE ? launch_as<BLOCK_DENSE>(f, fragments, fp32, stream) : launch_as<BLOCK_ROWS>(f, fragments, fp32, stream);
 }
 
 }  // namespace mg

@@ -146,33 +146,74 @@ struct Plan {
 
 int64_t output_rows(int mode, int groups, int64_t m) { return mode == BLOCK_SUM ? groups * m : m; }
 
-// Which kernel and how many slices of the sum.  Slices: where the tiles leave most of the chip idle, and no more than leaves four blocks to each.
+// What a kernel takes, in us, measured with random operands.  A compute unit that has one of its tiles: `alone` for a block of 128 of the sum while half of the
+// chip is idle, `full` while all of it is busy; with n of them n * `each` (two work-groups of 128 x 128 share a compute unit, two to four of 64 x 64).
+// Around the sum: `start`, and `more` for every round of tiles (C leaves).  Over 2048 x 2048 .. 8192 x 4096 with sums of 512 to 8192 within a tenth of the measured,
+// but for `each` of 128 x 128: 0.515 with uniform bits, where the clock stays up; with activations the smaller tiles slow down more than the large ones.
+struct Cost {
+    double alone, full, each, start, more;
+};
+Cost cost_of(int tile, int sums)
+{
+    const bool fp32 = sums_fp32(sums);
+    Cost c{};
+    switch (tile) {
+        case DMA_256: c = fp32 ? Cost{1.47, 1.7, 1.6, 4, 7} : Cost{1.38, 1.6, 1.55, 4, 6.5}; break;
+        case DMA_128: c = fp32 ? Cost{1.05, 1.19, 0.93, 3, 1.5} : Cost{0.6, 0.75, 0.6, 3, 1}; break;
+        case DMA_64: c = fp32 ? Cost{0.5, 0.52, 0.37, 3, 0.7} : Cost{0.3, 0.31, 0.24, 3, 0.5}; break;
+        case TILE_ANY: c = fp32 ? Cost{1.8, 2.1, 1.5, 4, 1.5} : Cost{1.2, 1.4, 1.0, 4, 1.5}; break;
+        default: c = fp32 ? Cost{0.9, 1.0, 0.6, 3.5, 0.7} : Cost{0.6, 0.66, 0.4, 3.5, 0.7}; break;
+    }
+    // scales of any value are multiplied in beside the matrix instructions (4096^3: 66 -> 76 us; 128 x 4096 x 4096 on 64 x 64 tiles 13 -> 17)
+    const double scaling = sums == SUMS_POW2 || sums == SUMS_FP32_POW2 ? 1. : tile == DMA_256 ? 1.17 : 1.4;
+    c.alone *= scaling;
+    c.full *= scaling;
+    c.each *= scaling;
+    return c;
+}
+
+// Which kernel and how many slices of the sum: the least of the estimates.  Slices cost a launch that reads what they wrote, and no slice gets fewer than four blocks.
 Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums, bool aligned, size_t workspace)
 {
-    Plan p{};
-    p.slices = 1;
+    Plan best{};
+    best.slices = 1;
     const int64_t few = mode == BLOCK_ROWS ? ceil_div(m, groups) : m < n ? m : n;       // rows of A (for an expert), or of the smaller operand
-    if (mode != BLOCK_SUM && few <= 32) {
-        p.tile = TILE_FEW;
-        p.few_b = mode == BLOCK_DENSE && n < m;
-        p.fragments = few <= 16 ? 1 : 2;
-        return p;
+    // The kernel for few rows reads them once for every 16 of the others.  8192 x 8192: 4 rows 15.9 us, 16 rows 22, 32 rows 33, 64 x 64 tiles 19; 4096 x 4096: 32 rows 10,
+    // 64 x 64 tiles 11.5.  Experts' rows are few wherever they are not 16 on average.
+    if (mode != BLOCK_SUM && (few <= 8 || (mode == BLOCK_ROWS && few <= 16) || (few <= 32 && (m < n ? n : m) * k <= int64_t(1) << 25))) {
+        best.tile = TILE_FEW;
+        best.few_b = mode == BLOCK_DENSE && n < m;
+        best.fragments = few <= 16 ? 1 : 2;
+        return best;
     }
     const int64_t batch = mode == BLOCK_SUM ? groups : 1;
-    auto tiles = [&](int tile) {
+    const double blocks = static_cast<double>(ceil_div(k, SCALE_BLOCK)) / batch + (mode == BLOCK_SUM ? 0.5 : 0.);
+    const double one = static_cast<double>(output_rows(mode, groups, m)) * n * 4;
+    double least = 0;
+    for (const int tile : {int(DMA_256), int(DMA_128), int(DMA_64), TILE_ANY, TILE_ANY_64}) {
+        if (aligned != (tile >= 0)) continue;
         const int64_t any = tile == TILE_ANY ? 128 : 64, bm = tile < 0 ? any : block_dma_rows(tile), bn = tile < 0 ? any : block_dma_cols(tile, sums);
+        Plan p{};
+        p.tile = tile;
         p.tiles_m = static_cast<int>(ceil_div(m, bm) + (mode == BLOCK_ROWS ? groups : 0));
         p.tiles_n = static_cast<int>(ceil_div(n, bn));
-        return (mode == BLOCK_ROWS ? ceil_div(m, bm) : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * batch;
-    };
-    p.tile = !aligned ? (tiles(TILE_ANY) >= 160 ? TILE_ANY : TILE_ANY_64) : tiles(DMA_256) >= 160 ? DMA_256 : tiles(DMA_128) >= 160 ? DMA_128 : DMA_64;
-    const int64_t count = tiles(p.tile);
-    const int64_t blocks = ceil_div(k, SCALE_BLOCK) / batch;
-    const size_t one = static_cast<size_t>(output_rows(mode, groups, m)) * n * 4;
-    int64_t s = 1;
-    while (s < 16 && count * s * 2 <= 256 && blocks / (s * 2) >= 4 && one * s * 2 <= workspace) s *= 2;
-    p.slices = static_cast<int>(s);
-    return p;
+        // (every expert's last tile is half full, if it has rows at all)
+        const int64_t ends = groups < m / bm ? groups / 2 : 0;
+        const int64_t tiles = (mode == BLOCK_ROWS ? ceil_div(m, bm) + ends : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * batch;
+        const Cost c = cost_of(tile, sums);
+        for (int s = 1; s <= 16; s *= 2) {
+            if (s > 1 && (blocks / s < 4 || one * s > static_cast<double>(workspace) || tiles * s > 512)) break;
+            const double per_unit = static_cast<double>(ceil_div(tiles * s, 256));
+            const double a_block = per_unit > 1 ? (c.each * per_unit > c.full ? c.each * per_unit : c.full) : tiles * s <= 128 ? c.alone : c.full;
+            const double us = c.start + c.more * per_unit + blocks / s * a_block + (s > 1 ? 4 + one * (s + 1) / 4e6 : 0);
+            if (least == 0 || us < least) {
+                least = us;
+                best = p;
+                best.slices = s;
+            }
+        }
+    }
+    return best;
 }
 
 // Rows on 16 bytes, and 32-bit offsets: inside a tile of 256 rows, or from the first row of A where rows are indexed
@@ -210,7 +251,7 @@ template <int MODE> hipError_t launch_mode(const BlockProblem &p, const BlockArg
 size_t block_gemm_workspace(int mode, int groups, int64_t m, int64_t n, int64_t k)
 {
     int slices = 1;
-    for (const int sums : {SUMS_POW2, SUMS_FP32})
+    for (const int sums : {SUMS_POW2, SUMS_ANY, SUMS_FP32, SUMS_FP32_POW2})
         for (const bool aligned : {false, true}) {
             const Plan p = plan(mode, groups, m, n, k, sums, aligned, SIZE_MAX);
             slices = slices > p.slices ? slices : p.slices;
@@ -233,7 +274,7 @@ hipError_t launch_block_gemm(const BlockProblem &p)
     args.tiles_m = how.tiles_m; args.tiles_n = how.tiles_n; args.slices = how.slices;
     args.partial = how.slices > 1 ? static_cast<float *>(p.workspace) : nullptr;
     args.partial_rows = output_rows(p.mode, p.groups.count, p.m);
-    if (how.tile == TILE_FEW) return launch_block_few(args, p.mode, how.few_b, how.fragments, p.stream);
+    if (how.tile == TILE_FEW) return launch_block_few(args, p.mode, how.few_b, how.fragments, sums_fp32(sums), p.stream);
     const hipError_t e = p.mode == BLOCK_DENSE ? launch_mode<BLOCK_DENSE>(p, args, sums, how.tile)
                          : p.mode == BLOCK_ROWS ? launch_mode<BLOCK_ROWS>(p, args, sums, how.tile) : launch_mode<BLOCK_SUM>(p, args, sums, how.tile);
     if (e != hipSuccess || how.slices == 1) return e;

@@ -133,6 +133,18 @@ __device__ inline uint32_t max_over_16_lanes(uint32_t v)
     return v;
 }
 
+// Sum over the lanes up to this one: inside rows of 16 lanes by shifts, then each row's total into those behind it
+__device__ inline int sum_up_to_lane(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);       // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);       // lane 15 of a row into the next, rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);       // lane 31 into rows 2 and 3
+    return v;
+}
+
 // The scale 2^e of a block whose largest magnitude has the bits `largest`: e is the least with largest / 2^e <= 448 = 1.75 * 2^8, -126 at least.
 // Adding 0x1fffff to the bits carries into the exponent exactly where the mantissa is above 1.75.
 __device__ inline int scale_exponent(uint32_t largest)
@@ -164,21 +176,16 @@ template <int LOG> __device__ inline bool find_row_tile(const Groups &g, int til
     for (int base = 0; base < g.count; base += 64) {
         const int lo = offset(base + lane), hi = offset(base + lane + 1);
         const int tiles = hi > lo ? (hi - lo + (1 << LOG) - 1) >> LOG : 0;
-        int sum = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d);
-            if (lane >= d) sum += o;
-        }
-        const int total = __builtin_amdgcn_readfirstlane(__shfl(sum, 63));          // (the compiler has to know that all lanes go the same way)
+        const int sum = sum_up_to_lane(tiles);
+        const int total = __builtin_amdgcn_readlane(sum, 63);          // (read by lane: the compiler has to know that all lanes go the same way)
         if (tile < before + total) {
             const uint64_t behind = __ballot(before + sum > tile);
             const int at = __ffsll(static_cast<unsigned long long>(behind)) - 1;
-            const int first_tile = before + __shfl(sum - tiles, at);
-            found->group = __builtin_amdgcn_readfirstlane(base + at);
-            found->start = __builtin_amdgcn_readfirstlane(__shfl(lo, at));
-            found->end = __builtin_amdgcn_readfirstlane(__shfl(hi, at));
-            found->first = found->start + (static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tile - first_tile)) << LOG);
+            const int first_tile = before + __builtin_amdgcn_readlane(sum - tiles, at);
+            found->group = base + at;
+            found->start = __builtin_amdgcn_readlane(lo, at);
+            found->end = __builtin_amdgcn_readlane(hi, at);
+            found->first = found->start + (static_cast<int64_t>(tile - first_tile) << LOG);
             return true;
         }
         before += total;
