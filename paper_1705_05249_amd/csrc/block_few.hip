@@ -1,16 +1,16 @@
 // Products with few rows in one operand (the tokens that are being generated): the other operand, the weights, is read once and little else counts.
 //
-// A work-group takes 16 rows of the weights and up to 16 TF of the few; its eight wavefronts share the sum, each every eighth block
-// of 128, straight from memory into registers (a fragment of 16 x 128 bytes is 32 bytes for each lane, four lanes to a row's 128): four blocks of the
-// weights on their way at a time, 128 KB for a compute unit, and two of the few, which come from the caches.  The wavefronts' sums meet in LDS and are added in their order.  Memory leaves the matrix pipes
-// nine tenths idle, so the sums are always FP32's (operands widened to FP16).
+// A work-group takes 16 rows of the weights and up to 16 TF of the few; its four or eight wavefronts share the sum, each every fourth or eighth block
+// of 128, straight from memory into registers (a fragment of 16 x 128 bytes is 32 bytes for each lane, four lanes to a row's 128): two blocks on
+// their way at a time.  The wavefronts' sums meet in LDS and are added in their order.  Bound by the weights' bytes
+// (1 x 4096 x 4096: 5.0 us, 3.4 TB/s and the launch; 1 x 16384 x 4096: 14.7, 4.6 TB/s), with more of the few also by what the caches pass on: the few
+// are read once for every 16 rows of the weights (32 x 8192 x 8192 took 33 us, 64 x 64 tiles take 18).
 #include "internal.h"
 #include "block_gemm_kernel.h"
 
 namespace mg {
 namespace {
 
-constexpr int FEW_WAVES = 8;
 
 struct FewArgs {
     const uint8_t *many, *few;                // the operands: `rows_many` rows that are streamed, few of the other
@@ -32,7 +32,7 @@ template <typename T> __device__ inline void write_one(T *c, float v, float alph
     *c = static_cast<T>(v);
 }
 
-template <int MODE, int TF, typename FRAGMENT> __global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(const FewArgs args)
+template <int MODE, int FEW_WAVES, int TF, typename FRAGMENT> __global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(const FewArgs args)
 {
     constexpr int FEW = 16 * TF, PITCH = 20;                              // floats between the rows of a sum in LDS
     __shared__ __attribute__((aligned(16))) float sums[FEW_WAVES][FEW * PITCH];
@@ -151,13 +151,21 @@ template <int MODE> hipError_t launch_as(const FewArgs &args, int fragments, boo
 {
     const int64_t tiles = ceil_div(args.rows_few, 16 * fragments) + (MODE == BLOCK_ROWS ? args.groups.count : 0);
     const dim3 grid(static_cast<uint32_t>(ceil_div(args.rows_many, 16)), static_cast<uint32_t>(tiles));
-    if (fragments == 1) {
-        if (fp32) block_few_kernel<MODE, 1, Fp16Fragment><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
-        else block_few_kernel<MODE, 1, Fp8Fragment><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
-    } else {
-        if (fp32) block_few_kernel<MODE, 2, Fp16Fragment><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
-        else block_few_kernel<MODE, 2, Fp8Fragment><<<grid, FEW_WAVES * 64, 0, stream>>>(args);
-    }
+    auto launch = [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        if (fragments == 1) {
+            if (fp32) block_few_kernel<MODE, W, 1, Fp16Fragment><<<grid, W * 64, 0, stream>>>(args);
+            else block_few_kernel<MODE, W, 1, Fp8Fragment><<<grid, W * 64, 0, stream>>>(args);
+        } else {
+            if (fp32) block_few_kernel<MODE, W, 2, Fp16Fragment><<<grid, W * 64, 0, stream>>>(args);
+            else block_few_kernel<MODE, W, 2, Fp8Fragment><<<grid, W * 64, 0, stream>>>(args);
+        }
+    };
+    // Two work-groups and more for each compute unit: four wavefronts each, of which more fit (32 experts with 2 rows, 2048 x 4096: 68 -> 55 us, 4.9 TB/s); fewer:
+    // eight, for the length of the sum (1 x 8192 x 4096: 7.5 us, with two wavefronts 10.6)
+    const int64_t busy = grid.x * (MODE == BLOCK_ROWS ? (args.rows_few < args.groups.count ? args.rows_few : args.groups.count) : tiles);
+    if (busy >= 512) launch(std::integral_constant<int, 4>{});
+    else launch(std::integral_constant<int, 8>{});
     return hipGetLastError();
 }
 

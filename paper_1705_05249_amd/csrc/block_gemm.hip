@@ -179,8 +179,9 @@ Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums, bool 
     best.slices = 1;
     const int64_t few = mode == BLOCK_ROWS ? ceil_div(m, groups) : m < n ? m : n;       // rows of A (for an expert), or of the smaller operand
     // The kernel for few rows reads them once for every 16 of the others.  8192 x 8192: 4 rows 15.9 us, 16 rows 22, 32 rows 33, 64 x 64 tiles 19; 4096 x 4096: 32 rows 10,
-    // 64 x 64 tiles 11.5.  Experts' rows are few wherever they are not 16 on average.
-    if (mode != BLOCK_SUM && (few <= 8 || (mode == BLOCK_ROWS && few <= 16) || (few <= 32 && (m < n ? n : m) * k <= int64_t(1) << 25))) {
+    // 64 x 64 tiles 11.5.  32 experts, 2048 x 4096 each: 16 rows 79 us, 17 rows 92,
+    // 64 x 64 tiles 84.
+    if (mode != BLOCK_SUM && (few <= 8 || (mode == BLOCK_ROWS && few <= 16) || (mode == BLOCK_DENSE && few <= 32 && (m < n ? n : m) * k <= int64_t(1) << 25))) {
         best.tile = TILE_FEW;
         best.few_b = mode == BLOCK_DENSE && n < m;
         best.fragments = few <= 16 ? 1 : 2;
