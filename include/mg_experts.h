@@ -13,6 +13,9 @@
  * stands for its 8-bit value times its block's scale.  Scales are row-major with a leading dimension of their own:
  * (row blocks) rows x ceil(cols/128), (square blocks) ceil(rows/128) x ceil(cols/128).
  *
+ * MG_ERR_DIM also covers what a launch cannot hold: 2^35 elements of a matrix that is quantised, 2^34 of a product's C,
+ * 2^32 pieces of four elements of the rows that are routed.
+ *
  * A kernel may read an aligned 16-byte piece of memory whole when at least one of its bytes belongs to an operand.
  */
 #ifndef MG_EXPERTS_H
@@ -34,8 +37,9 @@ enum {
 enum { MG_BF16 = 2 };                                             /* beside MG_F32 and MG_F16: bfloat16 */
 typedef enum { MG_BLOCK_ROW = 151, MG_BLOCK_SQUARE = 152 } mg_block;
 /* MG_SCALES_POW2: the caller states that every scale of both operands is a normal power of two (as mg_block_quantize
- * makes them): the scales then go into the matrix instructions as exponents.  Other scales given under it count as the
- * power of two below them. */
+ * makes them): the scales then go into the matrix instructions as exponents, or into the exponents of the elements, whose
+ * values have to be finite FP32 numbers then (below 2^-126 they may count as zero).  Other scales given under it count as
+ * the power of two below them. */
 typedef enum { MG_SCALES_ANY = 161, MG_SCALES_POW2 = 162 } mg_scales;
 /* May be added (|) to either: sums as of FP32 products whatever the type of C.  Without it C in FP32 gets those, and C in 16 bits is
  * summed on the FP8 matrix pipes, twice as fast: they add eight neighbouring products at a time on a grid of 2^-13 of the largest of the

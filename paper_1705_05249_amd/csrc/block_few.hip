@@ -11,7 +11,6 @@
 namespace mg {
 namespace {
 
-
 struct FewArgs {
     const uint8_t *many, *few;                // the operands: `rows_many` rows that are streamed, few of the other
     const float *s_many, *s_few;

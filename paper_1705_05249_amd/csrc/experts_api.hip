@@ -242,7 +242,7 @@ size_t mg_expert_sort_workspace_bytes(int64_t tokens, int fan, int experts)
 static mg_status check_rows(int64_t tokens, int fan, int64_t cols)
 {
     if (!extent(tokens) || !extent(cols) || __int128(tokens) * fan > (__int128(1) << 30)) return MG_ERR_DIM;
-    if (fan > 0 && __int128(tokens) * fan * ceil_div(cols, 4) > MOST_PIECES * 256) return MG_ERR_DIM;
+    if (fan > 0 && __int128(tokens) * fan * ceil_div(cols, 4) >= MOST_PIECES * 256) return MG_ERR_DIM;
     if (tokens > MOST_PIECES) return MG_ERR_DIM;                     // (a work-group for each in the gradient)
     return MG_OK;
 }
