@@ -13,8 +13,8 @@
  * stands for its 8-bit value times its block's scale.  Scales are row-major with a leading dimension of their own:
  * (row blocks) rows x ceil(cols/128), (square blocks) ceil(rows/128) x ceil(cols/128).
  *
- * MG_ERR_DIM also covers what a launch cannot hold: 2^35 elements of a matrix that is quantised, 2^34 of a product's C,
- * 2^32 pieces of four elements of the rows that are routed.
+ * MG_ERR_DIM also covers what the kernels' 32-bit counts and a launch cannot hold: extents from 2^31 - 1024 on, 2^35 elements of a
+ * matrix that is quantised, 2^34 of a product's C, and of the rows that are routed 2^31 pieces of four elements and 2^24 tokens.
  *
  * A kernel may read an aligned 16-byte piece of memory whole when at least one of its bytes belongs to an operand.
  */

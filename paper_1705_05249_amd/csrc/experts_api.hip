@@ -6,9 +6,9 @@
 namespace mg {
 namespace {
 
-constexpr int64_t MOST_EXTENT = int64_t(1) << 31;                 // every extent below it
+constexpr int64_t MOST_EXTENT = (int64_t(1) << 31) - 1024;        // every extent below it (kernels round them up in 32 bits)
 constexpr __int128 MOST_ELEMENTS = __int128(1) << 40;             // of a stored matrix
-constexpr __int128 MOST_PIECES = __int128(1) << 24;               // work-groups of a launch
+constexpr __int128 MOST_PIECES = __int128(1) << 24;               // work-groups of 256 threads that a launch does not reach
 
 bool extent(int64_t v) { return v >= 0 && v < MOST_EXTENT; }
 bool stored(int64_t rows, int64_t ld) { return __int128(rows) * ld <= MOST_ELEMENTS; }
@@ -33,7 +33,7 @@ mg_status quantize(QuantizeProblem &p, int block, int64_t turned_cols)
     if (t && !at_least(p.ldt, turned_cols)) return MG_ERR_LDC;
     if (!stored(p.rows, p.ldx) || (q && !stored(p.rows, p.ldq)) || (t && !stored(p.cols, p.ldt))) return MG_ERR_DIM;
     const bool empty = p.rows == 0 || p.cols == 0 || p.batch == 0;
-    if (!empty && (p.X == nullptr || (!q && !t) || (q && (p.Q == nullptr || p.S == nullptr)) || (t && (p.T == nullptr || p.ST == nullptr)))) return MG_ERR_NULL;
+    if (!empty && (p.X == nullptr || (p.groups.count > 0 && p.groups.offsets == nullptr) || (!q && !t) || (q && (p.Q == nullptr || p.S == nullptr)) || (t && (p.T == nullptr || p.ST == nullptr)))) return MG_ERR_NULL;
     if (p.batch < 0 || p.batch > 65535) return MG_ERR_BATCH;
     if (p.stride_x < 0 || p.stride_q < 0 || p.stride_s < 0 || p.stride_t < 0 || p.stride_st < 0) return MG_ERR_STRIDE;
     if (!type_known(p.dtype)) return MG_ERR_TYPE;
@@ -87,7 +87,6 @@ mg_status mg_block_quantize_grouped(int dtype, int groups, const int32_t *offset
         const mg_status st = quantize(p, MG_BLOCK_ROW, rows);
         return st != MG_OK ? st : MG_ERR_GROUPS;
     }
-    if (rows > 0 && cols > 0 && offsets == nullptr) return MG_ERR_NULL;
     return quantize(p, MG_BLOCK_ROW, mg_grouped_columns(rows, groups));
 }
 
@@ -146,7 +145,7 @@ mg_status mg_block_gemm_grouped(int groups, const int32_t *offsets, int64_t rows
                                 int64_t ldb, int64_t stride_b, const float *SB, int64_t ldsb, int64_t stride_sb, float beta, int c_type, void *C,
                                 int64_t ldc, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!extent(rows) || !extent(n) || !extent(k) || !tiles_fit(rows, n, MG_MOST_GROUPS)) return MG_ERR_DIM;
+    if (!extent(rows) || !extent(n) || !extent(k) || !tiles_fit(rows, n, groups_known(groups) ? groups : 1)) return MG_ERR_DIM;
     if (!at_least(lda, k)) return MG_ERR_LDA;
     if (!at_least(ldb, k)) return MG_ERR_LDB;
     if (!at_least(ldc, n)) return MG_ERR_LDC;
@@ -238,12 +237,13 @@ size_t mg_expert_sort_workspace_bytes(int64_t tokens, int fan, int experts)
     return expert_sort_workspace(tokens, fan, experts);
 }
 
-// What the three routines on rows check alike: extents (tokens x cols pieces of 16 bytes in a launch), and the fan at the end
+// What the three routines on rows check alike.  A launch has a thread for each piece of 16 bytes of tokens x fan rows, whose number is rounded up in every
+// row, to less than twice as many, or a work-group for each token.
 static mg_status check_rows(int64_t tokens, int fan, int64_t cols)
 {
     if (!extent(tokens) || !extent(cols) || __int128(tokens) * fan > (__int128(1) << 30)) return MG_ERR_DIM;
-    if (fan > 0 && __int128(tokens) * fan * ceil_div(cols, 4) >= MOST_PIECES * 256) return MG_ERR_DIM;
-    if (tokens > MOST_PIECES) return MG_ERR_DIM;                     // (a work-group for each in the gradient)
+    if (fan > 0 && __int128(tokens) * fan * ceil_div(cols, 4) > MOST_PIECES * 128) return MG_ERR_DIM;
+    if (tokens >= MOST_PIECES) return MG_ERR_DIM;
     return MG_OK;
 }
 

@@ -175,3 +175,28 @@ def test_routing_refusals():
 def test_wrong_types_raise():
     with pytest.raises(ctypes.ArgumentError):
         X.mg_expert_sort("tokens", 2, 8, None, None, None, None, None, 0)
+
+
+def test_what_a_launch_holds():
+    """Extents next to the limits: MG_ERR_NULL (-8) comes behind MG_ERR_DIM (-4) and shows that a size is taken."""
+    last = (1 << 31) - 1025                       # an extent that kernels can still round up to whole blocks in 32 bits
+    assert quantize(rows=1, cols=last, ldx=last, ldq=last, lds=1 << 24, X_=None) == -4           # (one row of that length: 2^24 blocks)
+    assert quantize(rows=1, cols=1 << 27, ldx=1 << 27, ldq=1 << 27, lds=1 << 20, X_=None) == -8
+    assert product(k=last, lda=last, ldb=last, C=None) == -8 and product(k=last + 1, lda=last + 1, ldb=last + 1, C=None) == -4
+
+    def grouped(groups, rows, n):
+        return X.mg_block_gemm_grouped(groups, FAKE, rows, n, 128, 1.0, X.MG_SCALES_POW2, FAKE, 128, FAKE, 1, None, 1, X.MG_BLOCK_SQUARE, FAKE, 128, 128 * n, FAKE, 1, n, 0.0,
+                                       X.MG_BF16, None, n, None, 0, check=False)
+    assert grouped(8, 16, 200000) == -8                                                          # few experts leave room for many columns
+    assert grouped(1024, 16, 200000) == -4
+
+    def rows(tokens, fan, cols, fn=X.mg_expert_combine):
+        return fn(X.MG_F32, tokens, fan, cols, None, cols, FAKE, None, None, cols, stream=0, check=False)
+    assert rows((1 << 24) - 1, 1, 4) == -8 and rows(1 << 24, 1, 4) == -4
+    assert rows(1 << 20, 1, 8192) == -8 and rows(1 << 20, 1, 8193) == -4
+
+
+def test_grouped_quantize_errors_in_order():
+    def call(offsets, ldx):
+        return X.mg_block_quantize_grouped(X.MG_F32, 2, offsets, 4, 8, FAKE, ldx, None, 1, FAKE, 8, FAKE, 1, None, 1, None, 1, stream=0, check=False)
+    assert call(None, 7) == -5 and call(None, 8) == -8
