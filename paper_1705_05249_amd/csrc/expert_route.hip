@@ -14,6 +14,9 @@ constexpr int SORT_KEYS = 4;                     // slots of a lane, 64 apart
 constexpr int SORT_WAVES = 16;
 constexpr int SORT_CHUNK = SORT_WAVES * 64 * SORT_KEYS;          // slots of a work-group
 constexpr int SORT_ROW = MG_MOST_GROUPS + 1;     // experts and, behind them, the dropped slots
+// Chunks up to which every one of them adds up what is in front of it by itself; with more a launch in between does.  64 experts, 64 chunks: 13.1 us alone, 15.5 with
+// the launch; 128: 16.2 and 15.7; 2048 (8 M slots): 411 and 105; 1024 experts: 19.3 and 19.6, 25.2 and 21.1, 1477 and 155.
+constexpr int SORT_UNSCANNED = 64;
 
 // Lanes with the same key, as a mask (keys below 2^bits; all 64 lanes take part)
 __device__ inline uint64_t same_key(int key, int bits)
@@ -72,8 +75,34 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void sort_count_kernel(int64_t slo
     for (int e = threadIdx.x; e <= experts; e += SORT_WAVES * 64) counts[static_cast<int64_t>(blockIdx.x) * (experts + 1) + e] = count[e];
 }
 
-// Rows of a chunk's slots; a wavefront has 64 SORT_KEYS of them in a row.  counts null: the call's only chunk, counted here.
-__global__ __launch_bounds__(SORT_WAVES * 64) void sort_place_kernel(int64_t slots, int experts, const int32_t *ids, const int32_t *counts, int chunks,
+// counts[chunk][key] -> sums over the chunks in front of each, and over all of them in a row behind the last.  A lane has a key, a wavefront a
+// run of chunks.
+__global__ __launch_bounds__(SORT_WAVES * 64) void sort_scan_kernel(int keys, int chunks, int32_t *counts)
+{
+    __shared__ int sums[SORT_WAVES][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, key = blockIdx.x * 64 + lane;
+    const int each = (chunks + SORT_WAVES - 1) / SORT_WAVES, first = wave * each < chunks ? wave * each : chunks;
+    const int end = key < keys ? first + each < chunks ? first + each : chunks : first;
+    int sum = 0;
+#pragma unroll 8
+    for (int c = first; c < end; ++c) sum += counts[static_cast<int64_t>(c) * keys + key];
+    sums[wave][lane] = sum;
+    __syncthreads();
+    int before = 0;
+    for (int w = 0; w < wave; ++w) before += sums[w][lane];
+#pragma unroll 8
+    for (int c = first; c < end; ++c) {
+        int32_t *const at = counts + static_cast<int64_t>(c) * keys + key;
+        const int v = *at;
+        *at = before;
+        before += v;
+    }
+    if (wave == SORT_WAVES - 1 && key < keys) counts[static_cast<int64_t>(chunks) * keys + key] = before;
+}
+
+// Rows of a chunk's slots; a wavefront has 64 SORT_KEYS of them in a row.  counts null: the call's only chunk, counted here.  scanned: counts as
+// sort_scan_kernel leaves them.
+__global__ __launch_bounds__(SORT_WAVES * 64) void sort_place_kernel(int64_t slots, int experts, const int32_t *ids, const int32_t *counts, int chunks, bool scanned,
                                                                      int32_t *offsets, int32_t *position, int32_t *source)
 {
     extern __shared__ int next[];                 // [wave][key]: how many slots of that key the wavefront has, then the row of its first one
@@ -104,7 +133,10 @@ __global__ __launch_bounds__(SORT_WAVES * 64) void sort_place_kernel(int64_t slo
         const int e = base + threadIdx.x;
         int all = 0, earlier = 0;
         if (e < keys) {
-            if (counts != nullptr) {
+            if (scanned) {
+                all = counts[static_cast<int64_t>(chunks) * keys + e];
+                earlier = counts[static_cast<int64_t>(blockIdx.x) * keys + e];
+            } else if (counts != nullptr) {
 #pragma unroll 8
                 for (int c = 0; c < chunks; ++c) {
                     const int v = counts[static_cast<int64_t>(c) * keys + e];
@@ -331,7 +363,7 @@ template <typename T> int64_t row_pieces(int64_t cols) { return ceil_div(cols, R
 size_t expert_sort_workspace(int64_t tokens, int fan, int experts)
 {
     const int64_t chunks = ceil_div(tokens * fan, SORT_CHUNK);
-    return chunks > 1 ? static_cast<size_t>(chunks) * (experts + 1) * sizeof(int32_t) : 0;
+    return chunks > 1 ? static_cast<size_t>(chunks + (chunks > SORT_UNSCANNED ? 1 : 0)) * (experts + 1) * sizeof(int32_t) : 0;
 }
 
 hipError_t launch_expert_sort(int64_t tokens, int fan, int experts, const int32_t *ids, int32_t *offsets, int32_t *position, int32_t *source,
@@ -342,6 +374,12 @@ hipError_t launch_expert_sort(int64_t tokens, int fan, int experts, const int32_
     int32_t *counts = chunks > 1 ? static_cast<int32_t *>(workspace) : nullptr;
     if (counts != nullptr) {
         sort_count_kernel<<<chunks, SORT_WAVES * 64, 0, stream>>>(slots, experts, ids, counts);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const bool scanned = chunks > SORT_UNSCANNED;
+    if (scanned) {
+        sort_scan_kernel<<<static_cast<uint32_t>(ceil_div(experts + 1, 64)), SORT_WAVES * 64, 0, stream>>>(experts + 1, chunks, counts);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -356,7 +394,7 @@ hipError_t launch_expert_sort(int64_t tokens, int fan, int experts, const int32_
         if (e != hipSuccess) return e;
         raised = true;
     }
-    sort_place_kernel<<<chunks > 0 ? chunks : 1, waves * 64, lds, stream>>>(slots, experts, ids, counts, chunks, offsets, position, source);
+    sort_place_kernel<<<chunks > 0 ? chunks : 1, waves * 64, lds, stream>>>(slots, experts, ids, counts, chunks, scanned, offsets, position, source);
     return hipGetLastError();
 }
 

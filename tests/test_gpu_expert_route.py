@@ -50,6 +50,22 @@ def test_sort(tokens, fan, experts):
             assert all(np.array_equal(x, y) for x, y in zip(got, R.sort(ids.tolist(), experts)))
 
 
+@pytest.mark.parametrize("slots,experts", ((64 * 4096, 7), (64 * 4096 + 1, 65), (1 << 20, 1024), ((1 << 21) + 4095, 3)))
+def test_sort_of_many(slots, experts):
+    rng = np.random.default_rng(slots)
+    ids = rng.integers(-1, experts + 1, slots)
+    ids[: slots // 3] = experts // 2                                       # one expert has most of the first chunks
+    offsets, position, source = sorted_on_gpu(ids, slots, 1, experts)
+    key = np.where((ids >= 0) & (ids < experts), ids, experts)
+    order = np.argsort(key, kind="stable")
+    want = np.concatenate([[0], np.cumsum(np.bincount(key, minlength=experts + 1)[:experts])])
+    total = int(want[-1])
+    where = np.full(slots, -1)
+    where[order[:total]] = np.arange(total)
+    assert np.array_equal(offsets, want) and np.array_equal(position, where)
+    assert np.array_equal(source, np.where(np.arange(slots) < total, order, -1))
+
+
 def routes(rng, tokens, fan, experts, dropped):
     ids = rng.integers(0, experts, tokens * fan)
     ids[rng.random(ids.size) < dropped] = -1
