@@ -56,7 +56,7 @@ class Experts:
     """the products of all experts with one matrix each: weights experts x n x k"""
 
     def __init__(self, weights):
-        self.weights = weights
+        self.weights = weights.contiguous()
         self.experts, self.n, self.k = weights.shape
         self.w = Quantized(self.n, self.k, _blocks(self.n), self.experts)
         self.turned = Quantized(self.k, self.n, _blocks(self.k), self.experts)
@@ -106,6 +106,7 @@ class ExpertLayer:
 
     def forward(self, x, ids, gates):
         """x: tokens x width; ids: tokens x fan (negative: dropped); gates: tokens x fan, FP32"""
+        x, gates = x.contiguous(), gates.contiguous()
         routes = Routes(ids, self.up.experts)
         h = self.up.forward(routes, x, of_tokens=True)
         a = torch.relu(h).square_()
@@ -118,6 +119,7 @@ class ExpertLayer:
     def backward(self, dy):
         """gradients (x, gates, W1, W2) of the last forward pass"""
         routes, x, gates, h, a, rows = self.kept
+        dy = dy.contiguous()
         code = TYPES[dy.dtype]
         d_rows, d_gates = torch.empty_like(rows), torch.empty_like(gates)
         X.mg_expert_combine_grad(code, routes.tokens, routes.fan, self.width, dy, self.width, rows, self.width, routes.position, gates, d_rows, self.width, d_gates)

@@ -87,6 +87,22 @@ def test_gradient_of_gates_against_differences():
         assert abs((loss[0] - loss[1]) / (2 * step) - float(d_gates[t, j])) <= size * 2.0 ** -20
 
 
+def test_views_as_arguments():
+    """rows of a wider tensor, transposed weights and gates that are not dense give what their copies give"""
+    rng = np.random.default_rng(3)
+    tokens, width, hidden, experts, fan = 21, 96, 130, 3, 2
+    new = lambda *shape: torch.tensor(rng.standard_normal(shape), dtype=torch.float32).cuda()  # noqa: E731
+    ids = torch.tensor(rng.integers(0, experts, (tokens, fan))).cuda()
+    x, dy, gates = new(tokens, width + 7)[:, 7:], new(width, tokens).T, new(fan, tokens).T
+    w1, w2 = new(experts, width, hidden).transpose(1, 2), new(experts, hidden, width).transpose(1, 2)
+    results = []
+    for copy in (False, True):
+        a = [t.contiguous() if copy else t for t in (x, dy, gates, w1, w2)]
+        layer = ExpertLayer(a[3], a[4])
+        results.append((layer.forward(a[0], ids, a[2]), *layer.backward(a[1])))
+    assert all(torch.equal(p, q) for p, q in zip(*results))
+
+
 def test_training_reaches_the_target(capsys):
     """the command: the loss falls by half in twenty steps"""
     from paper_1705_05249_amd import expert_layer
