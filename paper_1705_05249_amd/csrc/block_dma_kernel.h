@@ -85,7 +85,7 @@ __global__ __launch_bounds__(WM *WN * 64) void block_dma_kernel(const BlockArgs 
 
     BlockTile tile;
     if (!block_tile<MODE, LOG_BM, BN>(args, &tile)) return;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave % WM, wn = wave / WM;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wm = wave / WN, wn = wave % WN;
     // a last K-tile that ends inside a piece of 16 bytes is not in the loop
     const bool ragged = tile.b_end > tile.b0 && static_cast<int64_t>(tile.b_end) * SCALE_BLOCK > tile.k && tile.k % 16 != 0;
     const int ktiles = tile.b_end - tile.b0 - (ragged ? 1 : 0);
@@ -197,14 +197,6 @@ __global__ __launch_bounds__(WM *WN * 64) void block_dma_kernel(const BlockArgs 
         fence();
         __builtin_amdgcn_s_barrier();
         fence();
-        read_b(std::integral_constant<int, 0>{}, 0);
-        static_for<FM>([&](auto I) { read_a(I, 0); });
-
-        // (here and now: otherwise the compiler moves the additions behind the branch of the last phase and keeps every block's sum until then)
-        auto add_scaled = [&](floatx4 &sum, const floatx4 &d, float s, const u32x4 &sb) {
-            scale_add(sum, d, s, std::integral_constant<bool, SUMS == SUMS_SQUARE>{}, sb);
-            landed(sum);
-        };
         // behind the last read of a stage: the next K-tile is there, and the loads of the one `STAGES` on start
         auto turn = [&](int t, int stage) {
             if (t + 1 < ktiles) {
@@ -212,112 +204,131 @@ __global__ __launch_bounds__(WM *WN * 64) void block_dma_kernel(const BlockArgs 
                 if (t + STAGES < ktiles) load_tile(t + STAGES, stage);
             }
         };
-        int stage = 0;
-        if constexpr (SUMS == SUMS_FP32_POW2) {
-            // Operands are widened beside the matrix instructions: A's fragments in phase 0, each in front of its first use, B's in the
-            // second half of the phase before theirs.  (Widened all at once, both wavefronts of a SIMD did so at the same time: 1.65 us
-            // for a K-tile of 256 x 128 instead of 1.57.)
-            Bf16Fragment fa[FM], fb[2];
-            wait_reads();
-            landed_b(std::integral_constant<int, 0>{});
-            landed_a();
-            fb[0].set(rb[0], sb1[0]);
-            auto multiply = [&](auto J, auto I, auto Q) {
-                constexpr int j = decltype(J)::value, i = decltype(I)::value, q = decltype(Q)::value;
-                acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j % 2].v[q], fa[i].v[q], acc[j][i], 0, 0, 0);
+        // Nothing to multiply: this wavefront only loads.  (A SIMD's two wavefronts lie along m, so that in an expert's last tile every SIMD has one
+        // less: 16 experts of 61 to 2879 rows, 4096 x 2048: 208 -> 203 us.)
+        const bool idle = wm * WTM >= rows_a || wn * WTN >= rows_b;
+        if (idle) {
+            int stage = 0;
+            for (int t = 0; t < ktiles; ++t) {
+                turn(t, stage);
+                stage = stage + 1 < STAGES ? stage + 1 : 0;
+            }
+        } else {
+            read_b(std::integral_constant<int, 0>{}, 0);
+            static_for<FM>([&](auto I) { read_a(I, 0); });
+
+            // (here and now: otherwise the compiler moves the additions behind the branch of the last phase and keeps every block's sum until then)
+            auto add_scaled = [&](floatx4 &sum, const floatx4 &d, float s, const u32x4 &sb) {
+                scale_add(sum, d, s, std::integral_constant<bool, SUMS == SUMS_SQUARE>{}, sb);
+                landed(sum);
             };
+            int stage = 0;
+            if constexpr (SUMS == SUMS_FP32_POW2) {
+                // Operands are widened beside the matrix instructions: A's fragments in phase 0, each in front of its first use, B's in the
+                // second half of the phase before theirs.  (Widened all at once, both wavefronts of a SIMD did so at the same time: 1.65 us
+                // for a K-tile of 256 x 128 instead of 1.57.)
+                Bf16Fragment fa[FM], fb[2];
+                wait_reads();
+                landed_b(std::integral_constant<int, 0>{});
+                landed_a();
+                fb[0].set(rb[0], sb1[0]);
+                auto multiply = [&](auto J, auto I, auto Q) {
+                    constexpr int j = decltype(J)::value, i = decltype(I)::value, q = decltype(Q)::value;
+                    acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j % 2].v[q], fa[i].v[q], acc[j][i], 0, 0, 0);
+                };
+                for (int t = 0; t < ktiles; ++t) {
+                    const int next = stage + 1 < STAGES ? stage + 1 : 0;
+                    static_for<FN>([&](auto J) {
+                        constexpr int j = decltype(J)::value, following = (j + 1) % FN;
+                        using Following = std::integral_constant<int, following>;
+                        if constexpr (j == FN - 1) turn(t, stage);
+                        read_b(Following{}, j == FN - 1 ? next : stage);
+                        fence();
+                        if constexpr (j == 0) {
+                            fa[0].set(ra[0], sa[0]);
+                            static_for<4 * FM>([&](auto S) {
+                                constexpr int i = decltype(S)::value / 4, q = decltype(S)::value % 4;
+                                if constexpr (i + 1 < FM) fa[i + 1].template quarter<q>(ra[i + 1], sa[i + 1]);
+                                if constexpr (i + 1 == FM && q == 0) {
+                                    wait_reads();
+                                    landed_b(Following{});
+                                }
+                                if constexpr (i + 1 == FM) fb[1].template quarter<q>(rb[1], sb1[1]);
+                                multiply(J, std::integral_constant<int, i>{}, std::integral_constant<int, q>{});
+                                fence();
+                            });
+                        } else {
+                            // (a quarter of the block for all fragments of A, so that no instruction waits for the one in front of it)
+                            static_for<4 * FM>([&](auto S) {
+                                constexpr int s = decltype(S)::value, q = s / FM, i = s % FM;
+                                if constexpr (s == 2 * FM) {
+                                    wait_reads();
+                                    landed_b(Following{});
+                                    if constexpr (j == FN - 1) landed_a();
+                                }
+                                if constexpr (s >= 2 * FM && (s - 2 * FM) % (FM / 2) == 0) fb[following % 2].template quarter<(s - 2 * FM) / (FM / 2)>(rb[following % 2], sb1[following % 2]);
+                                multiply(J, std::integral_constant<int, i>{}, std::integral_constant<int, q>{});
+                                if constexpr (j == FN - 1 && s < FM) read_a(std::integral_constant<int, s>{}, next);
+                                fence();
+                            });
+                        }
+                    });
+                    stage = next;
+                }
+            } else
             for (int t = 0; t < ktiles; ++t) {
                 const int next = stage + 1 < STAGES ? stage + 1 : 0;
+                typename FragmentOf<SUMS>::type fa[FM];
+                int ea[FM];
+                float s[FM];
                 static_for<FN>([&](auto J) {
-                    constexpr int j = decltype(J)::value, following = (j + 1) % FN;
-                    using Following = std::integral_constant<int, following>;
-                    if constexpr (j == FN - 1) turn(t, stage);
-                    read_b(Following{}, j == FN - 1 ? next : stage);
-                    fence();
+                    constexpr int j = decltype(J)::value;
+                    wait_reads();
+                    landed_b(J);
                     if constexpr (j == 0) {
-                        fa[0].set(ra[0], sa[0]);
-                        static_for<4 * FM>([&](auto S) {
-                            constexpr int i = decltype(S)::value / 4, q = decltype(S)::value % 4;
-                            if constexpr (i + 1 < FM) fa[i + 1].template quarter<q>(ra[i + 1], sa[i + 1]);
-                            if constexpr (i + 1 == FM && q == 0) {
-                                wait_reads();
-                                landed_b(Following{});
-                            }
-                            if constexpr (i + 1 == FM) fb[1].template quarter<q>(rb[1], sb1[1]);
-                            multiply(J, std::integral_constant<int, i>{}, std::integral_constant<int, q>{});
-                            fence();
-                        });
-                    } else {
-                        // (a quarter of the block for all fragments of A, so that no instruction waits for the one in front of it)
-                        static_for<4 * FM>([&](auto S) {
-                            constexpr int s = decltype(S)::value, q = s / FM, i = s % FM;
-                            if constexpr (s == 2 * FM) {
-                                wait_reads();
-                                landed_b(Following{});
-                                if constexpr (j == FN - 1) landed_a();
-                            }
-                            if constexpr (s >= 2 * FM && (s - 2 * FM) % (FM / 2) == 0) fb[following % 2].template quarter<(s - 2 * FM) / (FM / 2)>(rb[following % 2], sb1[following % 2]);
-                            multiply(J, std::integral_constant<int, i>{}, std::integral_constant<int, q>{});
-                            if constexpr (j == FN - 1 && s < FM) read_a(std::integral_constant<int, s>{}, next);
-                            fence();
+                        landed_a();
+                        static_for<FM>([&](auto I) {
+                            constexpr int i = decltype(I)::value;
+                            fa[i].set(join(ra[i][0], ra[i][1]));
+                            if constexpr (SUMS == SUMS_POW2) ea[i] = scale_bits(sa[i]);
+                            else if constexpr (SUMS == SUMS_SQUARE) s[i] = sa[i] * sb1[0];
+                            else s[i] = sa[i];
                         });
                     }
+                    typename FragmentOf<SUMS>::type fb;
+                    fb.set(join(rb[j % 2][0], rb[j % 2][1]));
+                    if constexpr (j + 1 < FN) {
+                        read_b(std::integral_constant<int, j + 1>{}, stage);
+                    } else {
+                        turn(t, stage);
+                        read_b(std::integral_constant<int, 0>{}, next);       // (behind the last K-tile: nobody uses them)
+                    }
+                    fence();
+                    constexpr int LATER = FM < 3 ? FM - 1 : 2;      // a block's sum is scaled that many fragments later, when it is there
+                    floatx4 d[LATER + 1];
+                    static_for<FM>([&](auto I) {
+                        constexpr int i = decltype(I)::value;
+                        if constexpr (SUMS == SUMS_POW2) {
+                            add_block_pow2(acc[j][i], fb, fa[i], scale_bits(sb1[j % 2]), ea[i]);
+                        } else {
+                            d[i % (LATER + 1)] = block_sum(fb, fa[i]);
+                            if constexpr (i >= LATER) add_scaled(acc[j][i - LATER], d[(i - LATER) % (LATER + 1)], s[i - LATER], sb4[j % 2]);
+                            if constexpr (i == FM - 1)
+                                static_for<LATER>([&](auto L) {
+                                    constexpr int l = FM - LATER + decltype(L)::value;
+                                    add_scaled(acc[j][l], d[l % (LATER + 1)], s[l], sb4[j % 2]);
+                                });
+                        }
+                        if constexpr (j == FN - 1) read_a(I, next);
+                        fence();
+                    });
                 });
                 stage = next;
             }
-        } else
-        for (int t = 0; t < ktiles; ++t) {
-            const int next = stage + 1 < STAGES ? stage + 1 : 0;
-            typename FragmentOf<SUMS>::type fa[FM];
-            int ea[FM];
-            float s[FM];
-            static_for<FN>([&](auto J) {
-                constexpr int j = decltype(J)::value;
-                wait_reads();
-                landed_b(J);
-                if constexpr (j == 0) {
-                    landed_a();
-                    static_for<FM>([&](auto I) {
-                        constexpr int i = decltype(I)::value;
-                        fa[i].set(join(ra[i][0], ra[i][1]));
-                        if constexpr (SUMS == SUMS_POW2) ea[i] = scale_bits(sa[i]);
-                        else if constexpr (SUMS == SUMS_SQUARE) s[i] = sa[i] * sb1[0];
-                        else s[i] = sa[i];
-                    });
-                }
-                typename FragmentOf<SUMS>::type fb;
-                fb.set(join(rb[j % 2][0], rb[j % 2][1]));
-                if constexpr (j + 1 < FN) {
-                    read_b(std::integral_constant<int, j + 1>{}, stage);
-                } else {
-                    turn(t, stage);
-                    read_b(std::integral_constant<int, 0>{}, next);       // (behind the last K-tile: nobody uses them)
-                }
-                fence();
-                constexpr int LATER = FM < 3 ? FM - 1 : 2;      // a block's sum is scaled that many fragments later, when it is there
-                floatx4 d[LATER + 1];
-                static_for<FM>([&](auto I) {
-                    constexpr int i = decltype(I)::value;
-                    if constexpr (SUMS == SUMS_POW2) {
-                        add_block_pow2(acc[j][i], fb, fa[i], scale_bits(sb1[j % 2]), ea[i]);
-                    } else {
-                        d[i % (LATER + 1)] = block_sum(fb, fa[i]);
-                        if constexpr (i >= LATER) add_scaled(acc[j][i - LATER], d[(i - LATER) % (LATER + 1)], s[i - LATER], sb4[j % 2]);
-                        if constexpr (i == FM - 1)
-                            static_for<LATER>([&](auto L) {
-                                constexpr int l = FM - LATER + decltype(L)::value;
-                                add_scaled(acc[j][l], d[l % (LATER + 1)], s[l], sb4[j % 2]);
-                            });
-                    }
-                    if constexpr (j == FN - 1) read_a(I, next);
-                    fence();
-                });
-            });
-            stage = next;
+            wait_reads();                     // the reads behind the last K-tile still write registers
+            landed_b(std::integral_constant<int, 0>{});
+            landed_a();
         }
-        wait_reads();                     // the reads behind the last K-tile still write registers
-        landed_b(std::integral_constant<int, 0>{});
-        landed_a();
     }
     if (ragged) {
         const int64_t at = static_cast<int64_t>(tile.b_end - 1) * SCALE_BLOCK;

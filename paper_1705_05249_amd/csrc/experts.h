@@ -162,35 +162,52 @@ struct RowTile {
     int64_t start;                       // the expert's first row
 };
 
-// The `tile`-th of all experts' tiles, counted expert by expert; false behind the last one.  Every wavefront finds it by itself: 64 experts
-// at a time, a running sum of their tiles over the lanes.  Offsets are held to 0 .. rows, whatever the array says.
-template <int LOG> __device__ inline bool find_row_tile(const Groups &g, int tile, RowTile *found)
+// 64 experts' tiles, a lane each: rows lo .. hi-1, and the tiles up to this lane's.  Offsets are held to 0 .. rows, whatever the array says.
+struct RowTiles {
+    int lo, hi, tiles, sum;
+};
+template <int LOG> __device__ inline RowTiles row_tiles(const Groups &g, int base)
 {
-    const int lane = threadIdx.x % 64;
-    const int rows = static_cast<int>(g.rows);
-    auto offset = [&](int e) {
-        const int o = g.offsets[e < g.count ? e : g.count];
+    const int rows = static_cast<int>(g.rows), e = base + static_cast<int>(threadIdx.x % 64);
+    auto offset = [&](int i) {
+        const int o = g.offsets[i < g.count ? i : g.count];
         return o < 0 ? 0 : o > rows ? rows : o;
     };
+    RowTiles t{offset(e), offset(e + 1), 0, 0};
+    t.tiles = t.hi > t.lo ? (t.hi - t.lo + (1 << LOG) - 1) >> LOG : 0;
+    t.sum = sum_up_to_lane(t.tiles);
+    return t;
+}
+
+// The `tile`-th of all experts' tiles, counted expert by expert; false behind the last one.  Every wavefront finds it by itself: 64 experts
+// at a time, a running sum of their tiles over the lanes.
+template <int LOG> __device__ inline bool find_row_tile(const Groups &g, int tile, RowTile *found)
+{
     int before = 0;
     for (int base = 0; base < g.count; base += 64) {
-        const int lo = offset(base + lane), hi = offset(base + lane + 1);
-        const int tiles = hi > lo ? (hi - lo + (1 << LOG) - 1) >> LOG : 0;
-        const int sum = sum_up_to_lane(tiles);
-        const int total = __builtin_amdgcn_readlane(sum, 63);          // (read by lane: the compiler has to know that all lanes go the same way)
+        const RowTiles t = row_tiles<LOG>(g, base);
+        const int total = __builtin_amdgcn_readlane(t.sum, 63);        // (read by lane: the compiler has to know that all lanes go the same way)
         if (tile < before + total) {
-            const uint64_t behind = __ballot(before + sum > tile);
+            const uint64_t behind = __ballot(before + t.sum > tile);
             const int at = __ffsll(static_cast<unsigned long long>(behind)) - 1;
-            const int first_tile = before + __builtin_amdgcn_readlane(sum - tiles, at);
+            const int first_tile = before + __builtin_amdgcn_readlane(t.sum - t.tiles, at);
             found->group = base + at;
-            found->start = __builtin_amdgcn_readlane(lo, at);
-            found->end = __builtin_amdgcn_readlane(hi, at);
+            found->start = __builtin_amdgcn_readlane(t.lo, at);
+            found->end = __builtin_amdgcn_readlane(t.hi, at);
             found->first = found->start + (static_cast<int64_t>(tile - first_tile) << LOG);
             return true;
         }
         before += total;
     }
     return false;
+}
+
+// How many tiles all experts' rows make
+template <int LOG> __device__ inline int count_row_tiles(const Groups &g)
+{
+    int total = 0;
+    for (int base = 0; base < g.count; base += 64) total += __builtin_amdgcn_readlane(row_tiles<LOG>(g, base).sum, 63);
+    return total;
 }
 
 // Column at which an expert's rows start in a transposed matrix: a block boundary, with at least a block's room for rounding up in front of the next
