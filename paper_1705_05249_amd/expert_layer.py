@@ -14,10 +14,22 @@ import torch
 from . import experts as X
 
 TYPES = {torch.float32: X.MG_F32, torch.float16: X.MG_F16, torch.bfloat16: X.MG_BF16}
+INDEX_TYPES = (torch.uint8, torch.int8, torch.int16, torch.int32, torch.int64)
 
 
 def _blocks(size):
     return -(-size // X.BLOCK)
+
+
+def _checked(name, tensor, shape, device, types=tuple(TYPES)):
+    """the tensor, dense: the library's calls take addresses and believe what they are told of the memory behind them"""
+    if tensor.dtype not in types:
+        raise TypeError(f"{name}: {tensor.dtype} is none of {', '.join(str(t) for t in types)}")
+    if tuple(tensor.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(tensor.shape)}, expected {tuple(shape)}")
+    if not tensor.is_cuda or (device is not None and tensor.device != device):
+        raise ValueError(f"{name}: on {tensor.device}, expected on {device or 'the GPU'}")
+    return tensor.contiguous()
 
 
 class Quantized:
@@ -43,20 +55,25 @@ class Routes:
     """tokens sorted by expert"""
 
     def __init__(self, ids, experts):
+        if ids.dim() != 2:
+            raise ValueError(f"ids: shape {tuple(ids.shape)}, expected tokens x fan")
+        ids = _checked("ids", ids, ids.shape, None, INDEX_TYPES)
         self.tokens, self.fan = ids.shape
         self.experts, self.rows = experts, ids.numel()
         new = lambda n: torch.empty(n, dtype=torch.int32, device=ids.device)  # noqa: E731
         self.offsets, self.position, self.source = new(experts + 1), new(self.rows), new(self.rows)
         need = X.mg_expert_sort_workspace_bytes(self.tokens, self.fan, experts)
         workspace = torch.empty(need, dtype=torch.uint8, device=ids.device) if need else None
-        X.mg_expert_sort(self.tokens, self.fan, experts, ids.int().contiguous(), self.offsets, self.position, self.source, workspace)
+        X.mg_expert_sort(self.tokens, self.fan, experts, ids.int(), self.offsets, self.position, self.source, workspace)
 
 
 class Experts:
     """the products of all experts with one matrix each: weights experts x n x k"""
 
     def __init__(self, weights):
-        self.weights = weights.contiguous()
+        if weights.dim() != 3:
+            raise ValueError(f"weights: shape {tuple(weights.shape)}, expected experts x n x k")
+        self.weights = _checked("weights", weights, weights.shape, None)
         self.experts, self.n, self.k = weights.shape
         self.w = Quantized(self.n, self.k, _blocks(self.n), self.experts)
         self.turned = Quantized(self.k, self.n, _blocks(self.k), self.experts)
@@ -64,8 +81,13 @@ class Experts:
 
     def quantize(self):
         """after a change of the weights: both forms that the products read, in one pass"""
-        w = self.weights
+        w = _checked("weights", self.weights, (self.experts, self.n, self.k), self.w.q.device)
         X.mg_block_quantize_batched(TYPES[w.dtype], X.MG_BLOCK_SQUARE, self.experts, self.n, self.k, w, self.k, self.n * self.k, *self.w.each(), *self.turned.each())
+
+    def _rows(self, name, tensor, routes, of_tokens, cols):
+        if routes.experts != self.experts:
+            raise ValueError(f"routes to {routes.experts} experts, weights of {self.experts}")
+        return _checked(name, tensor, (routes.tokens if of_tokens else routes.rows, cols), routes.offsets.device)
 
     def _product(self, routes, a, source, fan, b, n, k, dtype):
         c = torch.empty(routes.rows, n, dtype=dtype, device=a.q.device)
@@ -77,12 +99,14 @@ class Experts:
 
     def forward(self, routes, x, of_tokens):
         """x: a row for each token (of_tokens: the products fetch every route's) or for each routed row"""
+        x = self._rows("x", x, routes, of_tokens, self.k)
         a = Quantized(x.shape[0], self.k)
         X.mg_block_quantize(TYPES[x.dtype], X.MG_BLOCK_ROW, x.shape[0], self.k, x, self.k, *a.at(), *NONE)
         return self._product(routes, a, routes.source if of_tokens else None, routes.fan if of_tokens else 1, self.w, self.n, self.k, x.dtype)
 
     def backward(self, routes, x, of_tokens, dy):
         """(gradient of the routed rows of x, gradient of the weights in FP32)"""
+        x, dy = self._rows("x", x, routes, of_tokens, self.k), self._rows("dy", dy, routes, False, self.n)
         rows, columns = routes.rows, X.mg_grouped_columns(routes.rows, self.experts)
         d, d_turned, x_turned = Quantized(rows, self.n), Quantized(self.n, columns), Quantized(self.k, columns)
         source, fan = (routes.source, routes.fan) if of_tokens else (None, 1)
@@ -98,15 +122,23 @@ class Experts:
 
 
 class ExpertLayer:
-    """weights: W1 experts x hidden x width, W2 experts x width x hidden, of one type"""
+    """weights: W1 experts x hidden x width, W2 experts x width x hidden, of one type.  Outside autograd: results carry no graph, `backward` gives the gradients."""
 
     def __init__(self, w1, w2):
+        if w1.dim() != 3 or tuple(w2.shape) != (w1.shape[0], w1.shape[2], w1.shape[1]):
+            raise ValueError(f"weights: shapes {tuple(w1.shape)} and {tuple(w2.shape)}, expected experts x hidden x width and experts x width x hidden")
         self.up, self.down = Experts(w1), Experts(w2)
         self.width = w1.shape[2]
+        self.kept = None
 
     def forward(self, x, ids, gates):
-        """x: tokens x width; ids: tokens x fan (negative: dropped); gates: tokens x fan, FP32"""
-        x, gates = x.contiguous(), gates.contiguous()
+        """x: tokens x width; ids: tokens x fan (negative: dropped); gates: tokens x fan (numbers of 16 bits are widened to the FP32 that the kernels read)"""
+        device = self.up.w.q.device
+        if ids.dim() != 2:
+            raise ValueError(f"ids: shape {tuple(ids.shape)}, expected tokens x fan")
+        ids = _checked("ids", ids, ids.shape, device, INDEX_TYPES)
+        x = _checked("x", x, (ids.shape[0], self.width), device)
+        gates = _checked("gates", gates, ids.shape, device).float()
         routes = Routes(ids, self.up.experts)
         h = self.up.forward(routes, x, of_tokens=True)
         a = torch.relu(h).square_()
@@ -117,9 +149,11 @@ class ExpertLayer:
         return y
 
     def backward(self, dy):
-        """gradients (x, gates, W1, W2) of the last forward pass"""
+        """gradients (x, gates, W1, W2) of the last forward pass; dy of x's type, the gradients of gates and weights in FP32"""
+        if self.kept is None:
+            raise RuntimeError("backward without a forward pass")
         routes, x, gates, h, a, rows = self.kept
-        dy = dy.contiguous()
+        dy = _checked("dy", dy, x.shape, x.device, (x.dtype,))
         code = TYPES[dy.dtype]
         d_rows, d_gates = torch.empty_like(rows), torch.empty_like(gates)
         X.mg_expert_combine_grad(code, routes.tokens, routes.fan, self.width, dy, self.width, rows, self.width, routes.position, gates, d_rows, self.width, d_gates)
