@@ -32,6 +32,13 @@ def _checked(name, tensor, shape, device, types=tuple(TYPES)):
     return tensor.contiguous()
 
 
+def dense_ids(ids, experts):
+    """ids as the sort reads them; what 32 bits cannot hold stays outside 0 .. experts-1 instead of losing its upper half"""
+    if ids.dtype == torch.int64:
+        ids = ids.clamp(-1, experts)
+    return ids.to(torch.int32).contiguous()
+
+
 class Quantized:
     """an 8-bit matrix with its scales; rows start on 16 bytes"""
 
@@ -64,7 +71,7 @@ class Routes:
         self.offsets, self.position, self.source = new(experts + 1), new(self.rows), new(self.rows)
         need = X.mg_expert_sort_workspace_bytes(self.tokens, self.fan, experts)
         workspace = torch.empty(need, dtype=torch.uint8, device=ids.device) if need else None
-        X.mg_expert_sort(self.tokens, self.fan, experts, ids.int(), self.offsets, self.position, self.source, workspace)
+        X.mg_expert_sort(self.tokens, self.fan, experts, dense_ids(ids, experts), self.offsets, self.position, self.source, workspace)
 
 
 class Experts:

@@ -8,6 +8,7 @@ from torch._subclasses.fake_tensor import FakeTensorMode
 
 from paper_1705_05249_amd import experts as X
 from paper_1705_05249_amd import expert_layer as L
+from paper_1705_05249_amd.expert_layer import INDEX_TYPES
 
 BYTES = {X.MG_F32: 4, X.MG_F16: 2, X.MG_BF16: 2}
 TOKENS, WIDTH, HIDDEN, EXPERTS, FAN = 64, 128, 160, 5, 2
@@ -259,3 +260,15 @@ def test_no_tokens(calls):
     y = mine.forward(new(0, WIDTH), new(0, FAN, kind=torch.int64), new(0, FAN, kind=torch.float32))
     dx, d_gates, dw1, _ = mine.backward(y)
     assert y.shape == dx.shape == (0, WIDTH) and d_gates.shape == (0, FAN) and dw1.shape == (EXPERTS, HIDDEN, WIDTH)
+
+
+@pytest.mark.parametrize("ids", INDEX_TYPES)
+def test_ids_keep_their_meaning_in_32_bits(ids):
+    """numbers that 32 bits cannot hold belong to no expert, as in 64 bits"""
+    values = [0, 1, 4] + ([-1, -7] if ids != torch.uint8 else []) + ([5, 100] if ids.itemsize < 4 else [5, 1 << 20, (1 << 31) - 1])
+    if ids == torch.int64:
+        values += [1 << 31, 1 << 32, (1 << 32) + 1, -(1 << 32) + 2, (1 << 63) - 1, -(1 << 63)]
+    given = torch.tensor(values, dtype=ids).view(-1, 1)
+    got = L.dense_ids(given, EXPERTS)
+    assert got.dtype == torch.int32 and got.shape == given.shape and got.is_contiguous()
+    assert [v if 0 <= v < EXPERTS else None for v in got.view(-1).tolist()] == [v if 0 <= v < EXPERTS else None for v in values]
