@@ -5,7 +5,8 @@
     python -m paper_1705_05249_amd.expert_layer [tokens] [width] [hidden] [experts] [fan]
 
 trains a layer to answer as another one does and prints the loss and the time of a step.  PyTorch holds the memory, computes the elementwise
-activation and makes the update; everything else runs in the library's kernels.  All buffers are allocated by the layer, none by the library.
+activation and makes the update; everything else runs in the library's kernels.  All buffers are allocated by the layer, on
+its weights' device, none by the library; the calls go to torch's current stream, so that device has to be the current one.
 """
 import sys
 
@@ -82,8 +83,8 @@ class Experts:
             raise ValueError(f"weights: shape {tuple(weights.shape)}, expected experts x n x k")
         self.weights = _checked("weights", weights, weights.shape, None)
         self.experts, self.n, self.k = weights.shape
-        self.w = Quantized(self.n, self.k, _blocks(self.n), self.experts)
-        self.turned = Quantized(self.k, self.n, _blocks(self.k), self.experts)
+        self.w = Quantized(self.n, self.k, _blocks(self.n), self.experts, weights.device)
+        self.turned = Quantized(self.k, self.n, _blocks(self.k), self.experts, weights.device)
         self.quantize()
 
     def quantize(self):
@@ -94,7 +95,9 @@ class Experts:
     def _rows(self, name, tensor, routes, of_tokens, cols):
         if routes.experts != self.experts:
             raise ValueError(f"routes to {routes.experts} experts, weights of {self.experts}")
-        return _checked(name, tensor, (routes.tokens if of_tokens else routes.rows, cols), routes.offsets.device)
+        if routes.offsets.device != self.w.q.device:
+            raise ValueError(f"routes on {routes.offsets.device}, weights on {self.w.q.device}")
+        return _checked(name, tensor, (routes.tokens if of_tokens else routes.rows, cols), self.w.q.device)
 
     def _product(self, routes, a, source, fan, b, n, k, dtype):
         c = torch.empty(routes.rows, n, dtype=dtype, device=a.q.device)
@@ -107,7 +110,7 @@ class Experts:
     def forward(self, routes, x, of_tokens):
         """x: a row for each token (of_tokens: the products fetch every route's) or for each routed row"""
         x = self._rows("x", x, routes, of_tokens, self.k)
-        a = Quantized(x.shape[0], self.k)
+        a = Quantized(x.shape[0], self.k, device=x.device)
         X.mg_block_quantize(TYPES[x.dtype], X.MG_BLOCK_ROW, x.shape[0], self.k, x, self.k, *a.at(), *NONE)
         return self._product(routes, a, routes.source if of_tokens else None, routes.fan if of_tokens else 1, self.w, self.n, self.k, x.dtype)
 
@@ -115,7 +118,7 @@ class Experts:
         """(gradient of the routed rows of x, gradient of the weights in FP32)"""
         x, dy = self._rows("x", x, routes, of_tokens, self.k), self._rows("dy", dy, routes, False, self.n)
         rows, columns = routes.rows, X.mg_grouped_columns(routes.rows, self.experts)
-        d, d_turned, x_turned = Quantized(rows, self.n), Quantized(self.n, columns), Quantized(self.k, columns)
+        d, d_turned, x_turned = (Quantized(*size, device=dy.device) for size in ((rows, self.n), (self.n, columns), (self.k, columns)))
         source, fan = (routes.source, routes.fan) if of_tokens else (None, 1)
         X.mg_block_quantize_grouped(TYPES[dy.dtype], self.experts, routes.offsets, rows, self.n, dy, self.n, None, 1, *d.at(), *d_turned.at())
         X.mg_block_quantize_grouped(TYPES[x.dtype], self.experts, routes.offsets, rows, self.k, x, self.k, source, fan, *NONE, *x_turned.at())

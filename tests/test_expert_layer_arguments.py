@@ -272,3 +272,18 @@ def test_ids_keep_their_meaning_in_32_bits(ids):
     got = L.dense_ids(given, EXPERTS)
     assert got.dtype == torch.int32 and got.shape == given.shape and got.is_contiguous()
     assert [v if 0 <= v < EXPERTS else None for v in got.view(-1).tolist()] == [v if 0 <= v < EXPERTS else None for v in values]
+
+
+def test_memory_is_on_the_device_of_the_arguments(calls):
+    """whatever that is called, and none of them mixed"""
+    on = "cuda:1"
+    mine = L.ExpertLayer(new(EXPERTS, HIDDEN, WIDTH, device=on), new(EXPERTS, WIDTH, HIDDEN, device=on))
+    y = mine.forward(new(TOKENS, WIDTH, device=on), new(TOKENS, FAN, kind=torch.int64, device=on), new(TOKENS, FAN, device=on))
+    parts = [y, *mine.backward(y), mine.up.w.q, mine.up.turned.s, mine.down.w.s]
+    assert {str(t.device) for t in parts} == {on}
+    with pytest.raises(ValueError, match="x"):
+        mine.forward(new(TOKENS, WIDTH), new(TOKENS, FAN, kind=torch.int64, device=on), new(TOKENS, FAN, device=on))
+    with pytest.raises(ValueError, match="x"):
+        mine.up.forward(L.Routes(new(TOKENS, FAN, kind=torch.int32, device=on), EXPERTS), new(TOKENS, WIDTH), True)
+    with pytest.raises(ValueError, match="weights"):
+        mine.up.forward(L.Routes(new(TOKENS, FAN, kind=torch.int32), EXPERTS), new(TOKENS, WIDTH), True)
