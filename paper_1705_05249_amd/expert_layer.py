@@ -141,8 +141,9 @@ class ExpertLayer:
         self.width = w1.shape[2]
         self.kept = None
 
-    def forward(self, x, ids, gates):
-        """x: tokens x width; ids: tokens x fan (negative: dropped); gates: tokens x fan (numbers of 16 bits are widened to the FP32 that the kernels read)"""
+    def forward(self, x, ids, gates, keep=True):
+        """x: tokens x width; ids: tokens x fan (negative: dropped); gates: tokens x fan (numbers of 16 bits are widened to the FP32 that the kernels read);
+        keep: hold on to what `backward` reads, in place of an earlier call's (without: to nothing, as for tokens that are served)"""
         device = self.up.w.q.device
         if ids.dim() != 2:
             raise ValueError(f"ids: shape {tuple(ids.shape)}, expected tokens x fan")
@@ -155,13 +156,13 @@ class ExpertLayer:
         rows = self.down.forward(routes, a, of_tokens=False)
         y = torch.empty_like(x)
         X.mg_expert_combine(TYPES[x.dtype], routes.tokens, routes.fan, self.width, rows, self.width, routes.position, gates, y, self.width)
-        self.kept = routes, x, gates, h, a, rows
+        self.kept = (routes, x, gates, h, a, rows) if keep else None
         return y
 
     def backward(self, dy):
         """gradients (x, gates, W1, W2) of the last forward pass; dy of x's type, the gradients of gates and weights in FP32"""
         if self.kept is None:
-            raise RuntimeError("backward without a forward pass")
+            raise RuntimeError("backward without a forward pass that kept its activations")
         routes, x, gates, h, a, rows = self.kept
         dy = _checked("dy", dy, x.shape, x.device, (x.dtype,))
         code = TYPES[dy.dtype]
@@ -183,7 +184,7 @@ def main(tokens=4096, width=1024, hidden=2048, experts=16, fan=2, steps=20, dtyp
     ids = torch.topk(normal(tokens, experts), fan).indices
     gates = torch.softmax(normal(tokens, fan), 1)
     x = normal(tokens, width).to(dtype)
-    target = teacher.forward(x, ids, gates)
+    target = teacher.forward(x, ids, gates, keep=False)
     begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     for step in range(steps):
         begin.record()
@@ -198,7 +199,7 @@ def main(tokens=4096, width=1024, hidden=2048, experts=16, fan=2, steps=20, dtyp
         torch.cuda.synchronize()
         loss = float(dy.float().square().mean())
         print(f"step {step:3d}  loss {loss:.4f}  {begin.elapsed_time(end):.3f} ms", flush=True)
-    one = layer.forward(x[:1], ids[:1], gates[:1])                     # a token that is being generated
+    one = layer.forward(x[:1], ids[:1], gates[:1], keep=False)         # a token that is being generated
     print(f"one token: {float((one - target[:1]).float().square().mean()):.4f}")
 
 

@@ -287,3 +287,15 @@ def test_memory_is_on_the_device_of_the_arguments(calls):
         mine.up.forward(L.Routes(new(TOKENS, FAN, kind=torch.int32, device=on), EXPERTS), new(TOKENS, WIDTH), True)
     with pytest.raises(ValueError, match="weights"):
         mine.up.forward(L.Routes(new(TOKENS, FAN, kind=torch.int32), EXPERTS), new(TOKENS, WIDTH), True)
+
+
+def test_a_served_call_keeps_nothing(calls):
+    """neither its own activations nor an earlier call's, which would not belong to its answer"""
+    mine = layer()
+    mine.forward(*given())
+    y = mine.forward(*given(), keep=False)
+    assert mine.kept is None
+    with pytest.raises(RuntimeError):
+        mine.backward(y)
+    mine.forward(*given())
+    mine.backward(y)
