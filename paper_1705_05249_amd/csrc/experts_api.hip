@@ -26,7 +26,7 @@ size_t usable(const void *workspace, size_t bytes) { return workspace != nullptr
 mg_status quantize(QuantizeProblem &p, int block, int64_t turned_cols)
 {
     if (!extent(p.rows) || !extent(p.cols)) return MG_ERR_DIM;
-    if (__int128(blocks(p.rows) + p.groups.count) * blocks(p.cols) * 8 > MOST_PIECES) return MG_ERR_DIM;
+    if (__int128(blocks(p.rows) + p.groups.count) * blocks(p.cols) * 8 >= MOST_PIECES) return MG_ERR_DIM;
     const bool q = p.Q != nullptr || p.S != nullptr, t = p.T != nullptr || p.ST != nullptr;
     if (!at_least(p.ldx, p.cols)) return MG_ERR_LDA;
     if (q && !at_least(p.ldq, p.cols)) return MG_ERR_LDB;

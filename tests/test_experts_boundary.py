@@ -200,3 +200,16 @@ def test_grouped_quantize_errors_in_order():
     def call(offsets, ldx):
         return X.mg_block_quantize_grouped(X.MG_F32, 2, offsets, 4, 8, FAKE, ldx, None, 1, FAKE, 8, FAKE, 1, None, 1, None, 1, stream=0, check=False)
     assert call(None, 7) == -5 and call(None, 8) == -8
+
+
+def test_a_launch_of_2_to_32_threads_is_refused_as_a_size():
+    """2^35 elements to quantise would be 2^24 work-groups of 256 threads, one more than a launch holds: a size (-4), not a launch that fails"""
+    def call(rows, cols):
+        tail = (None, cols, FAKE, cols, FAKE, cols >> 7, None, 1, None, 1)
+        return X.mg_block_quantize(X.MG_BF16, X.MG_BLOCK_ROW, rows, cols, *tail, stream=0, check=False)
+    assert call(1 << 18, 1 << 17) == -4 and call(1 << 21, 1 << 14) == -4
+    assert call((1 << 18) - 128, 1 << 17) == -8 and call(1 << 18, (1 << 17) - 128) == -8
+
+    def grouped(rows, groups, cols=1 << 14):
+        return X.mg_block_quantize_grouped(X.MG_BF16, groups, FAKE, rows, cols, None, cols, None, 1, FAKE, cols, FAKE, cols >> 7, None, 1, None, 1, stream=0, check=False)
+    assert grouped((1 << 21) - 128, 1) == -4 and grouped((1 << 21) - 256, 1) == -8
