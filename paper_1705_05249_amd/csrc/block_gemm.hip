@@ -1,5 +1,4 @@
-// Host side of the 8-bit products (which kernel, how many slices), the kernel for operands at any address, the kernel for few rows, and the
-// launch that adds slices.
+// Host side of the 8-bit products, the kernel for operands at any address, and the launch that adds slices.
 #include "internal.h"
 #include "block_gemm_kernel.h"
 
@@ -134,100 +133,6 @@ __global__ __launch_bounds__(256) void block_add_slices_kernel(const BlockArgs a
     write_block(whole, many ? static_cast<int>(row / args.m) : 0, many ? row % args.m : row, col, sum);
 }
 
-constexpr int TILE_ANY = -1, TILE_ANY_64 = -2; // the kernel for operands at any address
-constexpr int TILE_FEW = -3;                   // the kernel for few rows in one operand
-
-struct Plan {
-    int tile;                                 // BlockDmaTile or one of those
-    int tiles_m, tiles_n, slices;
-    int fragments;                            // TILE_FEW
-    bool few_b;
-};
-
-int64_t output_rows(int mode, int groups, int64_t m) { return mode == BLOCK_SUM ? groups * m : m; }
-
-// What a kernel takes, in us, measured with random operands.  A compute unit that has one of its tiles: `alone` for a block of 128 of the sum while half of the
-// chip is idle, `full` while all of it is busy; with n of them n * `each` (two work-groups of 128 x 128 share a compute unit, two to four of 64 x 64).
-// Around the sum: `start`, and `more` for every round of tiles (C leaves).  Over 2048 x 2048 .. 8192 x 4096 with sums of 512 to 8192 within a tenth of the measured,
-// but for `each` of 128 x 128: 0.515 with uniform bits, where the clock stays up; with activations the smaller tiles slow down more than the large ones.
-struct Cost {
-    double alone, full, each, start, more;
-};
-Cost cost_of(int tile, int sums)
-{
-    const bool fp32 = sums_fp32(sums);
-    Cost c{};
-    switch (tile) {
-        case DMA_256: c = fp32 ? Cost{1.47, 1.7, 1.6, 4, 7} : Cost{1.38, 1.6, 1.55, 4, 6.5}; break;
-        case DMA_128: c = fp32 ? Cost{1.05, 1.19, 0.93, 3, 1.5} : Cost{0.6, 0.75, 0.6, 3, 1}; break;
-        case DMA_64: c = fp32 ? Cost{0.5, 0.52, 0.37, 3, 0.7} : Cost{0.3, 0.31, 0.24, 3, 0.5}; break;
-        case TILE_ANY: c = fp32 ? Cost{1.8, 2.1, 1.5, 4, 1.5} : Cost{1.2, 1.4, 1.0, 4, 1.5}; break;
-        default: c = fp32 ? Cost{0.9, 1.0, 0.6, 3.5, 0.7} : Cost{0.6, 0.66, 0.4, 3.5, 0.7}; break;
-    }
-    // scales of any value are multiplied in beside the matrix instructions (4096^3: 66 -> 76 us; 128 x 4096 x 4096 on 64 x 64 tiles 13 -> 17)
-    const double scaling = sums == SUMS_POW2 || sums == SUMS_FP32_POW2 ? 1. : tile == DMA_256 ? 1.17 : 1.4;
-    c.alone *= scaling;
-    c.full *= scaling;
-    c.each *= scaling;
-    return c;
-}
-
-// Which kernel and how many slices of the sum: the least of the estimates.  Slices cost a launch that reads what they wrote, and no slice gets fewer than four blocks.
-Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums, bool aligned, size_t workspace)
-{
-    Plan best{};
-    best.slices = 1;
-    const int64_t few = mode == BLOCK_ROWS ? ceil_div(m, groups) : m < n ? m : n;       // rows of A (for an expert), or of the smaller operand
-    // The kernel for few rows reads them once for every 16 of the others.  8192 x 8192: 4 rows 15.9 us, 16 rows 22, 32 rows 33, 64 x 64 tiles 19; 4096 x 4096: 32 rows 10,
-    // 64 x 64 tiles 11.5.  32 experts, 2048 x 4096 each: 16 rows 79 us, 17 rows 92,
-    // 64 x 64 tiles 84.
-    if (mode != BLOCK_SUM && (few <= 8 || (mode == BLOCK_ROWS && few <= 16) || (mode == BLOCK_DENSE && few <= 32 && (m < n ? n : m) * k <= int64_t(1) << 25))) {
-        best.tile = TILE_FEW;
-        best.few_b = mode == BLOCK_DENSE && n < m;
-        best.fragments = few <= 16 ? 1 : 2;
-        return best;
-    }
-    const int64_t batch = mode == BLOCK_SUM ? groups : 1;
-    const double blocks = static_cast<double>(ceil_div(k, SCALE_BLOCK)) / batch + (mode == BLOCK_SUM ? 0.5 : 0.);
-    const double one = static_cast<double>(output_rows(mode, groups, m)) * n * 4;
-    double least = 0;
-    for (const int tile : {int(DMA_256), int(DMA_128), int(DMA_64), TILE_ANY, TILE_ANY_64}) {
-        if (aligned != (tile >= 0)) continue;
-        const int64_t any = tile == TILE_ANY ? 128 : 64, bm = tile < 0 ? any : block_dma_rows(tile), bn = tile < 0 ? any : block_dma_cols(tile, sums);
-        Plan p{};
-        p.tile = tile;
-        p.tiles_m = static_cast<int>(ceil_div(m, bm) + (mode == BLOCK_ROWS ? groups : 0));
-        p.tiles_n = static_cast<int>(ceil_div(n, bn));
-        // (every expert's last tile is half full, if it has rows at all)
-        const int64_t ends = groups < m / bm ? groups / 2 : 0;
-        const int64_t tiles = (mode == BLOCK_ROWS ? ceil_div(m, bm) + ends : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * batch;
-        const Cost c = cost_of(tile, sums);
-        for (int s = 1; s <= 16; s *= 2) {
-            if (s > 1 && (blocks / s < 4 || one * s > static_cast<double>(workspace) || tiles * s > 512)) break;
-            const double per_unit = static_cast<double>(ceil_div(tiles * s, 256));
-            const double a_block = per_unit > 1 ? (c.each * per_unit > c.full ? c.each * per_unit : c.full) : tiles * s <= 128 ? c.alone : c.full;
-            const double us = c.start + c.more * per_unit + blocks / s * a_block + (s > 1 ? 4 + one * (s + 1) / 4e6 : 0);
-            if (least == 0 || us < least) {
-                least = us;
-                best = p;
-                best.slices = s;
-            }
-        }
-    }
-    return best;
-}
-
-// Rows on 16 bytes, and 32-bit offsets: inside a tile of 256 rows, or from the first row of A where rows are indexed
-bool dma_operands(const BlockProblem &p)
-{
-    auto on16 = [](const void *x, int64_t a, int64_t b) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && a % 16 == 0 && b % 16 == 0; };
-    if (!on16(p.A, p.lda, 0) || !on16(p.B, p.ldb, p.mode == BLOCK_ROWS ? p.stride_b : 0)) return false;
-    const __int128 rows_a = p.mode == BLOCK_ROWS && p.groups.source != nullptr ? p.m : 256, most = (__int128(1) << 31) - (1 << 20);
-    const __int128 along = p.mode == BLOCK_SUM ? p.lda : p.k;
-    return rows_a * p.lda + along < most && __int128(256) * p.ldb + along < most && (rows_a * p.ldsa + along / 128) * 4 < most &&
-           (__int128(256) * p.ldsb + along / 128) * 4 < most;
-}
-
 template <int MODE> hipError_t launch_mode(const BlockProblem &p, const BlockArgs &args, int sums, int tile)
 {
     if (tile >= 0) {
@@ -262,8 +167,8 @@ size_t block_gemm_workspace(int mode, int groups, int64_t m, int64_t n, int64_t 
 
 hipError_t launch_block_gemm(const BlockProblem &p)
 {
-    const int sums = p.fp32_sums ? (p.pow2 ? SUMS_FP32_POW2 : SUMS_FP32) : p.pow2 ? SUMS_POW2 : p.b_square ? SUMS_SQUARE : SUMS_ANY;
-    const Plan how = plan(p.mode, p.groups.count, p.m, p.n, p.k, sums, dma_operands(p), p.workspace == nullptr ? 0 : p.workspace_bytes);
+    const int sums = block_sums(p);
+    const Plan how = plan(p);
     BlockArgs args{};
     args.A = p.A; args.lda = p.lda; args.SA = p.SA; args.ldsa = p.ldsa; args.a_shift = p.a_square ? 7 : 0;
     args.B = p.B; args.ldb = p.ldb; args.SB = p.SB; args.ldsb = p.ldsb; args.b_shift = p.b_square ? 7 : 0;

@@ -14,6 +14,7 @@
 // columns of one row of C, and with square blocks of B (weights) the scale of B is one number for all of a fragment.
 #pragma once
 
+#include "block_plan.h"
 #include "experts.h"
 #include "mfma_kernel.h"
 
@@ -92,16 +93,6 @@ template <int MODE, int LOG_BM, int BN> __device__ inline bool block_tile(const 
     return true;
 }
 
-// How a kernel sums: on the FP8 pipes with scales that are powers of two or any (SUMS_SQUARE: any, and square blocks of B, so that all of a
-// fragment's rows of B have one), on the FP16 pipes with any scales, or on the bfloat16 pipes, whose operands take scales that are powers of two
-// into their exponents while they are widened
-enum BlockSums { SUMS_POW2 = 0, SUMS_ANY = 1, SUMS_FP32 = 2, SUMS_SQUARE = 3, SUMS_FP32_POW2 = 4 };
-constexpr bool sums_fp32(int sums) { return sums == SUMS_FP32 || sums == SUMS_FP32_POW2; }
-
-// Kernels for operands whose rows start on 16 bytes (block_dma_kernel.h), by their tile
-enum BlockDmaTile { DMA_256 = 0, DMA_128 = 1, DMA_64 = 2 };
-constexpr int block_dma_rows(int tile) { return tile == DMA_256 ? 256 : tile == DMA_128 ? 128 : 64; }
-constexpr int block_dma_cols(int tile, int sums) { return tile == DMA_256 && sums_fp32(sums) ? 128 : block_dma_rows(tile); }
 hipError_t launch_block_dma_dense(const BlockArgs &args, int sums, int tile, hipStream_t stream);
 hipError_t launch_block_dma_rows(const BlockArgs &args, int sums, int tile, hipStream_t stream);
 hipError_t launch_block_dma_sum(const BlockArgs &args, int sums, int tile, hipStream_t stream);
