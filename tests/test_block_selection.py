@@ -1,0 +1,31 @@
+"""Which kernel a product of 8-bit matrices takes: that the cases of test_gpu_block_tiles.py run what they say, and what the rules are to keep."""
+import pytest
+
+from paper_1705_05249_amd import experts as X
+from tests import test_gpu_block_tiles as T
+from tests.block_choice import choices
+
+
+def problem(case):
+    mode, kernel, sums, m, n, k, _ = case
+    lead, start = T.leading(case)
+    experts = {"dense": 0, "rows": T.FIVE, "sum": T.TWO}[mode]
+    need = {"dense": lambda: X.mg_block_gemm_workspace_bytes(m, n, k), "rows": lambda: X.mg_block_gemm_grouped_workspace_bytes(experts, m, n, k),
+            "sum": lambda: X.mg_block_gemm_grouped_sum_workspace_bytes(experts, k, m, n)}[mode]()
+    return dict(mode=mode, m=m, n=n, k=k, pow2=sums.endswith("pow2"), fp32=sums in T.FP32_SUMS, b_square=sums == "square", groups=experts, lda=lead, ldb=lead, start=start,
+                workspace=need)
+
+
+def test_the_cases_run_the_kernels_they_name():
+    cases = T.DENSE + T.ROWS + T.SUM
+    for case, (kernel, sums, slices, _) in zip(cases, choices([problem(c) for c in cases])):
+        assert (kernel, sums, slices > 1) == (case[1], case[2], case[6]), (case, kernel, sums, slices)
+
+
+def test_every_kernel_has_a_case():
+    """aligned tiles and those for any address, every way of summing that a call of the mode can ask for"""
+    every = ("pow2", "any", "square", "fp32", "fp32 pow2")
+    for cases, sums in ((T.DENSE, every), (T.ROWS, every), (T.SUM, ("pow2", "any", "fp32", "fp32 pow2"))):
+        for kernel in ("256", "128", "any 128"):
+            assert {c[2] for c in cases if c[1] == kernel} == set(sums), (cases[0][0], kernel)
+    assert {c[2] for c in T.ROWS if c[1] == "few"} == set(every)

@@ -1,0 +1,205 @@
+"""Every kernel of the 8-bit products at sizes where it is the one that is taken, in all its ways of summing: whole numbers, whose products and sums are exact in
+each of them, at sizes that end inside a tile, a scale block and a piece of 16 bytes.  (That these cases take the kernels they name: test_block_selection.py.)
+
+Exact on the FP8 pipes too: elements up to 8 make products within 2^6 of each other, and the pipes keep what is within 2^13 of the largest of eight.  Everything
+stays below 2^24 of its last place: 2^6 * 20000 terms at most on average cancel, 8 * sqrt(20000) * 2^6 < 2^17, scales and halves add five binary places."""
+import pytest
+import torch
+
+from paper_1705_05249_amd import experts as X
+
+pytestmark = pytest.mark.gpu
+CODE = {"f32": X.MG_F32, "f16": X.MG_F16, "bf16": X.MG_BF16}
+TYPE = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+FP32_SUMS = ("fp32", "fp32 pow2")
+
+# (mode, kernel, sums, m, n, k, sliced): rows of C, or routed rows, or rows of each expert's C; k: the sum, or the routed rows
+DENSE = [("dense", kernel, sums, *size) for kernel, table in {
+    "256": {"square": [(2600, 4700, 400, False), (3590, 3601, 393, False), (520, 1800, 9000, True)], "any": [(2600, 4700, 393, False), (520, 1800, 9000, True)],
+            "pow2": [(2600, 4700, 1000, False), (5500, 5450, 400, False), (520, 1800, 20000, True)],
+            "fp32": [(1290, 3100, 1999, False), (140, 3100, 9000, True)], "fp32 pow2": [(1290, 3100, 4000, False), (1281, 3109, 4009, False), (520, 1800, 20000, True)]},
+    "128": {sums: [(520, 4100, 400, False), (641, 4099, 393, False), (140, 1500, 4000, True)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
+    "any 128": {sums: [(520, 5450, 400, False), (1929, 1901, 393, False), (140, 3100, 4000, True)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
+}.items() for sums, sizes in table.items() for size in sizes]
+
+ROWS = [("rows", kernel, sums, *size) for kernel, table in {
+    "256": {"square": [(2050, 5450, 400, False), (2600, 140, 20000, True)], "any": [(2050, 5450, 393, False)], "pow2": [(2050, 5450, 1000, False), (900, 900, 20000, True)],
+            "fp32": [(1500, 2600, 999, False), (2600, 140, 9000, True)], "fp32 pow2": [(1500, 4700, 400, False), (1500, 4700, 393, False), (1290, 520, 9000, True)]},
+    "128": {sums: [(520, 3100, 400, False), (520, 3111, 393, False), (520, 140, 9000, True)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
+    "64": {sums: [(301, 300, 393, False), (140, 140, 4000, True)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
+    "any 128": {sums: [(520, 3100, 393, False)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
+    "any 64": {sums: [(301, 300, 393, False)] for sums in ("pow2", "square", "fp32", "fp32 pow2")},
+    "few": {sums: [(70, 300, 393, False), (13, 2100, 1024, False), (80, 9000, 272, False)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
+}.items() for sums, sizes in table.items() for size in sizes]
+
+SUM = [("sum", kernel, sums, *size) for kernel, table in {
+    "256": {"any": [(1290, 4700, 400, False), (140, 3100, 20000, True)], "pow2": [(1290, 4700, 1000, False), (520, 1800, 20000, True)],
+            "fp32": [(1500, 1500, 2000, False), (140, 3100, 9000, True)], "fp32 pow2": [(1500, 1500, 9000, False), (520, 1800, 20000, True)]},
+    "128": {sums: [(1030, 1500, 400, False), (140, 900, 20000, True)] for sums in ("pow2", "any", "fp32", "fp32 pow2")},
+    "64": {sums: [(300, 301, 400, False)] for sums in ("pow2", "any", "fp32", "fp32 pow2")},
+    "any 128": {sums: [(1150, 1411, 400, False), (140, 1500, 9000, True)] for sums in ("pow2", "any", "fp32", "fp32 pow2")},
+    "any 64": {sums: [(300, 301, 400, False), (140, 140, 4000, True)] for sums in ("pow2", "any", "fp32", "fp32 pow2")},
+}.items() for sums, sizes in table.items() for size in sizes]
+FIVE, TWO = 5, 2                                    # experts of ROWS and of SUM
+
+
+def leading(case):
+    """distance of an operand's rows, and where the first one starts"""
+    mode, kernel, _, _, _, k, _ = case
+    along = X.mg_grouped_columns(k, TWO) if mode == "sum" else k
+    return (along + 3, 1) if kernel.startswith("any") else (-(-along // 16) * 16, 0)
+
+
+def kinds(sums):
+    """(type of C, flags) that are summed so"""
+    scales = X.MG_SCALES_POW2 if sums.endswith("pow2") else X.MG_SCALES_ANY
+    return (("f32", scales), ("bf16", scales | X.MG_SUMS_FP32)) if sums in FP32_SUMS else (("bf16", scales), ("f16", scales))
+
+
+class Operand:
+    """whole numbers up to 8 with scales of 1/2 to 2: NaN between the rows and behind the scales, and the values"""
+
+    def __init__(self, gen, rows, k, square, lead, start):
+        whole = torch.randint(-8, 9, (rows, k), generator=gen, device="cuda").float()
+        blocks = -(-k // 128)
+        tall = -(-rows // 128) if square else rows
+        scales = torch.exp2(torch.randint(-1, 2, (tall, blocks), generator=gen, device="cuda").float())
+        stored = torch.full((start + rows * lead + 16,), 0x7F, dtype=torch.uint8, device="cuda")
+        stored[start:start + rows * lead].view(rows, lead)[:, :k] = whole.to(torch.float8_e4m3fn).view(torch.uint8)
+        self.q, self.lead, self.lds = stored[start:], lead, blocks + 1
+        self.s = torch.full((tall, blocks + 1), float("nan"), device="cuda")
+        self.s[:, :blocks] = scales
+        spread = scales.double().repeat_interleave(128, 1)[:, :k]
+        self.values = whole.double() * (spread.repeat_interleave(128, 0)[:rows] if square else spread)
+        self.block = X.MG_BLOCK_SQUARE if square else X.MG_BLOCK_ROW
+
+    def at(self):
+        return self.q, self.lead, self.s, self.lds
+
+
+def scratch(need):
+    return torch.empty(need, dtype=torch.uint8, device="cuda").random_(0, 255) if need else None
+
+
+SCALARS = ((1.0, 0.0), (0.5, -2.0))
+
+
+@pytest.mark.parametrize("case", DENSE, ids=str)
+def test_dense(case):
+    _, kernel, sums, m, n, k, sliced = case
+    gen = torch.Generator(device="cuda").manual_seed(m + n + k)
+    lead, start = leading(case)
+    square = sums == "square"
+    a, b = Operand(gen, m, k, not square and k % 2 == 0, lead, start), Operand(gen, n, k, square, lead, 3 * start)
+    product = a.values @ b.values.T
+    ws = scratch(X.mg_block_gemm_workspace_bytes(m, n, k))
+    assert (ws is not None) >= sliced
+    for i, (kind, scales) in enumerate(kinds(sums)):
+        for alpha, beta in SCALARS:
+            row = (i + (beta != 0)) % 2 == 0
+            # (column-major C: the operands change places)
+            p, q = (a, b) if row else (b, a)
+            want = alpha * product
+            old = torch.randint(-9, 10, (m, n + 5), generator=gen, device="cuda").to(TYPE[kind])
+            c = old.clone() if beta else torch.full_like(old, float("nan"))
+            before = c.clone()
+            print(case, kind, scales, alpha, beta, row, flush=True)
+            X.mg_block_gemm(X.MG_ROW_MAJOR if row else X.MG_COL_MAJOR, *((m, n) if row else (n, m)), k, alpha, scales, p.block, *p.at(), q.block, *q.at(), beta, CODE[kind], c,
+                            n + 5, ws)
+            torch.cuda.synchronize()
+            if beta:
+                want = want + beta * old[:, :n].double()
+            assert torch.equal(c[:, :n], want.to(TYPE[kind])), (kind, alpha, beta, row)
+            assert torch.equal(c[:, n:].nan_to_num(3.0), before[:, n:].nan_to_num(3.0)), "written outside C"
+
+
+def shares(total, experts):
+    """how many rows each expert has: most of them one, none another, and a few rows of no expert"""
+    counts = [0] * experts
+    kept = total - 3
+    counts[0] = kept // 3
+    counts[-1] = 1 if experts > 2 else 0
+    counts[experts // 2] += kept - sum(counts)
+    return counts
+
+
+@pytest.mark.parametrize("case", ROWS, ids=str)
+def test_rows_of_experts(case):
+    _, kernel, sums, rows, n, k, sliced = case
+    fan = 2 if rows % 2 == 0 else 1
+    gen = torch.Generator(device="cuda").manual_seed(rows + n + k)
+    lead, start = leading(case)
+    square = sums in ("square", "fp32")
+    counts = shares(rows, FIVE)
+    total, offsets = sum(counts), torch.tensor([0] + counts).cumsum(0).int()
+    weights = [Operand(gen, n, k, square, lead, 0) for _ in range(FIVE)]
+    held = torch.full((start + FIVE * n * lead + 16,), 0x7F, dtype=torch.uint8, device="cuda")
+    for e, w in enumerate(weights):
+        held[start + e * n * lead:start + (e + 1) * n * lead] = w.q[:n * lead]
+    B, SB = held[start:], torch.stack([w.s for w in weights])
+    source = torch.full((rows,), -1, dtype=torch.int32)
+    source[:total] = torch.randperm(rows)[:total].int()
+    ws = scratch(X.mg_block_gemm_grouped_workspace_bytes(FIVE, rows, n, k))
+    assert (ws is not None) >= sliced
+    for indexed in (True, False):
+        a = Operand(gen, rows // fan if indexed else rows, k, False, lead, start)
+        index = source[:total].long().cuda() // fan if indexed else torch.arange(total, device="cuda")
+        product = torch.cat([a.values[index[lo:lo + count]] @ w.values.T for lo, count, w in zip(offsets.tolist(), counts, weights)])
+        for kind, scales in kinds(sums):
+            alpha, beta = SCALARS[int(indexed) ^ (kind == "bf16")]
+            old = torch.randint(-9, 10, (rows, n + 3), generator=gen, device="cuda").to(TYPE[kind])
+            c = old.clone() if beta else torch.full_like(old, float("nan"))
+            before = c.clone()
+            print(case, kind, scales, alpha, beta, indexed, flush=True)
+            X.mg_block_gemm_grouped(FIVE, offsets.cuda(), rows, n, k, alpha, scales, *a.at(), source.cuda() if indexed else None, fan if indexed else 1, weights[0].block,
+                                    B, lead, n * lead, SB, SB.shape[2], SB.shape[1] * SB.shape[2], beta, CODE[kind], c, n + 3, ws)
+            torch.cuda.synchronize()
+            want = alpha * product
+            if beta:
+                want = want + beta * old[:total, :n].double()
+            assert torch.equal(c[:total, :n], want.to(TYPE[kind])), (kind, alpha, beta, indexed)
+            assert torch.equal(c[total:].nan_to_num(3.0), before[total:].nan_to_num(3.0)) and torch.equal(c[:, n:].nan_to_num(3.0), before[:, n:].nan_to_num(3.0))
+
+
+@pytest.mark.parametrize("case", SUM, ids=str)
+def test_sums_over_experts_rows(case):
+    _, kernel, sums, m, n, rows, sliced = case
+    gen = torch.Generator(device="cuda").manual_seed(m + n + rows)
+    lead, start = leading(case)
+    columns = X.mg_grouped_columns(rows, TWO)
+    ws = scratch(X.mg_block_gemm_grouped_sum_workspace_bytes(TWO, rows, m, n))
+    assert (ws is not None) >= sliced
+    for turn, counts in enumerate(([rows // 3 - 1, rows - rows // 3 - 4], [0, rows - 5])):
+        offsets = [0, counts[0], sum(counts)]
+        operands, values = [], []
+        for high, shift in ((m, start), (n, 3 * start)):
+            stored = torch.full((shift + high * lead + 16,), 0x7F, dtype=torch.uint8, device="cuda")
+            s = torch.full((high, columns // 128 + 1), float("nan"), device="cuda")
+            mine = []
+            for e, count in enumerate(counts):
+                part = Operand(gen, high, max(count, 1), False, -(-max(count, 1) // 128) * 128, 0)
+                mine.append(part.values if count else None)
+                if count == 0:
+                    continue
+                at, wide = -(-offsets[e] // 128) * 128 + 128 * e, -(-count // 128) * 128
+                view = stored[shift:shift + high * lead].view(high, lead)
+                view[:, at:at + wide] = 0
+                view[:, at:at + count] = part.q[:high * wide].view(high, wide)[:, :count]
+                s[:, at // 128:(at + wide) // 128] = part.s[:, :-1]
+            operands.append((stored[shift:], lead, s, s.shape[1]))
+            values.append(mine)
+        for kind, scales in kinds(sums):
+            alpha, beta = SCALARS[turn ^ (kind == "bf16")]
+            old = torch.randint(-9, 10, (TWO, m, n + 3), generator=gen, device="cuda").to(TYPE[kind])
+            c = old.clone() if beta else torch.full_like(old, float("nan"))
+            before = c.clone()
+            print(case, counts, kind, scales, alpha, beta, flush=True)
+            X.mg_block_gemm_grouped_sum(TWO, torch.tensor(offsets, dtype=torch.int32).cuda(), rows, m, n, alpha, scales, *operands[0], *operands[1], beta, CODE[kind], c, n + 3,
+                                        m * (n + 3), ws)
+            torch.cuda.synchronize()
+            for e, count in enumerate(counts):
+                want = alpha * (values[0][e] @ values[1][e].T) if count else torch.zeros(m, n, dtype=torch.float64, device="cuda")
+                if beta:
+                    want = want + beta * old[e, :, :n].double()
+                assert torch.equal(c[e, :, :n], want.to(TYPE[kind])), (kind, alpha, beta, e)
+            assert torch.equal(c[:, :, n:].nan_to_num(3.0), before[:, :, n:].nan_to_num(3.0)), "written outside C"
