@@ -99,12 +99,12 @@ inline Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums
     return best;
 }
 
-// Rows on 16 bytes, and 32-bit offsets: inside a tile of 256 rows, or from the first row of A where rows are indexed
+// Rows on 16 bytes, and 32-bit offsets: inside a tile of 256 rows, or from the first row of A where rows are indexed (of those there is one for every `fan` slots)
 inline bool dma_operands(const BlockProblem &p)
 {
     auto on16 = [](const void *x, int64_t a, int64_t b) { return reinterpret_cast<uintptr_t>(x) % 16 == 0 && a % 16 == 0 && b % 16 == 0; };
     if (!on16(p.A, p.lda, 0) || !on16(p.B, p.ldb, p.mode == BLOCK_ROWS ? p.stride_b : 0)) return false;
-    const __int128 rows_a = p.mode == BLOCK_ROWS && p.groups.source != nullptr ? p.m : 256, most = (__int128(1) << 31) - (1 << 20);
+    const __int128 rows_a = p.mode == BLOCK_ROWS && p.groups.source != nullptr ? ceil_div(p.m, p.groups.fan) : 256, most = (__int128(1) << 31) - (1 << 20);
     const __int128 along = p.mode == BLOCK_SUM ? p.lda : p.k;
     return rows_a * p.lda + along < most && __int128(256) * p.ldb + along < most && (rows_a * p.ldsa + along / 128) * 4 < most &&
            (__int128(256) * p.ldsb + along / 128) * 4 < most;

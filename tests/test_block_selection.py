@@ -29,3 +29,14 @@ def test_every_kernel_has_a_case():
         for kernel in ("256", "128", "any 128"):
             assert {c[2] for c in cases if c[1] == kernel} == set(sums), (cases[0][0], kernel)
     assert {c[2] for c in T.ROWS if c[1] == "few"} == set(every)
+
+
+def test_indexed_rows_are_as_far_apart_as_tokens():
+    """rows fetched by slot / fan: A has a row for each token, and only its size decides whether 32-bit offsets reach them"""
+    many = dict(mode="rows", m=65536 * 8, n=2048, k=4096, groups=64, fan=8, pow2=True, b_square=True, indexed=True)
+    assert choices([many])[0][0] == "256"                                       # A spans 2^28 bytes
+    last = (1 << 31) - (1 << 20) - 4096                                         # from there on offsets do not fit
+    rows = {fan: fan * (last // 4096) for fan in (1, 3, 64)}
+    for fan, m in rows.items():
+        fits, beyond = choices([dict(many, m=m - fan, fan=fan), dict(many, m=m + fan + 1, fan=fan)])
+        assert fits[0] == "256" and beyond[0].startswith("any"), fan
