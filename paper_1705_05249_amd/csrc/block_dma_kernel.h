@@ -405,7 +405,9 @@ template <int MODE> hipError_t launch_block_dma(const BlockArgs &args, int sums,
 {
     if (tile == DMA_256) {
         if (sums == SUMS_POW2) return launch_block_dma_as<MODE, SUMS_POW2, 256, 256, 2, 4, 2>(args, stream);
-        if (sums == SUMS_SQUARE) return launch_block_dma_as<MODE, SUMS_SQUARE, 256, 256, 2, 4, 2>(args, stream);
+        if constexpr (MODE != BLOCK_SUM) {                 // (sums over experts' rows have row blocks on both sides)
+            if (sums == SUMS_SQUARE) return launch_block_dma_as<MODE, SUMS_SQUARE, 256, 256, 2, 4, 2>(args, stream);
+        }
         if (sums == SUMS_ANY) return launch_block_dma_as<MODE, SUMS_ANY, 256, 256, 4, 2, 2>(args, stream);
         if (sums == SUMS_FP32_POW2) return launch_block_dma_as<MODE, SUMS_FP32_POW2, 256, 128, 4, 2, 2>(args, stream);
         return launch_block_dma_as<MODE, SUMS_FP32, 256, 128, 4, 2, 2>(args, stream);
