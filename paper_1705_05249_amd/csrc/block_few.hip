@@ -34,12 +34,13 @@ template <typename T> __device__ inline void write_one(T *c, float v, float alph
 template <int MODE, int FEW_WAVES, int TF, typename FRAGMENT> __global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(const FewArgs args)
 {
     constexpr int FEW = 16 * TF, PITCH = 20;                              // floats between the rows of a sum in LDS
+    static_assert(MODE == BLOCK_DENSE || TF == 1, "tiles of 16 rows of an expert");
     __shared__ __attribute__((aligned(16))) float sums[FEW_WAVES][FEW * PITCH];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     int64_t first = static_cast<int64_t>(blockIdx.y) * FEW, end = args.rows_few, group = 0;
     if constexpr (MODE == BLOCK_ROWS) {
         RowTile tile;
-        if (!find_row_tile<TF == 1 ? 4 : 5>(args.groups, blockIdx.y, &tile)) return;
+        if (!find_row_tile<4>(args.groups, blockIdx.y, &tile)) return;
         first = __builtin_amdgcn_readfirstlane(static_cast<int>(tile.first));
         end = __builtin_amdgcn_readfirstlane(static_cast<int>(tile.end));
         group = __builtin_amdgcn_readfirstlane(tile.group);
@@ -152,13 +153,15 @@ template <int MODE> hipError_t launch_as(const FewArgs &args, int fragments, boo
     const dim3 grid(static_cast<uint32_t>(ceil_div(args.rows_many, 16)), static_cast<uint32_t>(tiles));
     auto launch = [&](auto waves) {
         constexpr int W = decltype(waves)::value;
-        if (fragments == 1) {
-            if (fp32) block_few_kernel<MODE, W, 1, Fp16Fragment><<<grid, W * 64, 0, stream>>>(args);
-            else block_few_kernel<MODE, W, 1, Fp8Fragment><<<grid, W * 64, 0, stream>>>(args);
-        } else {
-            if (fp32) block_few_kernel<MODE, W, 2, Fp16Fragment><<<grid, W * 64, 0, stream>>>(args);
-            else block_few_kernel<MODE, W, 2, Fp8Fragment><<<grid, W * 64, 0, stream>>>(args);
+        auto with = [&](auto count) {
+            constexpr int TF = decltype(count)::value;
+            if (fp32) block_few_kernel<MODE, W, TF, Fp16Fragment><<<grid, W * 64, 0, stream>>>(args);
+            else block_few_kernel<MODE, W, TF, Fp8Fragment><<<grid, W * 64, 0, stream>>>(args);
+        };
+        if constexpr (MODE == BLOCK_DENSE) {                              // (experts' rows: 16 at a time)
+            if (fragments == 2) return with(std::integral_constant<int, 2>{});
         }
+        with(std::integral_constant<int, 1>{});
     };
     // Two work-groups and more for each compute unit: four wavefronts each, of which more fit (32 experts with 2 rows, 2048 x 4096: 68 -> 55 us, 4.9 TB/s); fewer:
     // eight, for the length of the sum (1 x 8192 x 4096: 7.5 us, with two wavefronts 10.6)

@@ -49,6 +49,12 @@ def test_kernels_of_aligned_operands():
     assert built("dma") == dma()
 
 
+def test_kernels_of_any_address_and_of_few_rows():
+    assert built("any") == {(mode, sums, size) for mode in (DENSE, ROWS, SUM) for sums in (POW2, ANY, FP32) for size in (64, 128)}
+    # (rows of experts: 16 for an expert at most, two fragments only for up to 32 rows of one product)
+    assert built("few") == {(mode, waves, fragments, fp8) for mode in (DENSE, ROWS) for waves in (4, 8) for fragments in ((1, 2) if mode == DENSE else (1,)) for fp8 in (False, True)}
+
+
 def test_every_hand_waited_kernel_is_looked_over(tmp_path, monkeypatch):
     monkeypatch.setattr(T, "KERNEL", re.compile(r"^[0-9a-f]+ <(_ZN2mg16block_dma_kernelI\w+EvNS_9BlockArgsE)>:$"))
     seen, wrong = set(), {}
