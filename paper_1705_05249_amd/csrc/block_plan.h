@@ -59,11 +59,18 @@ inline Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums
 {
     Plan best{};
     best.slices = 1;
-    const int64_t few = mode == BLOCK_ROWS ? ceil_div(m, groups) : m < n ? m : n;       // rows of A (for an expert), or of the smaller operand
     // The kernel for few rows reads them once for every 16 of the others.  8192 x 8192: 4 rows 15.9 us, 16 rows 22, 32 rows 33, 64 x 64 tiles 19; 4096 x 4096: 32 rows 10,
-    // 64 x 64 tiles 11.5.  32 experts, 2048 x 4096 each: 16 rows 79 us, 17 rows 92,
-    // 64 x 64 tiles 84.
-    if (mode != BLOCK_SUM && (few <= 8 || (mode == BLOCK_ROWS && few <= 16) || (mode == BLOCK_DENSE && few <= 32 && (m < n ? n : m) * k <= int64_t(1) << 25))) {
+    // 64 x 64 tiles 11.5.
+    // Experts' rows: only their mean is known, and an expert with more of them has its weights read again for every 16.  So it is taken where the 64 x 64 tiles of all experts
+    // that can have rows do not outnumber the 256 compute units (twice for FP32 sums, in which tiles take longer), up to a mean of 8 rows, 16 where they reach half of the
+    // units.  2048 x 4096, FP8 pipes, even counts and then a router's, this kernel / tiles: 4 experts, 1 row 8.8 / 11.7 and 8.5 / 11.5 us, 8 rows 10.2 / 11.5 and 10.3 / 11.6;
+    // 16 experts, 1 row 29 / 22 and 17 / 13, 8 rows 36 / 22 and 37 / 21; 32 experts, 3 rows 56 / 40 and 34 / 30; 64 experts, 16 rows 155 / 107 and 191 / 105, and with
+    // all rows in eight of them 148 / 21.  FP32 sums: 8 experts, 1 row 15.5 / 18.8 and 11.8 / 17.6; 32 experts, 1 row 53 / 47 and 28 / 25.
+    const int64_t asked = m < groups ? m : groups;                                      // experts that can have rows
+    const int64_t few = mode == BLOCK_ROWS ? ceil_div(m, groups) : m < n ? m : n;       // rows of A (for an expert), or of the smaller operand
+    const int64_t small_tiles = asked * ceil_div(n, 64);
+    if (mode == BLOCK_ROWS ? small_tiles <= (sums_fp32(sums) ? 512 : 256) && few <= (small_tiles <= 128 ? 16 : 8)
+                           : mode == BLOCK_DENSE && (few <= 8 || (few <= 32 && (m < n ? n : m) * k <= int64_t(1) << 25))) {
         best.tile = TILE_FEW;
         best.few_b = mode == BLOCK_DENSE && n < m;
         best.fragments = few <= 16 ? 1 : 2;
@@ -80,9 +87,9 @@ inline Plan plan(int mode, int groups, int64_t m, int64_t n, int64_t k, int sums
         p.tile = tile;
         p.tiles_m = static_cast<int>(ceil_div(m, bm) + (mode == BLOCK_ROWS ? groups : 0));
         p.tiles_n = static_cast<int>(ceil_div(n, bn));
-        // (every expert's last tile is half full, if it has rows at all)
+        // (every expert's last tile is half full, if it has rows at all; where their mean is small each has one tile)
         const int64_t ends = groups < m / bm ? groups / 2 : 0;
-        const int64_t tiles = (mode == BLOCK_ROWS ? ceil_div(m, bm) + ends : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * batch;
+        const int64_t tiles = (mode == BLOCK_ROWS ? (few <= 16 ? asked : ceil_div(m, bm) + ends) : static_cast<int64_t>(p.tiles_m)) * p.tiles_n * batch;
         const Cost c = cost_of(tile, sums);
         for (int s = 1; s <= 16; s *= 2) {
             if (s > 1 && (blocks / s < 4 || one * s > static_cast<double>(workspace) || tiles * s > 512)) break;

@@ -40,3 +40,13 @@ def test_indexed_rows_are_as_far_apart_as_tokens():
     for fan, m in rows.items():
         fits, beyond = choices([dict(many, m=m - fan, fan=fan), dict(many, m=m + fan + 1, fan=fan)])
         assert fits[0] == "256" and beyond[0].startswith("any"), fan
+
+
+@pytest.mark.parametrize("groups,n,mean,kernel", (
+    (4, 2048, 1, "few"), (4, 2048, 12, "few"), (8, 2048, 8, "few"), (8, 2048, 12, "64"), (16, 2048, 2, "64"), (32, 2048, 1, "64"), (64, 2048, 16, "64"), (128, 1024, 1, "64"),
+    (256, 512, 4, "64"), (16, 1000, 8, "few"), (4, 7168, 2, "64"), (64, 200, 2, "few"), (32, 2048, 17, "64")))
+def test_few_rows_of_experts(groups, n, mean, kernel):
+    """tiles where all experts together have enough of them for the chip: they read an expert's weights once, however many of the rows it has"""
+    for lda in (4096, 4099):
+        got = choices([dict(mode="rows", m=mean * groups, n=n, k=4096, groups=groups, pow2=True, b_square=True, lda=lda, ldb=lda)])[0][0]
+        assert got == (kernel if lda == 4096 or kernel == "few" else "any 64"), got

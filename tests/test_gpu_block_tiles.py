@@ -29,7 +29,7 @@ ROWS = [("rows", kernel, sums, *size) for kernel, table in {
     "64": {sums: [(301, 300, 393, False), (140, 140, 4000, True)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
     "any 128": {sums: [(520, 3100, 393, False)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
     "any 64": {sums: [(301, 300, 393, False)] for sums in ("pow2", "square", "fp32", "fp32 pow2")},
-    "few": {sums: [(70, 300, 393, False), (13, 2100, 1024, False), (80, 9000, 272, False)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
+    "few": {sums: [(70, 300, 393, False), (13, 2100, 1024, False), (40, 3000, 272, False)] for sums in ("pow2", "any", "square", "fp32", "fp32 pow2")},
 }.items() for sums, sizes in table.items() for size in sizes]
 
 SUM = [("sum", kernel, sums, *size) for kernel, table in {
