@@ -22,15 +22,15 @@ def _blocks(size):
     return -(-size // X.BLOCK)
 
 
-def _checked(name, tensor, shape, device, types=tuple(TYPES)):
+def _checked(name, tensor, shape, device, types=TYPES):
     """the tensor, dense: the library's calls take addresses and believe what they are told of the memory behind them"""
+    if tensor.dtype in types and tensor.shape == shape and tensor.device == device and tensor.is_cuda:
+        return tensor.contiguous()
     if tensor.dtype not in types:
         raise TypeError(f"{name}: {tensor.dtype} is none of {', '.join(str(t) for t in types)}")
-    if tuple(tensor.shape) != tuple(shape):
+    if tensor.shape != shape:
         raise ValueError(f"{name}: shape {tuple(tensor.shape)}, expected {tuple(shape)}")
-    if not tensor.is_cuda or (device is not None and tensor.device != device):
-        raise ValueError(f"{name}: on {tensor.device}, expected on {device or 'the GPU'}")
-    return tensor.contiguous()
+    raise ValueError(f"{name}: on {tensor.device}, expected on {device if device.type == 'cuda' else 'the GPU'}")
 
 
 def dense_ids(ids, experts):
@@ -62,10 +62,10 @@ NONE = (None, 0, None, 0)
 class Routes:
     """tokens sorted by expert"""
 
-    def __init__(self, ids, experts):
+    def __init__(self, ids, experts, device=None):
         if ids.dim() != 2:
             raise ValueError(f"ids: shape {tuple(ids.shape)}, expected tokens x fan")
-        ids = _checked("ids", ids, ids.shape, None, INDEX_TYPES)
+        ids = _checked("ids", ids, ids.shape, device or ids.device, INDEX_TYPES)
         self.tokens, self.fan = ids.shape
         self.experts, self.rows = experts, ids.numel()
         new = lambda n: torch.empty(n, dtype=torch.int32, device=ids.device)  # noqa: E731
@@ -81,7 +81,7 @@ class Experts:
     def __init__(self, weights):
         if weights.dim() != 3:
             raise ValueError(f"weights: shape {tuple(weights.shape)}, expected experts x n x k")
-        self.weights = _checked("weights", weights, weights.shape, None)
+        self.weights = _checked("weights", weights, weights.shape, weights.device)
         self.experts, self.n, self.k = weights.shape
         self.w = Quantized(self.n, self.k, _blocks(self.n), self.experts, weights.device)
         self.turned = Quantized(self.k, self.n, _blocks(self.k), self.experts, weights.device)
@@ -109,7 +109,9 @@ class Experts:
 
     def forward(self, routes, x, of_tokens):
         """x: a row for each token (of_tokens: the products fetch every route's) or for each routed row"""
-        x = self._rows("x", x, routes, of_tokens, self.k)
+        return self._forward(routes, self._rows("x", x, routes, of_tokens, self.k), of_tokens)
+
+    def _forward(self, routes, x, of_tokens):
         a = Quantized(x.shape[0], self.k, device=x.device)
         X.mg_block_quantize(TYPES[x.dtype], X.MG_BLOCK_ROW, x.shape[0], self.k, x, self.k, *a.at(), *NONE)
         return self._product(routes, a, routes.source if of_tokens else None, routes.fan if of_tokens else 1, self.w, self.n, self.k, x.dtype)
@@ -145,15 +147,12 @@ class ExpertLayer:
         """x: tokens x width; ids: tokens x fan (negative: dropped); gates: tokens x fan (numbers of 16 bits are widened to the FP32 that the kernels read);
         keep: hold on to what `backward` reads, in place of an earlier call's (without: to nothing, as for tokens that are served)"""
         device = self.up.w.q.device
-        if ids.dim() != 2:
-            raise ValueError(f"ids: shape {tuple(ids.shape)}, expected tokens x fan")
-        ids = _checked("ids", ids, ids.shape, device, INDEX_TYPES)
-        x = _checked("x", x, (ids.shape[0], self.width), device)
+        x = _checked("x", x, (*ids.shape[:1], self.width), device)
         gates = _checked("gates", gates, ids.shape, device).float()
-        routes = Routes(ids, self.up.experts)
-        h = self.up.forward(routes, x, of_tokens=True)
+        routes = Routes(ids, self.up.experts, device)
+        h = self.up._forward(routes, x, of_tokens=True)
         a = torch.relu(h).square_()
-        rows = self.down.forward(routes, a, of_tokens=False)
+        rows = self.down._forward(routes, a, of_tokens=False)
         y = torch.empty_like(x)
         X.mg_expert_combine(TYPES[x.dtype], routes.tokens, routes.fan, self.width, rows, self.width, routes.position, gates, y, self.width)
         self.kept = (routes, x, gates, h, a, rows) if keep else None
