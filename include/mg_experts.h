@@ -13,8 +13,10 @@
  * stands for its 8-bit value times its block's scale.  Scales are row-major with a leading dimension of their own:
  * (row blocks) rows x ceil(cols/128), (square blocks) ceil(rows/128) x ceil(cols/128).
  *
- * MG_ERR_DIM also covers what the kernels' 32-bit counts and a launch cannot hold: extents from 2^31 - 1024 on, 2^35 elements of a
- * matrix that is quantised, 2^34 of a product's C, and of the rows that are routed 2^31 pieces of four elements and 2^24 tokens.
+ * MG_ERR_DIM also covers what the kernels' 32-bit counts and a launch cannot hold: extents from 2^31 - 1024 on, 2^21 blocks of 128 x 128
+ * of a matrix that is quantised and more than 2^20 of a product's C (2^35 and 2^34 elements; blocks that are not full count, so that a
+ * single row counts as 128, and one more row of blocks for every expert), and of the rows that are routed more than 2^31 pieces of four
+ * elements and 2^24 tokens.
  *
  * A kernel may read an aligned 16-byte piece of memory whole when at least one of its bytes belongs to an operand.
  */
@@ -38,12 +40,16 @@ enum { MG_BF16 = 2 };                                             /* beside MG_F
 typedef enum { MG_BLOCK_ROW = 151, MG_BLOCK_SQUARE = 152 } mg_block;
 /* MG_SCALES_POW2: the caller states that every scale of both operands is a normal power of two (as mg_block_quantize
  * makes them): the scales then go into the matrix instructions as exponents, or into the exponents of the elements, whose
- * values have to be finite FP32 numbers then (below 2^-126 they may count as zero).  Other scales given under it count as
- * the power of two below them. */
+ * values have to be finite FP32 numbers then (below 2^-126 they may count as zero).  Other scales given under it may count as
+ * the power of two below them, or as they are: that depends on the kernel. */
 typedef enum { MG_SCALES_ANY = 161, MG_SCALES_POW2 = 162 } mg_scales;
-/* May be added (|) to either: sums as of FP32 products whatever the type of C.  Without it C in FP32 gets those, and C in 16 bits is
- * summed on the FP8 matrix pipes, twice as fast: they add eight neighbouring products at a time on a grid of 2^-13 of the largest of the
- * eight (all else in FP32), an error of about 1.5e-5 of the result for normal data, below the rounding of either 16-bit type. */
+/* May be added (|) to either: sums as of FP32 products whatever the type of C, as C in FP32 gets them anyway.
+ * Without it C in 16 bits is not summed in FP32 throughout, but on the FP8 matrix pipes, twice as fast: they add eight neighbouring products
+ * at a time on a grid of 2^-13 of the largest of the eight, towards zero (these sums, and all else, then in FP32).  That is an error of about
+ * 1.5e-5 of the result for normal data, 5e-5 with outliers, whatever the length of the sum; where all terms have one sign it is a bias (measured,
+ * of the sum of magnitudes: -2.5e-6 for |normal| data, -9.5e-6 for squares of a rectifier's output, -6e-5 where the terms spread over
+ * exp(2 normal)).  The whole error of C, its rounding included: bfloat16 1.6612e-3 of the norm where FP32 sums have 1.6604e-3, FP16 2.13e-4 where
+ * they have 2.08e-4.  The largest loss there can be is 2^-10 of the sum of magnitudes. */
 enum { MG_SUMS_FP32 = 1 << 16 };
 #define MG_MOST_GROUPS 1024
 #define MG_MOST_FAN 64
@@ -85,7 +91,8 @@ int64_t mg_grouped_columns(int64_t rows, int groups);
 /* ---- product of two 8-bit matrices -----------------------------------------------------------------------------------
  *     C = alpha * A * B^T + beta * C        C(i,j): sum over blocks b of sa(i,b) * sb(j,b) * sum over l in b of A(i,l) * B(j,l)
  * A m x k, B n x k, both with the summed index contiguous in memory; C m x n of c_type (MG_F32, MG_F16, MG_BF16), stored as
- * `layout` says (column-major: element (i, j) at C[i + j*ldc]).  FP32 accumulation (see MG_SUMS_FP32), one rounding.  alpha, beta: host scalars;
+ * `layout` says (column-major: element (i, j) at C[i + j*ldc]).  How it is summed follows from c_type and MG_SUMS_FP32 (above): FP32 throughout for
+ * C in FP32 or with the flag, on the FP8 pipes' grid otherwise; one rounding to c_type.  alpha, beta: host scalars;
  * beta == 0: C is not read; alpha == 0 or k == 0: A and B are not read.
  * workspace (256-byte aligned, may be NULL): with mg_block_gemm_workspace_bytes() few outputs with long sums run as slices
  * that a second launch adds; with less, in fewer slices: same result up to summation order.

@@ -9,8 +9,10 @@
 // LDS rows of 128 bytes as in lds_layout.h for 16-row fragments: a lane's 32 bytes of a fragment are the chunks l / 16 and l / 16 + 4 of row
 // l % 16, in either operand, so that both see the same order of the sum.
 //
-// Bound by the matrix pipes at the part's power limit, and by what a tile does before and behind its loop (4 us until the first K-tile of 256 x 256 is there, 8 for C):
-// 4096^3 into bfloat16 66 us (2.1 PFLOP/s; 70 with scales of any value), 8192 x 4096 x 4096 149, with FP32 sums 4096 x 4096 x 8192 285 to 306 (0.9 to 1.0 PFLOP/s).
+// Bound by the matrix pipes at the part's power limit, and by what a tile does before and behind its loop (4 us until the first K-tile of 256 x 256 is there, 8 for C).
+// Calls in a row, activations times weights: 4096^3 into bfloat16 67 to 74 us (2.0 PFLOP/s; 72 to 75 with scales of any value and square blocks), 8192 x 4096 x 4096 121
+// (2.3; 139, and 160 with row blocks on both sides), with FP32 sums 4096 x 4096 x 8192 240 to 248 (1.1 PFLOP/s).
+// Under a profiler's kernel trace the same kernels take a fifth longer (148 and 296).
 // A work-group that stays for its next tile and loads it while C leaves has no registers for it with 256 x 256, and gains nothing with 256 x 128.
 //
 // Ends: rows behind an operand's last one are its last one again (their products are not stored).  Pieces of 16 bytes behind the end of the sum are not

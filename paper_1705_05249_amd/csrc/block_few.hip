@@ -3,7 +3,7 @@
 // A work-group takes 16 rows of the weights and up to 16 TF of the few; its four or eight wavefronts share the sum, each every fourth or eighth block
 // of 128, straight from memory into registers (a fragment of 16 x 128 bytes is 32 bytes for each lane, four lanes to a row's 128): two blocks on
 // their way at a time.  The wavefronts' sums meet in LDS and are added in their order.  Bound by the weights' bytes
-// (1 x 4096 x 4096: 5.0 us, 3.4 TB/s and the launch; 1 x 16384 x 4096: 14.7, 4.6 TB/s), with more of the few also by what the caches pass on: the few
+// (1 x 4096 x 4096: 5.4 us, 3.1 TB/s and the launch; 1 x 16384 x 4096: 14.2, 4.7 TB/s), with more of the few also by what the caches pass on: the few
 // are read once for every 16 rows of the weights (32 x 8192 x 8192 took 33 us, 64 x 64 tiles take 18).
 #include "internal.h"
 #include "block_gemm_kernel.h"
@@ -163,8 +163,9 @@ template <int MODE> hipError_t launch_as(const FewArgs &args, int fragments, boo
         }
         with(std::integral_constant<int, 1>{});
     };
-    // Two work-groups and more for each compute unit: four wavefronts each, of which more fit (32 experts with 2 rows, 2048 x 4096: 68 -> 55 us, 4.9 TB/s); fewer:
-    // eight, for the length of the sum (1 x 8192 x 4096: 7.5 us, with two wavefronts 10.6)
+    // Two work-groups and more for each compute unit: four wavefronts each, of which more fit (1024 work-groups: 8 experts with 2 rows, 2048 x 4096, 22.8 -> 15.7 us;
+    // 1 x 16384 x 4096 20.8 -> 14.2; 512 work-groups: within 3 % of each other, 1 x 8192 x 4096 7.4 either way); fewer: eight, for the length of the sum
+    // (1 x 8192 x 4096 with two wavefronts 10.6)
     const int64_t busy = grid.x * (MODE == BLOCK_ROWS ? (args.rows_few < args.groups.count ? args.rows_few : args.groups.count) : tiles);
     if (busy >= 512) launch(std::integral_constant<int, 4>{});
     else launch(std::integral_constant<int, 8>{});

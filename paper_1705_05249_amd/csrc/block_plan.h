@@ -30,8 +30,11 @@ inline int64_t output_rows(int mode, int groups, int64_t m) { return mode == BLO
 
 // What a kernel takes, in us, measured with random operands.  A compute unit that has one of its tiles: `alone` for a block of 128 of the sum while half of the
 // chip is idle, `full` while all of it is busy; with n of them n * `each` (two work-groups of 128 x 128 share a compute unit, two to four of 64 x 64).
-// Around the sum: `start`, and `more` for every round of tiles (C leaves).  Over 2048 x 2048 .. 8192 x 4096 with sums of 512 to 8192 within a tenth of the measured,
-// but for `each` of 128 x 128: 0.515 with uniform bits, where the clock stays up; with activations the smaller tiles slow down more than the large ones.
+// Around the sum: `start`, and `more` for every round of tiles (C leaves).  Over 2048 x 2048 .. 8192 x 4096 with sums of 512 to 8192 within a tenth of what calls in a row take
+// (8192 x 4096 x 4096 with activations: estimated 116 us, measured 121; with FP32 sums 4096 x 4096 x 8192 223 and 238 to 248; 16 experts' rows, 16384 x 4096 x 2048, 161 and 175),
+// with two exceptions: `each` of 128 x 128 is 0.515 with uniform bits, where the clock stays up (with activations the smaller tiles slow down more than the large ones), and
+// many tiles with short sums that write FP32, the experts' weights' gradient, take longer than their estimate (16384 rows of 16 experts, 4096 x 2048: 304 us, measured
+// 338 with equal counts and 421 with a router's).
 struct Cost {
     double alone, full, each, start, more;
 };

@@ -3,7 +3,7 @@
 // Sorting is a stable counting sort, the same result whatever the timing: a wavefront walks its slots 64 at a time; which lanes before a lane
 // have the same expert follows from a ballot for every bit of the expert's number, and only one wavefront counts in a row of the table.
 // Everything else is bound by memory (rows) or by the launch (few tokens): 131072 slots of 64 experts sorted in 13 us, their rows of 2048 bfloat16 gathered in 150
-// (604 MB, 4.0 TB/s); 8192 tokens of four choices and 4096 columns combined in 73 (336 MB, 4.6 TB/s), the gradient 139 (604 MB, 4.3 TB/s); 16 tokens 3.
+// (604 MB, 4.0 TB/s), with weights in 170; 8192 tokens of four choices and 4096 columns combined in 73 (336 MB, 4.6 TB/s), the gradient 139 (604 MB, 4.3 TB/s); 16 tokens 3.
 #include "internal.h"
 #include "experts.h"
 
@@ -188,7 +188,9 @@ inline RowShape row_shape(int64_t pieces)
     return {log, static_cast<uint32_t>(ceil_div(pieces, int64_t(1) << log))};
 }
 
-// 16 bytes that nobody reads soon
+// 16 bytes past the caches.  What that does depends on the size and on who reads them next; rows of 2048 bfloat16, past the caches / as usual, alone and with a pass
+// behind it that quantises them: 8192 rows 8.9 / 10.4 us and 21.8 / 20.3; 32768 rows 38 / 39 and 71 / 70; 131072 rows (more than the last-level cache holds) 151 / 150 and
+// 290 / 318; 2048 rows and fewer the same.
 template <typename T, int N> __device__ inline void store_streaming(T *p, const Piece<T, N> &x)
 {
     typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
