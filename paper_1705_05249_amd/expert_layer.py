@@ -7,6 +7,8 @@
 trains a layer to answer as another one does and prints the loss and the time of a step.  PyTorch holds the memory, computes the elementwise
 activation and makes the update; everything else runs in the library's kernels.  All buffers are allocated by the layer, on
 its weights' device, none by the library; the calls go to torch's current stream, so that device has to be the current one.
+Rows of 16 bits are products on the FP8 matrix pipes, whose sums have fewer bits than FP32 (MG_SUMS_FP32 in include/mg_experts.h says how many);
+rows in FP32 and the weights' gradients are summed in FP32.
 """
 import sys
 
