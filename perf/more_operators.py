@@ -1,0 +1,423 @@
+"""The dense layers of a language model's training step: what programs ask of `paper_1705_05249_amd.layers`.
+
+Gated feed-forward blocks (forward, backward, single tokens), the softmax cross entropy over a large vocabulary with the last projection in it and its
+gradient, and clipping by the global norm of all gradients.  `listed()` names twelve calls, from a token through a block to a training step of the
+loss; `draw(rng)` gives more of the same ranges.  `prepare` makes what a program holds before the call, `run` is the call: with `own` through the
+library's entry points, otherwise the same formulas in elementary torch operations, in FP32 with one rounding at the end.  `exact` computes the
+definitions once more in 64 bits.
+
+    block      Y = (act(X Wg^T) * (X Wu^T)) Wd^T                        X tokens x width, Wg and Wu hidden x width, Wd width x hidden
+    loss       loss[t] = log(sum over v of exp(z[t, v])) - z[t, target[t]],  z = X W^T;   0 where the target is no row of W (an ignored token)
+               its gradient for the weights w[t] of the tokens' losses:  dz[t, v] = w[t] (exp(z[t, v] - lse[t]) - (v == target[t]))
+    clipping   norm = sqrt(sum of all squares);  every gradient times max_norm / norm where norm > max_norm
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+SIZE = {"f32": 4, "f16": 2, "bf16": 2}
+MOST_STEP_FLOPS = 18.0 * 8192 * 2048 * 8192      # of a drawn training step of a block: the largest listed one
+MOST_FORWARD_FLOPS = 6.0 * 4096 * 4096 * 8192    # of a drawn forward pass
+MOST_WEIGHTS = 4096 * 16384                      # elements of one of a drawn block's matrices
+MOST_LOSS_FLOPS = 8.0 * 8192 * 2048 * 65536      # of a drawn step of the loss
+MOST_FP32_FLOPS = 4.0e11                         # of a drawn case in FP32
+MOST_GRADIENTS = 400_000_000                     # elements of all gradients of a drawn model
+PLAIN_ROWS = 2048                                # tokens whose logits the plain form holds at a time
+
+
+def listed():
+    return [
+        # a token that is being generated
+        dict(name="block_1x4096x8192", routine="block", tokens=1, width=4096, hidden=8192, act="silu", dtype="bf16", odd_ld=False),
+        # a few tokens, one of each of several conversations
+        dict(name="block_24x2048x4096", routine="block", tokens=24, width=2048, hidden=4096, act="gelu_tanh", dtype="f16", odd_ld=False),
+        # a long prompt
+        dict(name="block_4096x4096x8192", routine="block", tokens=4096, width=4096, hidden=8192, act="silu", dtype="bf16", odd_ld=False),
+        # sizes that are no multiple of any tile, activations that are a part of a larger matrix: rows start at any element
+        dict(name="block_step_333x1001x1999", routine="block_step", tokens=333, width=1001, hidden=1999, act="gelu", dtype="f16", odd_ld=True),
+        # a training step: output, gradients of the input and of the three matrices
+        dict(name="block_step_8192x2048x8192", routine="block_step", tokens=8192, width=2048, hidden=8192, act="silu", dtype="bf16", odd_ld=False),
+        # the same in FP32, a small batch
+        dict(name="block_step_512x1024x2048", routine="block_step", tokens=512, width=1024, hidden=2048, act="relu2", dtype="f32", odd_ld=False),
+        # the score of a few tokens' continuations
+        dict(name="loss_16x2048x32768", routine="loss", tokens=16, width=2048, vocab=32768, weights="mean", ignored=0.0, dtype="bf16", odd_ld=False),
+        # a training step of the last layer and its loss, padding tokens ignored
+        dict(name="loss_step_8192x2048x65536", routine="loss_step", tokens=8192, width=2048, vocab=65536, weights="mean", ignored=0.05, dtype="bf16", odd_ld=False),
+        # an odd vocabulary, every token with a weight of its own
+        dict(name="loss_step_1000x1001x9999", routine="loss_step", tokens=1000, width=1001, vocab=9999, weights="each", ignored=0.3, dtype="f16", odd_ld=True),
+        # the same in FP32, a small batch
+        dict(name="loss_step_256x512x16384", routine="loss_step", tokens=256, width=512, vocab=16384, weights="mean", ignored=0.1, dtype="f32", odd_ld=False),
+        # the gradients of a small model, which are within the limit
+        dict(name="clip_16_small", routine="clip", tensors=16, total=200_000, clipped=False, dtype="f32"),
+        # the gradients of a model of 300 tensors
+        dict(name="clip_300_large", routine="clip", tensors=300, total=400_000_000, clipped=True, dtype="bf16"),
+    ]
+
+
+# ------------------------------------------------------------------------------------------------ drawn cases
+
+def _size(rng, lo, hi, unit=64):
+    """spread over the logarithm of lo .. hi; half are multiples of `unit`"""
+    v = int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    if v >= unit and rng.random() < 0.5:
+        v = v // unit * unit
+    return max(lo, min(hi, v))
+
+
+def draw(rng):
+    routine = rng.choice(("block", "block", "block_step", "block_step", "loss", "loss_step", "loss_step", "clip"))
+    dtype = rng.choice(("bf16", "bf16", "f16", "f32"))
+    while True:
+        case = _drawn(rng, routine, dtype)
+        if case is not None:
+            return case
+
+
+def _drawn(rng, routine, dtype):
+    if routine == "clip":
+        return dict(routine=routine, tensors=_size(rng, 1, 400, 8), total=_size(rng, 2000, MOST_GRADIENTS), clipped=rng.random() < 0.6, dtype=dtype)
+    odd_ld = rng.random() < 0.25
+    if routine in ("block", "block_step"):
+        tokens = _size(rng, 1, 64, 8) if routine == "block" and rng.random() < 0.5 else _size(rng, 32, 8192)
+        width, hidden = _size(rng, 64, 8192), _size(rng, 64, 16384)
+        flops = (6.0 if routine == "block" else 18.0) * tokens * width * hidden
+        if width * hidden > MOST_WEIGHTS or flops > (MOST_FORWARD_FLOPS if routine == "block" else MOST_STEP_FLOPS) or (dtype == "f32" and flops > MOST_FP32_FLOPS):
+            return None
+        return dict(routine=routine, tokens=tokens, width=width, hidden=hidden, act=rng.choice(("silu", "gelu", "gelu_tanh", "relu2")), dtype=dtype, odd_ld=odd_ld)
+    tokens, width, vocab = _size(rng, 1, 8192), _size(rng, 64, 4096), _size(rng, 100, 131072)
+    flops = (2.0 if routine == "loss" else 8.0) * tokens * width * vocab
+    if width * vocab > 2048 * 131072 or tokens * vocab > 8192 * 65536 or flops > MOST_LOSS_FLOPS or (dtype == "f32" and flops > MOST_FP32_FLOPS):
+        return None
+    return dict(routine=routine, tokens=tokens, width=width, vocab=vocab, weights=rng.choice(("mean", "each")), ignored=rng.choice((0.0, 0.1, 0.5)),
+                dtype=dtype, odd_ld=odd_ld)
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+
+class _Draw:
+    """activations with a few large channels, weights of variance 1 / k"""
+
+    def __init__(self, seed):
+        self.gen = torch.Generator(device="cuda").manual_seed(seed)
+
+    def normal(self, *shape, sigma=1.0):
+        return torch.empty(shape, device="cuda").normal_(0.0, sigma, generator=self.gen)
+
+    def rows(self, rows, cols, dtype, odd, sigma=1.0, spread=0.5):
+        """rows x cols; `odd`: a part of a matrix whose rows are an odd number of elements"""
+        x = (self.normal(rows, cols, sigma=sigma) * torch.exp(self.normal(cols, sigma=spread))).to(TYPES[dtype])
+        if not odd:
+            return x
+        held = torch.zeros(rows, cols + 7 - cols % 2, dtype=x.dtype, device="cuda")
+        held[:, :cols] = x
+        return held[:, :cols]
+
+    def weights(self, rows, cols, dtype, sigma=1.0):
+        return self.normal(rows, cols, sigma=sigma * cols ** -0.5).to(TYPES[dtype])
+
+
+def _sizes(case):
+    """how many elements the tensors of a model have: some matrices, more vectors; one element at least"""
+    count, rng = case["tensors"], random.Random(case["tensors"] * 1000003 + case["total"])
+    share = [math.exp(rng.gauss(0.0, 2.0)) for _ in range(count)]
+    return [max(1, int(case["total"] * x / sum(share))) for x in share]
+
+
+def prepare(case, seed):
+    s = dict(case)
+    d, routine, dtype = _Draw(seed), case["routine"], case["dtype"]
+    new = lambda *shape, kind=None: torch.empty(shape, dtype=kind or TYPES[dtype], device="cuda")  # noqa: E731
+    if routine in ("block", "block_step"):
+        tokens, width, hidden = case["tokens"], case["width"], case["hidden"]
+        s["x"] = d.rows(tokens, width, dtype, case["odd_ld"])
+        s["wg"], s["wu"], s["wd"] = (d.weights(*size, dtype) for size in ((hidden, width), (hidden, width), (width, hidden)))
+        s["y"] = new(tokens, width)
+        if routine == "block_step":
+            s["dy"] = d.rows(tokens, width, dtype, case["odd_ld"])
+            s["dx"], s["dwg"], s["dwu"], s["dwd"] = new(tokens, width), new(hidden, width), new(hidden, width), new(width, hidden)
+    elif routine in ("loss", "loss_step"):
+        tokens, width, vocab = case["tokens"], case["width"], case["vocab"]
+        s["x"], s["w"] = d.rows(tokens, width, dtype, case["odd_ld"]), d.weights(vocab, width, dtype, sigma=1.5)
+        s["targets"] = torch.randint(0, vocab, (tokens,), device="cuda", generator=d.gen)
+        s["targets"][torch.rand(tokens, device="cuda", generator=d.gen) < case["ignored"]] = -100
+        s["loss"], s["lse"] = new(tokens, kind=torch.float32), new(tokens, kind=torch.float32)
+        if routine == "loss_step":
+            # a mean over the tokens that count (in FP16 with a loss scale), or weights of the tokens' sources
+            counted = (s["targets"] >= 0).sum().clamp(min=1)
+            mean = torch.full((tokens,), 1024.0 if dtype == "f16" else 1.0, device="cuda") / counted
+            s["token_weights"] = mean if case["weights"] == "mean" else torch.empty(tokens, device="cuda").uniform_(0.5, 1.5, generator=d.gen)
+            s["dx"], s["dw"] = new(tokens, width), new(vocab, width)
+    else:
+        # matrices in the model's type and vectors in FP32, one behind the other in two buffers
+        sizes = _sizes(case)
+        kinds = ["f32" if n < 20000 else dtype for n in sizes]
+        totals = {kind: sum(n for n, k in zip(sizes, kinds) if k == kind) for kind in ("f32", dtype)}
+        s["grads"] = {kind: d.normal(n).to(TYPES[kind]) for kind, n in totals.items()}
+        s["results"] = {kind: torch.empty_like(g) for kind, g in s["grads"].items()}
+        s["max_norm"] = (0.1 if case["clipped"] else 10.0) * math.sqrt(sum(sizes))
+        s["norm"] = new(1, kind=torch.float32)
+        _plan_clip(s, sizes, kinds)
+    _workspaces(s)
+    return s
+
+
+def _plan_clip(s, sizes, kinds):
+    """where every tensor and its result is, as a program lists them once for buffers that stay"""
+    at, sources, results, codes = {kind: 0 for kind in s["grads"]}, [], [], []
+    for n, kind in zip(sizes, kinds):
+        offset = at[kind] * SIZE[kind]
+        sources.append(s["grads"][kind].data_ptr() + offset)
+        results.append(s["results"][kind].data_ptr() + offset)
+        codes.append({"f32": 0, "f16": 1, "bf16": 2}[kind])
+        at[kind] += n
+    s["codes"], s["sizes"] = torch.tensor(codes, dtype=torch.int32), torch.tensor(sizes)
+    s["sources"], s["targets_of"] = torch.tensor(sources), torch.tensor(results)
+
+
+def _workspaces(s):
+    """what the library asks a program to keep for a call, as bytes of scratch memory, and what a block's forward pass keeps for its backward pass"""
+    s["ws"] = s["kept"] = None
+    try:
+        from paper_1705_05249_amd import layers as L
+    except ImportError:                      # the plain forms need none
+        return
+    code, routine = {"f32": 0, "f16": 1, "bf16": 2}[s["dtype"]], s["routine"]
+    kept = 0
+    if routine in ("block", "block_step"):
+        size = (code, s["tokens"], s["width"], s["hidden"])
+        need = L.mg_gated_forward_workspace_bytes(*size)
+        if routine == "block_step":
+            kept = L.mg_gated_kept_bytes(*size)
+            need = max(need, L.mg_gated_backward_workspace_bytes(*size))
+    elif routine in ("loss", "loss_step"):
+        size = (code, s["tokens"], s["width"], s["vocab"])
+        need = L.mg_vocab_loss_workspace_bytes(*size)
+        if routine == "loss_step":
+            need = max(need, L.mg_vocab_loss_grad_workspace_bytes(*size))
+    else:
+        need = L.mg_gradient_workspace_bytes(s["tensors"], s["sizes"])
+    s["ws"] = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    s["kept"] = torch.empty(kept, dtype=torch.uint8, device="cuda") if kept else None
+
+
+# ------------------------------------------------------------------------------------------------ the calls
+
+def run(s):
+    return (_OWN if own else _PLAIN)[s["routine"]](s)
+
+
+def _codes(s):
+    from paper_1705_05249_amd import layers as L
+    return L, {"f32": L.MG_F32, "f16": L.MG_F16, "bf16": L.MG_BF16}[s["dtype"]]
+
+
+def _act_code(L, s):
+    return {"silu": L.MG_ACT_SILU, "gelu": L.MG_ACT_GELU, "gelu_tanh": L.MG_ACT_GELU_TANH, "relu2": L.MG_ACT_RELU2}[s["act"]]
+
+
+def _own_block(s):
+    L, code = _codes(s)
+    tokens, width, hidden = s["tokens"], s["width"], s["hidden"]
+    L.mg_gated_forward(code, _act_code(L, s), tokens, width, hidden, s["x"], s["x"].stride(0), s["wg"], width, s["wu"], width, s["wd"], hidden,
+                       s["y"], width, s["kept"], s["ws"])
+    return s["y"]
+
+
+def _own_block_step(s):
+    L, code = _codes(s)
+    tokens, width, hidden = s["tokens"], s["width"], s["hidden"]
+    _own_block(s)
+    L.mg_gated_backward(code, _act_code(L, s), tokens, width, hidden, s["x"], s["x"].stride(0), s["wg"], width, s["wu"], width, s["wd"], hidden,
+                        s["dy"], s["dy"].stride(0), s["kept"], s["dx"], width, s["dwg"], width, s["dwu"], width, s["dwd"], hidden, s["ws"])
+    return s["y"], s["dx"], s["dwg"], s["dwu"], s["dwd"]
+
+
+def _own_loss(s):
+    L, code = _codes(s)
+    width = s["width"]
+    L.mg_vocab_loss(code, s["tokens"], width, s["vocab"], s["x"], s["x"].stride(0), s["w"], width, s["targets"], s["loss"], s["lse"], s["ws"])
+    return s["loss"], s["lse"]
+
+
+def _own_loss_step(s):
+    L, code = _codes(s)
+    width = s["width"]
+    _own_loss(s)
+    L.mg_vocab_loss_grad(code, s["tokens"], width, s["vocab"], s["x"], s["x"].stride(0), s["w"], width, s["targets"], s["lse"], s["token_weights"],
+                         s["dx"], width, s["dw"], width, s["ws"])
+    return s["loss"], s["lse"], s["dx"], s["dw"]
+
+
+def _own_clip(s):
+    from paper_1705_05249_amd import layers as L
+    L.mg_gradient_clip(s["tensors"], s["codes"], s["sources"], s["targets_of"], s["sizes"], s["max_norm"], s["norm"], s["ws"])
+    return s["norm"], list(s["results"].values())
+
+
+_OWN = {"block": _own_block, "block_step": _own_block_step, "loss": _own_loss, "loss_step": _own_loss_step, "clip": _own_clip}
+
+
+# ------------------------------------------------------------------------------------------------ the same, plainly
+
+def _act(g, act):
+    """(act(g), its derivative)"""
+    if act == "silu":
+        p = 1 / (1 + torch.exp(-g))
+        return g * p, p * (1 + g * (1 - p))
+    if act == "relu2":
+        positive = torch.where(g > 0, g, 0.0)
+        return positive * positive, 2 * positive
+    if act == "gelu":
+        below = 0.5 * (1 + torch.erf(g * 0.5 ** 0.5))
+        return g * below, below + g * torch.exp(-0.5 * g * g) * (2 * math.pi) ** -0.5
+    a = (2 / math.pi) ** 0.5
+    t = torch.tanh(a * (g + 0.044715 * g * g * g))
+    return 0.5 * g * (1 + t), 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * a * (1 + 3 * 0.044715 * g * g)
+
+
+def _plain_block(s):
+    x = s["x"].float()
+    h = _act(x @ s["wg"].float().T, s["act"])[0] * (x @ s["wu"].float().T)
+    return (h @ s["wd"].float().T).to(TYPES[s["dtype"]])
+
+
+def _plain_block_step(s):
+    kind = TYPES[s["dtype"]]
+    x, dy, wg, wu, wd = (s[name].float() for name in ("x", "dy", "wg", "wu", "wd"))
+    u = x @ wu.T
+    a, da = _act(x @ wg.T, s["act"])
+    h = a * u
+    y = h @ wd.T
+    dh = dy @ wd
+    dwd = dy.T @ h
+    dg, du = dh * u * da, dh * a
+    return [v.to(kind) for v in (y, dg @ wg + du @ wu, dg.T @ x, du.T @ x, dwd)]
+
+
+def _scores(x, w, targets):
+    """(z, exp(z - largest), lse, which rows count, their targets) of some tokens"""
+    z = x @ w.T
+    largest = z.amax(1, keepdim=True)
+    p = torch.exp(z - largest)
+    counts = (targets >= 0) & (targets < w.shape[0])
+    return z, p, largest[:, 0] + torch.log(p.sum(1)), counts, torch.where(counts, targets, 0)
+
+
+def _plain_loss(s):
+    x, w = s["x"].float(), s["w"].float()
+    loss, lse = [], []
+    for some, targets in zip(x.split(PLAIN_ROWS), s["targets"].split(PLAIN_ROWS)):
+        z, _, total, counts, at = _scores(some, w, targets)
+        loss.append(torch.where(counts, total - z.gather(1, at[:, None])[:, 0], 0.0))
+        lse.append(total)
+    return torch.cat(loss), torch.cat(lse)
+
+
+def _plain_loss_step(s):
+    x, w, kind = s["x"].float(), s["w"].float(), TYPES[s["dtype"]]
+    loss, lse, dx, dw = [], [], [], torch.zeros_like(w)
+    for some, targets, weight in zip(x.split(PLAIN_ROWS), s["targets"].split(PLAIN_ROWS), s["token_weights"].split(PLAIN_ROWS)):
+        z, p, total, counts, at = _scores(some, w, targets)
+        loss.append(torch.where(counts, total - z.gather(1, at[:, None])[:, 0], 0.0))
+        lse.append(total)
+        p /= p.sum(1, keepdim=True)
+        p.scatter_add_(1, at[:, None], -torch.ones_like(p[:, :1]))
+        p *= torch.where(counts, weight, 0.0)[:, None]
+        dx.append(p @ w)
+        dw += p.T @ some
+    return torch.cat(loss), torch.cat(lse), torch.cat(dx).to(kind), dw.to(kind)
+
+
+def _plain_clip(s):
+    norm = sum(g.double().square().sum() for g in s["grads"].values()).sqrt()
+    factor = torch.where(norm > s["max_norm"], s["max_norm"] / norm, 1.0).float()
+    return norm.float()[None], [(g.float() * factor).to(g.dtype) for g in s["grads"].values()]
+
+
+_PLAIN = {"block": _plain_block, "block_step": _plain_block_step, "loss": _plain_loss, "loss_step": _plain_loss_step, "clip": _plain_clip}
+
+
+# ------------------------------------------------------------------------------------------------ 64 bits
+
+def _exact_act(g, act):
+    """act(g) with its derivative by torch's own differentiation"""
+    g = g.detach().requires_grad_()
+    if act == "silu":
+        a = g * torch.sigmoid(g)
+    elif act == "relu2":
+        a = g.clamp(min=0) ** 2
+    elif act == "gelu":
+        a = g * torch.special.ndtr(g)
+    else:
+        a = g * torch.sigmoid(2 * math.sqrt(2 / math.pi) * (g + 0.044715 * g ** 3))       # (1 + tanh(b)) / 2 = sigmoid(2 b)
+    slope, = torch.autograd.grad(a.sum(), g)
+    return a.detach(), slope
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    routine = case["routine"]
+    if routine in ("block", "block_step"):
+        x, wg, wu, wd = (s[name].double() for name in ("x", "wg", "wu", "wd"))
+        gate, up = torch.mm(x, wg.t()), torch.mm(x, wu.t())
+        a, slope = _exact_act(gate, case["act"])
+        y = torch.mm(a * up, wd.t())
+        if routine == "block":
+            return y
+        dy = s["dy"].double()
+        dh = torch.mm(dy, wd)
+        both = torch.cat((dh * up * slope, dh * a), 1)                                      # gradients of both projections, side by side
+        dw = torch.mm(both.t(), x)
+        return y, torch.mm(both, torch.cat((wg, wu))), dw[:case["hidden"]], dw[case["hidden"]:], torch.mm(dy.t(), a * up)
+    if routine in ("loss", "loss_step"):
+        w = s["w"].double()
+        loss, lse = [], []
+        dx, dw = [], torch.zeros_like(w)
+        for lo in range(0, case["tokens"], 512):
+            x, target = s["x"][lo:lo + 512].double(), s["targets"][lo:lo + 512]
+            z = torch.mm(x, w.t())
+            total = torch.logsumexp(z, 1)
+            here = torch.zeros_like(z)
+            rows = (target >= 0).nonzero()[:, 0]
+            here[rows, target[rows]] = 1.0
+            loss.append((here * (total[:, None] - z)).sum(1))
+            lse.append(total)
+            if routine == "loss_step":
+                weight = s["token_weights"][lo:lo + 512].double() * here.sum(1)
+                dz = weight[:, None] * (torch.exp(z - total[:, None]) - here)
+                dx.append(torch.mm(dz, w))
+                dw += torch.mm(dz.t(), x)
+        loss, lse = torch.cat(loss), torch.cat(lse)
+        return (loss, lse) if routine == "loss" else (loss, lse, torch.cat(dx), dw)
+    squares = 0.0
+    for g in s["grads"].values():
+        for part in g.split(1 << 24):
+            squares += float(torch.dot(part.double(), part.double()))
+    norm = math.sqrt(squares)
+    factor = min(1.0, s["max_norm"] / norm)
+    return torch.tensor([norm], dtype=torch.float64), [g.double() * factor for g in s["grads"].values()]
+
+
+# ------------------------------------------------------------------------------------------------ what a call cannot do without
+
+def work(case):
+    """each input read once, each output written once; what a block's forward pass keeps for its backward pass is not counted.  The gradient of the
+    loss makes the logits a second time, as nobody keeps them."""
+    routine, z = case["routine"], SIZE[case["dtype"]]
+    if routine in ("block", "block_step"):
+        t, w, h = case["tokens"], case["width"], case["hidden"]
+        if routine == "block":
+            return {"bytes": z * (2 * t * w + 3 * w * h), "flops": 6.0 * t * w * h}
+        return {"bytes": z * (4 * t * w + 6 * w * h), "flops": 18.0 * t * w * h}
+    if routine in ("loss", "loss_step"):
+        t, w, v = case["tokens"], case["width"], case["vocab"]
+        if routine == "loss":
+            return {"bytes": z * (t * w + v * w) + 16 * t, "flops": 2.0 * t * w * v}
+        return {"bytes": z * 2 * (t * w + v * w) + 20 * t, "flops": 8.0 * t * w * v}
+    sizes = _sizes(case)
+    count = sum(n * (4 if n < 20000 else z) for n in sizes)
+    return {"bytes": 2.0 * count, "flops": 3.0 * sum(sizes)}
