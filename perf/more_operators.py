@@ -199,7 +199,7 @@ def _workspaces(s):
         if routine == "loss_step":
             need = max(need, L.mg_vocab_loss_grad_workspace_bytes(*size))
     else:
-        need = L.mg_gradient_workspace_bytes(s["tensors"], s["sizes"])
+        need = L.mg_gradient_workspace_bytes(s["tensors"])
     s["ws"] = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
     s["kept"] = torch.empty(kept, dtype=torch.uint8, device="cuda") if kept else None
 
