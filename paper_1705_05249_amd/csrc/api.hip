@@ -9,7 +9,7 @@
 
 #include <string>
 
-#include "../../include/mg_experts.h"
+#include "../../include/mg_layers.h"
 #include "internal.h"
 #include "select.h"
 #include "lds_layout.h"
@@ -1334,6 +1334,9 @@ const char *mg_status_string(mg_status status)
         case MG_ERR_BLOCK: return "unknown block form or kind of scales";
         case MG_ERR_GROUPS: return "number of groups, experts or choices out of range";
         case MG_ERR_SCALES: return "leading dimension of scales too small";
+        case MG_ERR_ACTIVATION: return "unknown activation";
+        case MG_ERR_KEPT: return "what a forward pass keeps is missing, misaligned or too small";
+        case MG_ERR_LIMIT: return "max_norm negative or not a number";
         default: return "unknown status";
     }
 }

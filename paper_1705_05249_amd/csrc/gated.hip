@@ -1,0 +1,237 @@
+// Gated feed-forward blocks: which products a call is made of, and the elementwise kernels between the products of FP32.
+//
+// Forward, 16 bits: one product with gate and up weights as one matrix, 16 rows of each in turn, so that a lane holds g and u of the same element and
+// H leaves the kernel (6 tokens width hidden operations in two launches); then Y.  Backward: dH never exists in memory, dG and dU leave its product;
+// dX is one sum over 2 hidden, dG's half and dU's; the gradients of gate and up weights are one product with twice the rows.
+// FP32: products as mg_sgemm makes them, with G and U in memory.
+#include "linear_end.h"
+#include "internal.h"
+
+namespace mg {
+namespace {
+
+constexpr int64_t F = sizeof(float);
+
+// H = act(G) * U
+template <int ACT> __global__ __launch_bounds__(256) void gated_act_kernel(const float *G, const float *U, float *H, int64_t count)
+{
+    const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (at >= count) return;
+    float g[4], u[4], h[4], slope;
+    load_piece<float, 4>(G + at, static_cast<int>(count - at < 4 ? count - at : 4), g);
+    load_piece<float, 4>(U + at, static_cast<int>(count - at < 4 ? count - at : 4), u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        activation_of<ACT, true>(g[e], h[e], slope);
+        h[e] *= u[e];
+    }
+    store_piece<float, 4>(H + at, static_cast<int>(count - at < 4 ? count - at : 4), h);
+}
+
+// dG (where dH is) and dU
+template <int ACT> __global__ __launch_bounds__(256) void gated_grad_kernel(const float *G, const float *U, float *dH, float *dU, int64_t count)
+{
+    const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (at >= count) return;
+    const int valid = static_cast<int>(count - at < 4 ? count - at : 4);
+    float g[4], u[4], d[4], other[4];
+    load_piece<float, 4>(G + at, valid, g);
+    load_piece<float, 4>(U + at, valid, u);
+    load_piece<float, 4>(dH + at, valid, d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float h, slope;
+        activation_of<ACT, true>(g[e], h, slope);
+        other[e] = d[e] * h;
+        d[e] = d[e] * u[e] * slope;
+    }
+    store_piece<float, 4>(dH + at, valid, d);
+    store_piece<float, 4>(dU + at, valid, other);
+}
+
+uint32_t pieces(int64_t count) { return static_cast<uint32_t>(ceil_div(count, 1024)); }
+
+// calls fn with the activation as a type
+template <typename Fn> hipError_t with_activation(int act, Fn &&fn)
+{
+    if (act == MG_ACT_SILU) fn(std::integral_constant<int, MG_ACT_SILU>{});
+    else if (act == MG_ACT_GELU) fn(std::integral_constant<int, MG_ACT_GELU>{});
+    else if (act == MG_ACT_GELU_TANH) fn(std::integral_constant<int, MG_ACT_GELU_TANH>{});
+    else fn(std::integral_constant<int, MG_ACT_RELU2>{});
+    return hipGetLastError();
+}
+
+// what a forward pass of FP32 keeps, tokens x hidden each
+struct KeptF32 {
+    float *G, *U, *H;
+    KeptF32(void *at, int64_t tokens, int64_t hidden) : G(static_cast<float *>(at)), U(G + tokens * hidden), H(U + tokens * hidden) {}
+};
+
+size_t sgemm_workspace(int ta, int tb, int64_t m, int64_t n, int64_t k, int64_t lda, int64_t ldb, int64_t ldc)
+{
+    return mg_gemm_workspace_bytes(MG_F32, MG_ROW_MAJOR, ta, tb, m, n, k, lda, ldb, ldc);
+}
+
+// room for the products of dense matrices; with other leading dimensions a product may want more, and runs in what there is
+size_t sgemm_room(int64_t tokens, int64_t width, int64_t hidden, bool backward)
+{
+    size_t most = 0;
+    auto add = [&](size_t v) { most = v > most ? v : most; };
+    add(sgemm_workspace(MG_NO_TRANS, MG_TRANS, tokens, hidden, width, width, width, hidden));
+    add(sgemm_workspace(MG_NO_TRANS, MG_TRANS, tokens, width, hidden, hidden, hidden, width));
+    if (backward) {
+        add(sgemm_workspace(MG_NO_TRANS, MG_NO_TRANS, tokens, hidden, width, width, hidden, hidden));
+        add(sgemm_workspace(MG_NO_TRANS, MG_NO_TRANS, tokens, width, hidden, hidden, width, width));
+        add(sgemm_workspace(MG_TRANS, MG_NO_TRANS, hidden, width, tokens, hidden, width, width));
+        add(sgemm_workspace(MG_TRANS, MG_NO_TRANS, width, hidden, tokens, width, hidden, hidden));
+    }
+    return most;
+}
+
+mg_status forward_f32(const GatedProblem &p)
+{
+    Arena ws = p.workspace;
+    const KeptF32 kept(p.kept != nullptr ? p.kept : ws.take(3 * p.tokens * p.hidden * F), p.tokens, p.hidden);
+    const size_t room = ws.left();
+    void *const scratch = ws.take(0);
+    const float *X = static_cast<const float *>(p.X);
+    auto product = [&](const float *A, int64_t lda, const void *B, int64_t ldb, int64_t n, int64_t k, float *C, int64_t ldc) {
+        return mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_TRANS, p.tokens, n, k, 1.f, A, lda, static_cast<const float *>(B), ldb, 0.f, C, ldc, scratch, room, p.stream);
+    };
+    if (const mg_status st = product(X, p.ldx, p.WG, p.ldwg, p.hidden, p.width, kept.G, p.hidden)) return st;
+    if (const mg_status st = product(X, p.ldx, p.WU, p.ldwu, p.hidden, p.width, kept.U, p.hidden)) return st;
+    const int64_t count = p.tokens * p.hidden;
+    const hipError_t e = with_activation(p.activation, [&](auto act) {
+        gated_act_kernel<decltype(act)::value><<<pieces(count), 256, 0, p.stream>>>(kept.G, kept.U, kept.H, count);
+    });
+    if (e != hipSuccess) return MG_ERR_LAUNCH;
+    return product(kept.H, p.hidden, p.WD, p.ldwd, p.width, p.hidden, static_cast<float *>(p.Y), p.ldy);
+}
+
+mg_status backward_f32(const GatedProblem &p)
+{
+    Arena ws = p.workspace;
+    const int64_t count = p.tokens * p.hidden;
+    const KeptF32 kept(p.kept, p.tokens, p.hidden);
+    float *const dG = static_cast<float *>(ws.take(2 * count * F)), *const dU = dG + count;
+    const size_t room = ws.left();
+    void *const scratch = ws.take(0);
+    auto product = [&](int ta, int64_t m, int64_t n, int64_t k, const void *A, int64_t lda, const void *B, int64_t ldb, float beta, void *C, int64_t ldc) {
+        return mg_sgemm(MG_ROW_MAJOR, ta, MG_NO_TRANS, m, n, k, 1.f, static_cast<const float *>(A), lda, static_cast<const float *>(B), ldb, beta, static_cast<float *>(C),
+                        ldc, scratch, room, p.stream);
+    };
+    mg_status st = MG_OK;
+    if (p.dX != nullptr || p.dWG != nullptr || p.dWU != nullptr) {
+        st = product(MG_NO_TRANS, p.tokens, p.hidden, p.width, p.dY, p.lddy, p.WD, p.ldwd, 0.f, dG, p.hidden);
+        if (st != MG_OK) return st;
+        const hipError_t e = with_activation(p.activation, [&](auto act) {
+            gated_grad_kernel<decltype(act)::value><<<pieces(count), 256, 0, p.stream>>>(kept.G, kept.U, dG, dU, count);
+        });
+        if (e != hipSuccess) return MG_ERR_LAUNCH;
+    }
+    if (p.dX != nullptr) {
+        st = product(MG_NO_TRANS, p.tokens, p.width, p.hidden, dG, p.hidden, p.WG, p.ldwg, 0.f, p.dX, p.lddx);
+        if (st == MG_OK) st = product(MG_NO_TRANS, p.tokens, p.width, p.hidden, dU, p.hidden, p.WU, p.ldwu, 1.f, p.dX, p.lddx);
+    }
+    if (st == MG_OK && p.dWG != nullptr) st = product(MG_TRANS, p.hidden, p.width, p.tokens, dG, p.hidden, p.X, p.ldx, 0.f, p.dWG, p.lddwg);
+    if (st == MG_OK && p.dWU != nullptr) st = product(MG_TRANS, p.hidden, p.width, p.tokens, dU, p.hidden, p.X, p.ldx, 0.f, p.dWU, p.lddwu);
+    if (st == MG_OK && p.dWD != nullptr) st = product(MG_TRANS, p.width, p.hidden, p.tokens, p.dY, p.lddy, kept.H, p.hidden, 0.f, p.dWD, p.lddwd);
+    return st;
+}
+
+// G and U in front of H
+size_t kept_scores(int64_t tokens, int64_t hidden) { return static_cast<size_t>(kept_at((tokens + 15) / 16 * 16, 0, hidden)) * F; }
+size_t held_rows(int64_t tokens, int64_t cols) { return static_cast<size_t>(tokens * padded(cols)) * 2; }
+
+mg_status launched(hipError_t e) { return e == hipSuccess ? MG_OK : MG_ERR_LAUNCH; }
+
+mg_status product(const GatedProblem &p, int form, int end, LinearArgs args)
+{
+    args.k_per_slice = static_cast<int>(padded(args.k));
+    return launched(launch_linear_any(p.dtype, form, end, args, 1, p.stream));
+}
+
+mg_status forward_16(const GatedProblem &p)
+{
+    Arena ws = p.workspace;
+    float *const kept = static_cast<float *>(p.kept);
+    void *const H = kept != nullptr ? static_cast<char *>(p.kept) + kept_scores(p.tokens, p.hidden) : ws.take(held_rows(p.tokens, p.hidden));
+    LinearArgs a{};
+    a.P = p.X; a.ldp = p.ldx;
+    a.Q0 = p.WG; a.ldq0 = p.ldwg; a.Q1 = p.WU; a.ldq1 = p.ldwu;
+    a.rows = static_cast<int>(p.tokens); a.cols = static_cast<int>(kept_blocks(p.hidden) * 32); a.k = static_cast<int>(p.width);
+    a.hidden = static_cast<int>(p.hidden); a.activation = p.activation; a.kept = kept;
+    a.C0 = H; a.ldc0 = padded(p.hidden);
+    if (const mg_status st = product(p, FORM_KK, END_GATED, a)) return st;
+    LinearArgs b{};
+    b.P = H; b.ldp = padded(p.hidden); b.Q0 = p.WD; b.ldq0 = p.ldwd;
+    b.rows = a.rows; b.cols = static_cast<int>(p.width); b.k = static_cast<int>(p.hidden);
+    b.C0 = p.Y; b.ldc0 = p.ldy;
+    return product(p, FORM_KK, END_STORE, b);
+}
+
+mg_status backward_16(const GatedProblem &p)
+{
+    Arena ws = p.workspace;
+    const int64_t half = padded(p.hidden);
+    void *const d = ws.take(held_rows(p.tokens, p.hidden) * 2);         // dG and dU, side by side
+    float *const kept = static_cast<float *>(p.kept);
+    const int tokens = static_cast<int>(p.tokens), width = static_cast<int>(p.width), hidden = static_cast<int>(p.hidden);
+    if (p.dX != nullptr || p.dWG != nullptr || p.dWU != nullptr) {
+        LinearArgs a{};
+        a.P = p.dY; a.ldp = p.lddy; a.Q0 = p.WD; a.ldq0 = p.ldwd;
+        a.rows = tokens; a.cols = hidden; a.k = width;
+        a.hidden = hidden; a.activation = p.activation; a.kept = kept;
+        a.C0 = d; a.ldc0 = 2 * half;
+        if (const mg_status st = product(p, FORM_KN, END_GATED_GRAD, a)) return st;
+    }
+    if (p.dX != nullptr) {
+        LinearArgs a{};
+        a.P = d; a.ldp = 2 * half; a.Q0 = p.WG; a.ldq0 = p.ldwg; a.Q1 = p.WU; a.ldq1 = p.ldwu;
+        a.segment = static_cast<int>(half); a.lines = hidden;
+        a.rows = tokens; a.cols = width; a.k = static_cast<int>(2 * half);
+        a.C0 = p.dX; a.ldc0 = p.lddx;
+        if (const mg_status st = product(p, FORM_KN, END_STORE, a)) return st;
+    }
+    if (p.dWG != nullptr || p.dWU != nullptr) {
+        LinearArgs a{};
+        a.P = d; a.ldp = 2 * half; a.Q0 = p.X; a.ldq0 = p.ldx;
+        a.rows = static_cast<int>(2 * half); a.cols = width; a.k = tokens;
+        a.second = static_cast<int>(half); a.rows0 = hidden;
+        a.C0 = p.dWG; a.ldc0 = p.lddwg; a.C1 = p.dWU; a.ldc1 = p.lddwu;
+        if (const mg_status st = product(p, FORM_NN, END_STORE, a)) return st;
+    }
+    if (p.dWD != nullptr) {
+        LinearArgs a{};
+        a.P = p.dY; a.ldp = p.lddy;
+        a.Q0 = static_cast<char *>(p.kept) + kept_scores(p.tokens, p.hidden); a.ldq0 = half;
+        a.rows = width; a.cols = hidden; a.k = tokens;
+        a.C0 = p.dWD; a.ldc0 = p.lddwd;
+        if (const mg_status st = product(p, FORM_NN, END_STORE, a)) return st;
+    }
+    return MG_OK;
+}
+
+}  // namespace
+
+size_t gated_kept(int dtype, int64_t tokens, int64_t hidden)
+{
+    return dtype == MG_F32 ? static_cast<size_t>(3 * tokens * hidden) * F : kept_scores(tokens, hidden) + held_rows(tokens, hidden);
+}
+
+size_t gated_workspace(int dtype, int64_t tokens, int64_t width, int64_t hidden, bool backward)
+{
+    Arena ws{nullptr, 0, 0};
+    if (dtype == MG_F32) {
+        ws.take(static_cast<size_t>((backward ? 2 : 3) * tokens * hidden) * F);
+        ws.take(sgemm_room(tokens, width, hidden, backward));
+    } else {
+        ws.take(held_rows(tokens, hidden) * (backward ? 2 : 1));
+    }
+    return ws.used;
+}
+
+mg_status gated_forward(const GatedProblem &p) { return p.dtype == MG_F32 ? forward_f32(p) : forward_16(p); }
+mg_status gated_backward(const GatedProblem &p) { return p.dtype == MG_F32 ? backward_f32(p) : backward_16(p); }
+
+}  // namespace mg

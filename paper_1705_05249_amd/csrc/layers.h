@@ -1,0 +1,169 @@
+// What the kernels of mg_layers.h share: the products of 16-bit matrices and what becomes of their results.
+//
+// Every product of the block and of the loss is C(r, c) = sum over l of P(r, l) Q(c, l), C row-major.  P and Q each lie along the sum
+// (element (r, l) at P[r*ld + l]) or across it (at P[l*ld + r]); the results stay in registers until they have become what the operator stores.
+#pragma once
+
+#include "experts.h"
+#include "../../include/mg_layers.h"
+
+namespace mg {
+
+constexpr int64_t LAYER_PIECE = 64;               // columns of the matrices that the library lays out itself are padded to this, with zeros
+
+__host__ __device__ inline int64_t padded(int64_t v) { return (v + LAYER_PIECE - 1) / LAYER_PIECE * LAYER_PIECE; }
+
+// What becomes of the sums
+enum LinearEnd {
+    END_STORE = 0,          // C in the operands' type, its rows in one matrix or two, or slices of FP32 sums
+    END_GATED = 1,          // Q is gate and up weights, 16 rows of each in turn: H = act(G) * U, and G and U for the backward pass
+    END_GATED_GRAD = 2,     // the sums are dH: dG and dU beside each other
+    END_SCORES = 3,         // the sums are logits: largest one and sum of exponentials of a tile's columns, the target's logit
+    END_SCORES_GRAD = 4     // the sums are logits: dz
+};
+
+// Operands.  Matrix 1 is the second half of Q: END_GATED (up weights), or with `segment` the lines from l = segment on.
+struct LinearArgs {
+    const void *P, *Q0, *Q1;
+    int64_t ldp, ldq0, ldq1;
+    int rows, cols;             // of C; END_GATED: cols is 32 * ceil(hidden / 16), the interleaved columns
+    int k;                      // length of the sum
+    int segment;                // 0, or where in the sum Q1 takes over (a multiple of 64; P has zeros between `lines` and it)
+    int lines;                  // with `segment`: lines that Q0 and Q1 have
+    int hidden;                 // END_GATED, END_GATED_GRAD
+    int tiles_r, tiles_c;
+    int k_per_slice;            // a multiple of 64; slice z of the sum starts at z * k_per_slice
+    // results
+    void *C0, *C1;              // END_STORE: rows from `second` on are rows 0.. of C1 (`second` rows: of C0, `rows0` of which exist, as many of C1)
+    int64_t ldc0, ldc1;
+    int second, rows0;
+    float *partial;             // END_STORE: instead of C, FP32 sums: slice z at partial + z * partial_stride, rows x partial_ld
+    int64_t partial_ld, partial_stride;
+    const float *scale;         // END_STORE: device scalar that every result is multiplied with; null: 1
+    int activation;
+    float *kept;                // END_GATED (null: nothing is kept), END_GATED_GRAD: see kept_at
+    // END_SCORES, END_SCORES_GRAD: columns are the vocabulary's from `first` on
+    int64_t first, vocab;
+    const int64_t *targets;
+    float2 *scores;             // [tile of columns][row]: (largest, sum of exp(z - largest))
+    float *target_score;        // [row]
+    const float *lse;
+    const float *weights;       // null: 1
+    const float *weight_scale;  // device scalar beside the weights; null: 1
+};
+
+// G and U as a block keeps them: 16 x 16 blocks in the order in which a matrix instruction leaves them (lane l: row l % 16, columns 4 (l / 16) .. + 3),
+// G's block in front of U's.  A wavefront moves a block as 1 KB on end.
+__host__ __device__ inline int64_t kept_blocks(int64_t hidden) { return (hidden + 15) / 16; }
+__host__ __device__ inline int64_t kept_at(int64_t row, int64_t col, int64_t hidden) { return ((row / 16) * kept_blocks(hidden) + col / 16) * 512; }
+
+// Which of P and Q lie along the sum
+enum LinearForm { FORM_KK = 0, FORM_KN = 1, FORM_NN = 2 };       // both; P along, Q across; both across
+
+// dtype MG_F16 or MG_BF16.  The launches of operands at any address (any) and of operands whose rows start on 16 bytes (dma).
+hipError_t launch_linear_any(int dtype, int form, int end, LinearArgs args, int slices, hipStream_t stream);
+
+// adds the slices of END_STORE and writes C in dtype
+hipError_t launch_linear_sum(int dtype, const LinearArgs &args, int slices, hipStream_t stream);
+
+// Memory of a workspace, handed out on 256 bytes; without a base it only counts
+struct Arena {
+    char *base;
+    size_t bytes, used;
+    void *take(size_t wanted)
+    {
+        void *const at = base == nullptr ? nullptr : base + used;
+        used += (wanted + 255) / 256 * 256;
+        return at;
+    }
+    size_t left() const { return used < bytes ? bytes - used : 0; }
+};
+
+struct GatedProblem {
+    int dtype, activation;
+    int64_t tokens, width, hidden;
+    const void *X, *WG, *WU, *WD, *dY;
+    int64_t ldx, ldwg, ldwu, ldwd, lddy;
+    void *Y, *dX, *dWG, *dWU, *dWD;
+    int64_t ldy, lddx, lddwg, lddwu, lddwd;
+    void *kept;
+    Arena workspace;
+    hipStream_t stream;
+};
+size_t gated_kept(int dtype, int64_t tokens, int64_t hidden);
+size_t gated_workspace(int dtype, int64_t tokens, int64_t width, int64_t hidden, bool backward);
+mg_status gated_forward(const GatedProblem &p);          // sizes above zero
+mg_status gated_backward(const GatedProblem &p);
+
+struct LossProblem {
+    int dtype;
+    int64_t tokens, width, vocab;
+    const void *X, *W;
+    int64_t ldx, ldw;
+    const int64_t *targets;
+    float *loss;
+    float *lse;                       // read by the gradient
+    const float *weights;
+    void *dX, *dW;
+    int64_t lddx, lddw;
+    Arena workspace;
+    hipStream_t stream;
+};
+size_t loss_workspace(int dtype, int64_t tokens, int64_t width, int64_t vocab, bool gradient);
+mg_status vocab_loss(const LossProblem &p);              // vocab may be zero, tokens not
+mg_status vocab_loss_grad(const LossProblem &p);         // sizes above zero but for width
+
+struct ClipProblem {
+    int64_t count;
+    const int32_t *types;
+    const void *const *sources;
+    void *const *results;             // null: in place
+    const int64_t *sizes;
+    bool scales;
+    float max_norm;
+    float *norm;
+    void *workspace;
+    hipStream_t stream;
+};
+size_t clip_workspace(int64_t count);
+hipError_t launch_clip(const ClipProblem &p);
+
+// zeros in a matrix (rows x cols elements of `size` bytes)
+hipError_t launch_zero_rows(void *X, int64_t rows, int64_t cols, int64_t ld, int size, hipStream_t stream);
+
+#if defined(__HIPCC__)
+
+// e^x by the hardware's exponential of base two: relative error below 2^-23 (1 + |x|)
+__device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+template <bool PRECISE> __device__ inline float exp_of(float x)
+{
+    if constexpr (PRECISE) return expf(x);
+    else return exp_fast(x);
+}
+
+// act(g) and its derivative (PRECISE: for results in FP32).  GELU_TANH: (1 + tanh(b)) / 2 = 1 / (1 + exp(-2 b)), which loses nothing for small results; GELU: the normal
+// distribution function as erfc(-g / sqrt 2) / 2, for the same reason.
+template <int ACT, bool PRECISE = false> __device__ inline void activation_of(float g, float &a, float &slope)
+{
+    if constexpr (ACT == MG_ACT_SILU) {
+        const float p = 1.f / (1.f + exp_of<PRECISE>(-g));
+        a = g * p;
+        slope = p * (1.f + g * (1.f - p));
+    } else if constexpr (ACT == MG_ACT_RELU2) {
+        const float v = g > 0.f ? g : g != g ? g : 0.f;
+        a = v * v;
+        slope = 2.f * v;
+    } else if constexpr (ACT == MG_ACT_GELU) {
+        const float below = 0.5f * erfcf(-0.70710678118654752440f * g);
+        a = g * below;
+        slope = below + g * exp_of<PRECISE>(-0.5f * g * g) * 0.39894228040143267794f;
+    } else {
+        constexpr float A = 1.59576912160573071176f, B = 0.044715f;       // 2 sqrt(2 / pi)
+        const float g2 = fminf(g * g, 1e30f), p = 1.f / (1.f + exp_of<PRECISE>(-A * g * (1.f + B * g2)));
+        a = g * p;
+        slope = p + g * p * (1.f - p) * A * (1.f + 3.f * B * g2);
+    }
+}
+#endif
+
+}  // namespace mg

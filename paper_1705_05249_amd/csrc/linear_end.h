@@ -1,0 +1,252 @@
+// What becomes of the sums of a product (LinearEnd): from the registers of a wavefront's tile to memory.
+//
+// acc[j][i] is the 16 x 16 block of rows row0 + 16 j and columns col0 + 16 i: lane l holds row l % 16, columns 4 (l / 16) .. + 3.  Stored from there, a
+// wavefront's store would write 16 pieces of 8 bytes in each of 16 rows; the rows of a block go through LDS instead, so that a store instruction
+// writes 16 bytes a lane and rows of the wavefront's tile whole (4096 x 4096 in bfloat16 behind one K-tile of an 8-bit product: 29 us from registers, 11.6 so).
+#pragma once
+
+#include "layers.h"
+
+namespace mg {
+
+#if defined(__HIPCC__)
+
+typedef float end_floatx4 __attribute__((ext_vector_type(4)));
+
+// LDS bytes of a wavefront's region: 16 rows of its columns in FP32 or two matrices of 16 bits, 16 bytes apart from each other's banks
+template <int WTM> constexpr int end_region() { return 16 * (WTM * 4 + 16); }
+
+// waits for nothing in hardware (a wavefront's LDS operations run in order); keeps the compiler from moving reads across other lanes' writes
+__device__ inline void end_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <typename T> struct __attribute__((packed, aligned(8))) Four {
+    T v[4];
+};
+
+// COLS columns of 16 rows, U elements, in the wavefront's region -> base(row) + col; rows below `rows`, columns below `cols`
+template <typename U, int COLS, typename Row> __device__ inline void end_drain(const char *region, int row_bytes, int row, int col, int rows, int cols, int lane, Row &&at)
+{
+    constexpr int PER = 16 / static_cast<int>(sizeof(U)), CH = COLS / PER;
+    static_assert(COLS % PER == 0, "whole pieces");
+#pragma unroll
+    for (int pass = 0; pass < (16 * CH + 63) / 64; ++pass) {
+        const int id = lane + 64 * pass, c = id % CH, r = id / CH;
+        if (16 * CH % 64 != 0 && r >= 16) continue;
+        const int left = cols - (col + c * PER);
+        if (row + r >= rows || left <= 0) continue;
+        const Piece<U, PER> x = __builtin_bit_cast(Piece<U, PER>, *reinterpret_cast<const end_floatx4 *>(region + r * row_bytes + c * 16));
+        U *to = at(row + r) + col + c * PER;
+        if (left >= PER) {
+            *reinterpret_cast<Piece<U, PER> *>(to) = x;
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                if (e < left) to[e] = x.v[e];
+        }
+    }
+}
+
+template <typename T> __device__ inline void end_stage(char *at, float a, float b, float c, float d)
+{
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<end_floatx4 *>(at) = end_floatx4{a, b, c, d};
+    else *reinterpret_cast<Four<T> *>(at) = Four<T>{{static_cast<T>(a), static_cast<T>(b), static_cast<T>(c), static_cast<T>(d)}};
+}
+
+// Whether the activation's derivative is formed
+template <int ACT, typename T, bool GRAD, int FM, int FN>
+__device__ __forceinline__ void end_gated(const LinearArgs &args, const end_floatx4 (&acc)[FN][FM], char *region, int row0, int col0, int lane)
+{
+    const int held = (args.hidden + 15) / 16 * 16;              // columns of H, dG and dU that are written: zeros from `hidden` on
+    T *const C = static_cast<T *>(args.C0);
+    if constexpr (!GRAD) {
+        constexpr int HALF = FM / 2, ROWB = HALF * 32 + 16;
+        const int out0 = col0 / 2;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int row = row0 + 16 * j;
+            end_fence();
+#pragma unroll
+            for (int i = 0; i < HALF; ++i) {
+                const end_floatx4 g = acc[j][2 * i], u = acc[j][2 * i + 1];
+                if (args.kept != nullptr && row < args.rows && out0 + 16 * i < held) {
+                    float *const to = args.kept + kept_at(row, out0 + 16 * i, args.hidden) + 4 * lane;
+                    *reinterpret_cast<end_floatx4 *>(to) = g;
+                    *reinterpret_cast<end_floatx4 *>(to + 256) = u;
+                }
+                float h[4], slope;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    activation_of<ACT>(g[e], h[e], slope);
+                    h[e] *= u[e];
+                }
+                end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, h[0], h[1], h[2], h[3]);
+            }
+            end_fence();
+            end_drain<T, HALF * 16>(region, ROWB, row, out0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
+        }
+    } else {
+        constexpr int ROWB = FM * 32 + 16;
+        const int64_t beside = args.ldc0 / 2;                   // dU's columns behind dG's
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int row = row0 + 16 * j;
+            Four<T> du[FM];
+            end_fence();
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int col = col0 + 16 * i;
+                float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
+                if (row < args.rows && col < held) {
+                    const float *const from = args.kept + kept_at(row, col, args.hidden) + 4 * lane;
+                    const end_floatx4 g = *reinterpret_cast<const end_floatx4 *>(from), u = *reinterpret_cast<const end_floatx4 *>(from + 256);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float h, slope;
+                        activation_of<ACT>(g[e], h, slope);
+                        // (columns behind the last one are sums of whatever lies behind the rows of WD)
+                        const bool there = col + 4 * (lane / 16) + e < args.hidden;
+                        a[e] = there ? acc[j][i][e] * u[e] * slope : 0.f;
+                        b[e] = there ? acc[j][i][e] * h : 0.f;
+                    }
+                }
+                end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, a[0], a[1], a[2], a[3]);
+                du[i] = Four<T>{{static_cast<T>(b[0]), static_cast<T>(b[1]), static_cast<T>(b[2]), static_cast<T>(b[3])}};
+            }
+            end_fence();
+            end_drain<T, FM * 16>(region, ROWB, row, col0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
+            end_fence();
+#pragma unroll
+            for (int i = 0; i < FM; ++i) *reinterpret_cast<Four<T> *>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8) = du[i];
+            end_fence();
+            end_drain<T, FM * 16>(region, ROWB, row, col0, args.rows, held, lane, [&](int r) { return C + beside + r * args.ldc0; });
+        }
+    }
+}
+
+// (largest, sum of exp(z - largest)) of two sets of logits
+__device__ inline float2 join_scores(float2 a, float2 b)
+{
+    const float m = fmaxf(a.x, b.x), from = m == -__builtin_inff() ? 0.f : m;
+    return make_float2(m, a.y * exp_fast(a.x - from) + b.y * exp_fast(b.x - from));
+}
+
+// All wavefronts of the work-group come here, and nobody uses the LDS any more.  The wavefront's tile starts at (row0, col0) and is wavefront
+// (wr, wc) of WR x WC; region: its own; shared: WR * FN * 16 * WC float2 that no region overlaps (END_SCORES).
+template <typename T, int END, int FM, int FN, int WR, int WC>
+__device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (&acc)[FN][FM], char *region, float2 *shared, int tile_row, int tile_col, int wr, int wc, int lane)
+{
+    const int row0 = tile_row + wr * FN * 16, col0 = tile_col + wc * FM * 16;
+    if constexpr (END == END_STORE) {
+        if (args.partial != nullptr) {
+            constexpr int ROWB = FM * 64 + 16;
+            float *const to = args.partial + blockIdx.z * args.partial_stride;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                end_fence();
+#pragma unroll
+                for (int i = 0; i < FM; ++i) *reinterpret_cast<end_floatx4 *>(region + (lane % 16) * ROWB + i * 64 + (lane / 16) * 16) = acc[j][i];
+                end_fence();
+                end_drain<float, FM * 16>(region, ROWB, row0 + 16 * j, col0, args.rows, args.cols, lane, [&](int r) { return to + r * args.partial_ld; });
+            }
+        } else {
+            constexpr int ROWB = FM * 32 + 16;
+            const float scale = args.scale == nullptr ? 1.f : *args.scale;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                end_fence();
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+                    end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, acc[j][i][0] * scale, acc[j][i][1] * scale, acc[j][i][2] * scale, acc[j][i][3] * scale);
+                end_fence();
+                // (16 rows are of one matrix: `second` is a multiple of 64)
+                const int row = row0 + 16 * j;
+                const bool other = args.second > 0 && row >= args.second;
+                T *const C = static_cast<T *>(other ? args.C1 : args.C0) - (other ? args.second * args.ldc1 : 0);
+                const int64_t ldc = other ? args.ldc1 : args.ldc0;
+                const int rows = args.second == 0 ? args.rows : other ? args.second + args.rows0 : args.rows0;
+                if ((other ? args.C1 : args.C0) != nullptr) end_drain<T, FM * 16>(region, ROWB, row, col0, rows, args.cols, lane, [&](int r) { return C + r * ldc; });
+            }
+        }
+    } else if constexpr (END == END_GATED || END == END_GATED_GRAD) {
+        constexpr bool GRAD = END == END_GATED_GRAD;
+        if (args.activation == MG_ACT_SILU) end_gated<MG_ACT_SILU, T, GRAD>(args, acc, region, row0, col0, lane);
+        else if (args.activation == MG_ACT_GELU) end_gated<MG_ACT_GELU, T, GRAD>(args, acc, region, row0, col0, lane);
+        else if (args.activation == MG_ACT_GELU_TANH) end_gated<MG_ACT_GELU_TANH, T, GRAD>(args, acc, region, row0, col0, lane);
+        else end_gated<MG_ACT_RELU2, T, GRAD>(args, acc, region, row0, col0, lane);
+    } else if constexpr (END == END_SCORES) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int row = row0 + 16 * j + lane % 16;
+            const int64_t wanted = row < args.rows ? args.targets[row] - args.first : -1;
+            float m = -__builtin_inff(), s = 0.f;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int col = col0 + 16 * i + 4 * (lane / 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (col + e >= args.cols) acc[j][i][e] = -__builtin_inff();
+                    m = fmaxf(m, acc[j][i][e]);
+                    if (col + e == wanted && col + e < args.cols) args.target_score[row] = acc[j][i][e];
+                }
+            }
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float from = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += exp_fast(acc[j][i][e] - from);
+            s += __shfl_xor(s, 16);
+            s += __shfl_xor(s, 32);
+            if (lane < 16) shared[wc * (WR * FN * 16) + wr * FN * 16 + 16 * j + lane] = make_float2(m, s);
+        }
+        __syncthreads();
+        for (int r = threadIdx.x; r < WR * FN * 16; r += WR * WC * 64) {
+            if (tile_row + r >= args.rows) continue;
+            float2 all = shared[r];
+#pragma unroll
+            for (int w = 1; w < WC; ++w) all = join_scores(all, shared[w * (WR * FN * 16) + r]);
+            args.scores[static_cast<int64_t>(tile_col / (WC * FM * 16)) * args.rows + tile_row + r] = all;
+        }
+    } else {
+        constexpr int ROWB = FM * 32 + 16;
+        T *const C = static_cast<T *>(args.C0);
+        const int held = (args.cols + 15) / 16 * 16;
+        const float weight_scale = args.weight_scale == nullptr ? 1.f : *args.weight_scale;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int row = row0 + 16 * j + lane % 16;
+            int64_t wanted = -1;
+            float w = 0.f, lse = 0.f;
+            if (row < args.rows) {
+                wanted = args.targets[row];
+                if (wanted >= 0 && wanted < args.vocab) {
+                    w = (args.weights == nullptr ? 1.f : args.weights[row]) * weight_scale;
+                    lse = args.lse[row];
+                }
+                wanted -= args.first;
+            }
+            end_fence();
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int col = col0 + 16 * i + 4 * (lane / 16);
+                float d[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = exp_fast(acc[j][i][e] - lse) - (col + e == wanted ? 1.f : 0.f);
+                    d[e] = w != 0.f && col + e < args.cols ? w * p : 0.f;           // (a token that adds nothing adds nothing, whatever its logits are)
+                }
+                end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, d[0], d[1], d[2], d[3]);
+            }
+            end_fence();
+            end_drain<T, FM * 16>(region, ROWB, row0 + 16 * j, col0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
+        }
+    }
+}
+#endif
+
+}  // namespace mg

@@ -1,0 +1,307 @@
+// Softmax cross entropy over a vocabulary, with the projection in it.
+//
+// Logits of 16-bit matrices stay in the registers of the product's kernel: a tile leaves the largest one and the sum of exponentials of each of its
+// rows, and a second kernel joins the tiles (the running maximum and sum of a softmax, over tiles).  The gradient makes the logits again, a piece of the
+// vocabulary at a time, and leaves dz = w (exp(z - lse) - [target]) in the operands' type for the two products that read it: dX is a sum over all
+// pieces, each an FP32 slice of its own, dW's rows belong to one piece each.  FP32: pieces of logits in memory, products as mg_sgemm makes them.
+#include "linear_end.h"
+#include "internal.h"
+
+namespace mg {
+namespace {
+
+constexpr int64_t F = sizeof(float);
+constexpr int64_t PIECE_ELEMENTS = int64_t(1) << 27;              // of dz in 16 bits (256 MB, what the last-level cache holds); FP32: logits, half as many
+
+// columns of a piece: a multiple of 256, or the vocabulary
+int64_t piece_columns(int dtype, int64_t tokens, int64_t vocab)
+{
+    const int64_t most = (dtype == MG_F32 ? PIECE_ELEMENTS / 2 : PIECE_ELEMENTS) / tokens / 256 * 256;
+    const int64_t columns = most < 256 ? 256 : most;
+    return columns < vocab ? columns : vocab;
+}
+
+mg_status launched(hipError_t e) { return e == hipSuccess ? MG_OK : MG_ERR_LAUNCH; }
+
+// FP32: (largest, sum of exponentials) of a row of a piece of logits, and the target's logit.  A work-group a row; z is read twice, the second time from L2.
+__global__ __launch_bounds__(256) void scores_kernel(const float *Z, int64_t ldz, int cols, int64_t first, int tokens, const int64_t *targets, float2 *scores, float *target_score)
+{
+    __shared__ float parts[4];
+    const int row = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const float *z = Z + row * ldz;
+    float m = -__builtin_inff();
+    for (int c = threadIdx.x; c < cols; c += 256) m = fmaxf(m, z[c]);
+    for (int d = 32; d > 0; d /= 2) m = fmaxf(m, __shfl_xor(m, d));
+    if (lane == 0) parts[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(parts[0], parts[1]), fmaxf(parts[2], parts[3]));
+    __syncthreads();
+    const float from = m == -__builtin_inff() ? 0.f : m;
+    float s = 0.f;
+    for (int c = threadIdx.x; c < cols; c += 256) s += expf(z[c] - from);
+    for (int d = 32; d > 0; d /= 2) s += __shfl_xor(s, d);
+    if (lane == 0) parts[wave] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        scores[row] = make_float2(m, (parts[0] + parts[1]) + (parts[2] + parts[3]));
+        const int64_t t = targets[row] - first;
+        if (t >= 0 && t < cols) target_score[row] = z[t];
+    }
+    (void)tokens;
+}
+
+// FP32: dz in the place of z
+__global__ __launch_bounds__(256) void scores_grad_kernel(float *Z, int64_t ldz, int cols, int64_t first, int64_t vocab, const int64_t *targets, const float *lse,
+                                                          const float *weights)
+{
+    const int row = blockIdx.x;
+    const int64_t target = targets[row];
+    const float w = target >= 0 && target < vocab ? weights == nullptr ? 1.f : weights[row] : 0.f, l = lse[row];
+    float *z = Z + row * ldz;
+    for (int c = threadIdx.x; c < cols; c += 256) z[c] = w != 0.f ? w * (expf(z[c] - l) - (first + c == target ? 1.f : 0.f)) : 0.f;
+}
+
+// 16 tokens a work-group, 16 lanes a token: joins the tiles' scores in a fixed order
+__global__ __launch_bounds__(256) void join_scores_kernel(const float2 *scores, int tiles, int tokens, int64_t vocab, const int64_t *targets, const float *target_score, float *loss,
+                                                          float *lse)
+{
+    const int row = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
+    __shared__ float2 parts[256];
+    float2 all = make_float2(-__builtin_inff(), 0.f);
+    if (row < tokens)
+        for (int t = part; t < tiles; t += 16) all = join_scores(all, scores[static_cast<int64_t>(t) * tokens + row]);
+    parts[threadIdx.x] = all;
+    __syncthreads();
+    if (part != 0 || row >= tokens) return;
+    for (int p = 1; p < 16; ++p) all = join_scores(all, parts[16 * p + threadIdx.x]);
+    const float total = all.x + logf(all.y);
+    const int64_t target = targets[row];
+    lse[row] = total;
+    loss[row] = target >= 0 && target < vocab ? total - target_score[row] : 0.f;
+}
+
+// FP16: scale[0] = the power of two with which the largest weight becomes at most 2^14 (dz is a probability times a weight: its largest then is a
+// quarter of the largest FP16 number, probabilities down to 2^-28 of the largest weight are normal numbers); scale[1]: its inverse
+__global__ __launch_bounds__(256) void weight_scale_kernel(const float *weights, int tokens, float *scale)
+{
+    __shared__ uint32_t parts[4];
+    uint32_t most = weights == nullptr ? 0x3f800000u : 0u;
+    if (weights != nullptr)
+        for (int t = threadIdx.x; t < tokens; t += 256) {
+            const uint32_t w = __builtin_bit_cast(uint32_t, weights[t]) & 0x7fffffffu;
+            most = w < 0x7f800000u && w > most ? w : most;
+        }
+    for (int d = 32; d > 0; d /= 2) {
+        const uint32_t other = __shfl_xor(most, d);
+        most = other > most ? other : most;
+    }
+    if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = most;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < 4; ++w) most = parts[w] > most ? parts[w] : most;
+    // both the scale and its inverse have to be normal numbers
+    const int e = static_cast<int>(most >> 23) - 127, up = 13 - e < -126 ? -126 : 13 - e > 126 ? 126 : 13 - e;
+    scale[0] = most == 0 ? 1.f : power_of_two(up);
+    scale[1] = most == 0 ? 1.f : power_of_two(-up);
+}
+
+struct LossMemory {
+    float2 *scores;
+    float *target_score, *pieces;          // pieces: FP32 logits
+    size_t left;
+    void *rest;
+};
+
+LossMemory loss_memory(Arena &ws, int dtype, int64_t tokens, int64_t vocab)
+{
+    LossMemory m{};
+    const int64_t columns = vocab > 0 ? piece_columns(dtype, tokens, vocab) : 0;
+    m.target_score = static_cast<float *>(ws.take(tokens * F));
+    if (dtype == MG_F32) {
+        m.scores = static_cast<float2 *>(ws.take(vocab > 0 ? ceil_div(vocab, columns) * tokens * 8 : 0));
+        m.pieces = static_cast<float *>(ws.take(tokens * columns * F));
+    } else {
+        m.scores = static_cast<float2 *>(ws.take(ceil_div(vocab, 64) * tokens * 8));
+    }
+    m.left = ws.left();
+    m.rest = ws.take(0);
+    return m;
+}
+
+struct LossGradMemory {
+    void *dz;                              // a piece
+    float *scale;
+    float *slices;
+    int64_t slice;                         // elements of one
+    size_t left;
+    void *rest;
+};
+
+LossGradMemory loss_grad_memory(Arena &ws, int dtype, int64_t tokens, int64_t width, int64_t vocab)
+{
+    LossGradMemory m{};
+    const int64_t columns = piece_columns(dtype, tokens, vocab), count = ceil_div(vocab, columns);
+    m.scale = static_cast<float *>(ws.take(2 * F));
+    m.dz = ws.take(tokens * padded(columns) * (dtype == MG_F32 ? 4 : 2));
+    m.slice = tokens * padded(width);
+    if (dtype != MG_F32 && count > 1) m.slices = static_cast<float *>(ws.take(count * m.slice * F));
+    m.left = ws.left();
+    m.rest = ws.take(0);
+    return m;
+}
+
+size_t sgemm_room(int64_t tokens, int64_t width, int64_t vocab, bool gradient)
+{
+    const int64_t columns = piece_columns(MG_F32, tokens, vocab);
+    size_t most = 0;
+    auto add = [&](int ta, int tb, int64_t m, int64_t n, int64_t k, int64_t lda, int64_t ldb, int64_t ldc) {
+        const size_t v = mg_gemm_workspace_bytes(MG_F32, MG_ROW_MAJOR, ta, tb, m, n, k, lda, ldb, ldc);
+        most = v > most ? v : most;
+    };
+    for (int64_t some : {columns, vocab % columns})
+        if (some > 0) {
+            add(MG_NO_TRANS, MG_TRANS, tokens, some, width, width, width, columns);
+            if (gradient) {
+                add(MG_NO_TRANS, MG_NO_TRANS, tokens, width, some, columns, width, width);
+                add(MG_TRANS, MG_NO_TRANS, some, width, tokens, columns, width, width);
+            }
+        }
+    return most;
+}
+
+const float *row_of(const void *X, int64_t row, int64_t ld) { return static_cast<const float *>(X) + row * ld; }
+
+mg_status loss_f32(const LossProblem &p, const LossMemory &m)
+{
+    const int64_t columns = piece_columns(MG_F32, p.tokens, p.vocab);
+    for (int64_t first = 0, n = 0; first < p.vocab; first += columns, ++n) {
+        const int64_t some = p.vocab - first < columns ? p.vocab - first : columns;
+        const mg_status st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_TRANS, p.tokens, some, p.width, 1.f, static_cast<const float *>(p.X), p.ldx, row_of(p.W, first, p.ldw), p.ldw, 0.f,
+                                      m.pieces, columns, m.rest, m.left, p.stream);
+        if (st != MG_OK) return st;
+        scores_kernel<<<static_cast<uint32_t>(p.tokens), 256, 0, p.stream>>>(m.pieces, columns, static_cast<int>(some), first, static_cast<int>(p.tokens), p.targets, m.scores + n * p.tokens,
+                                                                             m.target_score);
+        if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
+    }
+    return MG_OK;
+}
+
+mg_status grad_f32(const LossProblem &p, const LossGradMemory &m)
+{
+    const int64_t columns = piece_columns(MG_F32, p.tokens, p.vocab);
+    float *const Z = static_cast<float *>(m.dz);
+    for (int64_t first = 0; first < p.vocab; first += columns) {
+        const int64_t some = p.vocab - first < columns ? p.vocab - first : columns;
+        const float *W = row_of(p.W, first, p.ldw), *X = static_cast<const float *>(p.X);
+        mg_status st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_TRANS, p.tokens, some, p.width, 1.f, X, p.ldx, W, p.ldw, 0.f, Z, columns, m.rest, m.left, p.stream);
+        if (st != MG_OK) return st;
+        scores_grad_kernel<<<static_cast<uint32_t>(p.tokens), 256, 0, p.stream>>>(Z, columns, static_cast<int>(some), first, p.vocab, p.targets, p.lse, p.weights);
+        if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
+        if (p.dX != nullptr)
+            st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_NO_TRANS, p.tokens, p.width, some, 1.f, Z, columns, W, p.ldw, first > 0 ? 1.f : 0.f, static_cast<float *>(p.dX), p.lddx, m.rest,
+                          m.left, p.stream);
+        if (st == MG_OK && p.dW != nullptr)
+            st = mg_sgemm(MG_ROW_MAJOR, MG_TRANS, MG_NO_TRANS, some, p.width, p.tokens, 1.f, Z, columns, X, p.ldx, 0.f, static_cast<float *>(p.dW) + first * p.lddw, p.lddw, m.rest, m.left,
+                          p.stream);
+        if (st != MG_OK) return st;
+    }
+    return MG_OK;
+}
+
+mg_status product(const LossProblem &p, int form, int end, LinearArgs args)
+{
+    args.k_per_slice = static_cast<int>(padded(args.k));
+    return launched(launch_linear_any(p.dtype, form, end, args, 1, p.stream));
+}
+
+LinearArgs logits(const LossProblem &p, int64_t first, int64_t columns)
+{
+    LinearArgs a{};
+    a.P = p.X; a.ldp = p.ldx;
+    a.Q0 = static_cast<const uint16_t *>(p.W) + first * p.ldw; a.ldq0 = p.ldw;
+    a.rows = static_cast<int>(p.tokens); a.cols = static_cast<int>(columns); a.k = static_cast<int>(p.width);
+    a.first = first; a.vocab = p.vocab; a.targets = p.targets;
+    return a;
+}
+
+mg_status grad_16(const LossProblem &p, const LossGradMemory &m)
+{
+    if (p.dtype == MG_F16) {
+        weight_scale_kernel<<<1, 256, 0, p.stream>>>(p.weights, static_cast<int>(p.tokens), m.scale);
+        if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
+    }
+    const int64_t columns = piece_columns(p.dtype, p.tokens, p.vocab), lead = padded(columns);
+    const int count = static_cast<int>(ceil_div(p.vocab, columns));
+    LinearArgs x{};                                        // dX
+    x.P = m.dz; x.ldp = lead; x.ldq0 = p.ldw;
+    x.rows = static_cast<int>(p.tokens); x.cols = static_cast<int>(p.width);
+    x.C0 = p.dX; x.ldc0 = p.lddx;
+    x.scale = p.dtype == MG_F16 ? m.scale + 1 : nullptr;
+    x.partial_ld = padded(p.width);
+    x.partial_stride = m.slice;
+    for (int64_t first = 0, n = 0; first < p.vocab; first += columns, ++n) {
+        const int64_t some = p.vocab - first < columns ? p.vocab - first : columns;
+        LinearArgs z = logits(p, first, some);
+        z.lse = p.lse; z.weights = p.weights; z.weight_scale = p.dtype == MG_F16 ? m.scale : nullptr;
+        z.C0 = m.dz; z.ldc0 = lead;
+        if (const mg_status st = product(p, FORM_KK, END_SCORES_GRAD, z)) return st;
+        if (p.dX != nullptr) {
+            x.Q0 = z.Q0;
+            x.k = static_cast<int>(some);
+            x.partial = count > 1 ? m.slices + n * m.slice : nullptr;
+            if (const mg_status st = product(p, FORM_KN, END_STORE, x)) return st;
+        }
+        if (p.dW != nullptr) {
+            LinearArgs w{};
+            w.P = m.dz; w.ldp = lead; w.Q0 = p.X; w.ldq0 = p.ldx;
+            w.rows = static_cast<int>(some); w.cols = static_cast<int>(p.width); w.k = static_cast<int>(p.tokens);
+            w.C0 = static_cast<uint16_t *>(p.dW) + first * p.lddw; w.ldc0 = p.lddw;
+            w.scale = x.scale;
+            if (const mg_status st = product(p, FORM_NN, END_STORE, w)) return st;
+        }
+    }
+    if (p.dX != nullptr && count > 1) {
+        x.partial = m.slices;
+        return launched(launch_linear_sum(p.dtype, x, count, p.stream));
+    }
+    return MG_OK;
+}
+
+}  // namespace
+
+size_t loss_workspace(int dtype, int64_t tokens, int64_t width, int64_t vocab, bool gradient)
+{
+    Arena ws{nullptr, 0, 0};
+    if (gradient) loss_grad_memory(ws, dtype, tokens, width, vocab);
+    else loss_memory(ws, dtype, tokens, vocab);
+    if (dtype == MG_F32 && vocab > 0) ws.take(sgemm_room(tokens, width, vocab, gradient));
+    return ws.used;
+}
+
+mg_status vocab_loss(const LossProblem &p)
+{
+    Arena ws = p.workspace;
+    const LossMemory m = loss_memory(ws, p.dtype, p.tokens, p.vocab);
+    int tiles = 0;
+    if (p.vocab > 0 && p.dtype == MG_F32) {
+        if (const mg_status st = loss_f32(p, m)) return st;
+        tiles = static_cast<int>(ceil_div(p.vocab, piece_columns(MG_F32, p.tokens, p.vocab)));
+    } else if (p.vocab > 0) {
+        LinearArgs a = logits(p, 0, p.vocab);
+        a.scores = m.scores;
+        a.target_score = m.target_score;
+        if (const mg_status st = product(p, FORM_KK, END_SCORES, a)) return st;
+        tiles = static_cast<int>(ceil_div(p.vocab, 64));
+    }
+    join_scores_kernel<<<static_cast<uint32_t>(ceil_div(p.tokens, 16)), 256, 0, p.stream>>>(m.scores, tiles, static_cast<int>(p.tokens), p.vocab, p.targets, m.target_score, p.loss, p.lse);
+    return launched(hipGetLastError());
+}
+
+mg_status vocab_loss_grad(const LossProblem &p)
+{
+    Arena ws = p.workspace;
+    const LossGradMemory m = loss_grad_memory(ws, p.dtype, p.tokens, p.width, p.vocab);
+    return p.dtype == MG_F32 ? grad_f32(p, m) : grad_16(p, m);
+}
+
+}  // namespace mg

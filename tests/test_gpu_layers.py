@@ -1,0 +1,448 @@
+"""Gated blocks, the loss over a vocabulary and clipping on the GPU against 64 bits (layer_reference.py), within bounds element by element."""
+import functools
+import math
+
+import pytest
+import torch
+
+from paper_1705_05249_amd import dense_layers as D, layers as L
+from tests import layer_reference as R
+
+pytestmark = pytest.mark.gpu
+
+KINDS = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+CODES = {torch.float32: L.MG_F32, torch.float16: L.MG_F16, torch.bfloat16: L.MG_BF16}
+MARK = -77.0                                # what memory outside the results holds
+
+
+def say(*what):
+    print(*what, flush=True)
+
+
+def normal(seed, *shape, sigma=1.0):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)) * sigma
+
+
+class Held:
+    """a matrix on the GPU inside a larger allocation: `lead` elements in front of it and rows `ld` apart, everything else MARK (or NaN around an operand)"""
+
+    def __init__(self, x, lead=0, extra=0, around=math.nan):
+        rows, cols = x.shape
+        self.ld = max(cols + extra, 1)
+        self.all = torch.full((lead + rows * self.ld + 64,), around, dtype=x.dtype)
+        view = self.all[lead:lead + rows * self.ld].view(rows, self.ld)[:, :cols]
+        view.copy_(x)
+        self.mask = torch.ones(self.all.shape, dtype=torch.bool)
+        self.mask[lead:lead + rows * self.ld].view(rows, self.ld)[:, :cols] = False
+        self.host, self.all = self.all.clone(), self.all.cuda()
+        self.x = self.all[lead:lead + rows * self.ld].view(rows, self.ld)[:, :cols]
+
+    def at(self):
+        return self.x.data_ptr(), self.ld
+
+    def untouched(self):
+        bits = torch.int32 if self.all.dtype == torch.float32 else torch.int16
+        return torch.equal(self.all.cpu().view(bits)[self.mask], self.host.view(bits)[self.mask])
+
+
+def result(rows, cols, dtype, lead=0, extra=0):
+    return Held(torch.full((rows, cols), MARK, dtype=dtype), lead, extra, around=MARK)
+
+
+def scratch(size):
+    """a workspace of exactly that size, full of NaN, with a guard behind it"""
+    held = torch.full((size + 4096,), 255, dtype=torch.uint8, device="cuda")
+    return held, held[:size]
+
+
+# (tokens, width, hidden): one of everything, ends inside pieces of 8, 16, 64 and tiles of 64, 128, 256, sums of one and of many pieces
+BLOCKS = [(1, 1, 1), (1, 8, 16), (2, 64, 15), (3, 200, 129), (17, 33, 100), (64, 64, 64), (65, 136, 72), (130, 257, 65), (300, 72, 264), (257, 520, 136), (1, 520, 600), (9, 1000, 31),
+          (33, 96, 300), (5, 2056, 40)]
+
+
+def run_block(case, act, dtype, lead=0, extra=0, keep=True, backward=True, wanted=(True,) * 4, room="all"):
+    tokens, width, hidden = case
+    code, kind = CODES[dtype], D.ACTIVATIONS[act]
+    x, wg, wu, wd, dy = (t.to(dtype) for t in (normal(1, tokens, width), normal(2, hidden, width, sigma=width ** -0.5), normal(3, hidden, width, sigma=width ** -0.5),
+                                                normal(4, width, hidden, sigma=hidden ** -0.5), normal(5, tokens, width)))
+    want = R.block(x, wg, wu, wd, act, dtype, dy)
+    held = [Held(t, lead, extra) for t in (x, wg, wu, wd)]
+    arguments = [v for h in held for v in h.at()]
+    y = result(tokens, width, dtype, lead, extra)
+    kept_all, kept = scratch(L.mg_gated_kept_bytes(code, *case)) if keep else (None, None)
+    ws_all, ws = scratch(L.mg_gated_forward_workspace_bytes(code, *case))
+    L.mg_gated_forward(code, kind, *case, *arguments, *y.at(), kept, ws)
+    torch.cuda.synchronize()
+    R.check(y.x, want["y"], "y")
+    assert y.untouched() and bool((ws_all[len(ws):] == 255).all())
+    assert kept_all is None or bool((kept_all[len(kept):] == 255).all())
+    if not backward:
+        return
+    before = kept.clone()
+    d = Held(dy, lead, extra)
+    outs = [result(*shape, dtype, lead, extra) if on else None for on, shape in zip(wanted, ((tokens, width), (hidden, width), (hidden, width), (width, hidden)))]
+    ws_all, ws = scratch(L.mg_gated_backward_workspace_bytes(code, *case))
+    L.mg_gated_backward(code, kind, *case, *arguments, *d.at(), kept, *(v for o in outs for v in (o.at() if o else (None, 0))), ws)
+    torch.cuda.synchronize()
+    for name, o in zip(("dx", "dwg", "dwu", "dwd"), outs):
+        if o is not None:
+            R.check(o.x, want[name], name)
+            assert o.untouched(), name
+    assert torch.equal(before, kept) and bool((ws_all[len(ws):] == 255).all())
+    assert all(h.untouched() for h in held)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("case", BLOCKS, ids=lambda c: "x".join(map(str, c)))
+def test_block(case, dtype):
+    say("block", case, dtype)
+    run_block(case, R.ACTS[(sum(case) + len(dtype)) % 4], KINDS[dtype])
+
+
+@pytest.mark.parametrize("act", R.ACTS)
+@pytest.mark.parametrize("dtype", KINDS)
+def test_activations(act, dtype):
+    run_block((70, 80, 90), act, KINDS[dtype])
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("lead,extra", [(1, 0), (0, 1), (3, 5), (8, 8), (0, 24)])
+@pytest.mark.parametrize("case", [(40, 72, 136), (33, 61, 75), (3, 264, 72)], ids=lambda c: "x".join(map(str, c)))
+def test_block_of_parts_of_larger_matrices(case, lead, extra, dtype):
+    run_block(case, "gelu_tanh", KINDS[dtype], lead, extra)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("case", [(1, 264, 72), (4, 1024, 520), (16, 64, 2048), (17, 513, 100), (48, 256, 256), (64, 1000, 1000), (100, 128, 64)], ids=lambda c: "x".join(map(str, c)))
+def test_served_tokens(case, dtype):
+    say("served", case, dtype)
+    for lead, extra in ((0, 0), (1, 2)):
+        run_block(case, "silu", KINDS[dtype], lead, extra, keep=False, backward=False)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("wanted", [(True, False, False, False), (False, True, False, False), (False, False, True, False), (False, False, False, True), (False, True, True, False)])
+def test_gradients_that_are_wanted(wanted, dtype):
+    run_block((70, 72, 90), "gelu", KINDS[dtype], wanted=wanted)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+def test_blocks_without_work(dtype):
+    kind, code = KINDS[dtype], CODES[KINDS[dtype]]
+    y = result(3, 5, kind, extra=2)
+    w = torch.zeros(8, dtype=kind, device="cuda")
+    L.mg_gated_forward(code, L.MG_ACT_SILU, 3, 5, 0, w, 5, w, 5, w, 5, w, 1, *y.at())
+    assert not bool(y.x.any()) and y.untouched()
+    outs = [result(*shape, kind, extra=1) for shape in ((0, 5), (4, 5), (4, 5), (5, 4))]
+    L.mg_gated_backward(code, L.MG_ACT_SILU, 0, 5, 4, None, 5, w, 5, w, 5, w, 4, None, 5, None, *(v for o in outs for v in o.at()))
+    torch.cuda.synchronize()
+    assert all(not bool(o.x.any()) and o.untouched() for o in outs)
+
+
+# (tokens, width, vocab)
+LOSSES = [(1, 1, 1), (1, 8, 100), (2, 64, 65), (3, 33, 1000), (16, 256, 513), (17, 100, 64), (64, 72, 300), (70, 136, 1029), (130, 65, 200), (300, 264, 520), (257, 64, 257), (5, 1032, 4100)]
+
+
+def run_loss(case, dtype, lead=0, extra=0, weights="each", ignored=0.3, wanted=(True, True), sigma=2.0):
+    tokens, width, vocab = case
+    code = CODES[dtype]
+    x, w = normal(1, tokens, width).to(dtype), normal(2, vocab, width, sigma=sigma * width ** -0.5).to(dtype)
+    gen = torch.Generator().manual_seed(3)
+    targets = torch.randint(0, vocab, (tokens,), generator=gen)
+    out = torch.rand(tokens, generator=gen) < ignored
+    targets[out] = torch.tensor([-100, -1, vocab, 1 << 40, -(1 << 33)])[torch.arange(tokens) % 5][out]
+    token_weights = {"each": torch.rand(tokens, generator=gen) * 2 - 0.5, "mean": torch.full((tokens,), 1.0 / 7001), "none": None, "large": torch.full((tokens,), 1024.0),
+                     "zeros": torch.where(torch.arange(tokens) % 2 == 0, 0.0, 1.0)}[weights]
+    want = R.loss(x, w, targets, dtype, token_weights, gradient=True)
+    held = [Held(t, lead, extra) for t in (x, w)]
+    arguments = [v for h in held for v in h.at()]
+    target = targets.cuda()
+    loss, lse = (result(1, tokens, torch.float32) for _ in range(2))
+    ws_all, ws = scratch(L.mg_vocab_loss_workspace_bytes(code, *case))
+    L.mg_vocab_loss(code, *case, *arguments, target, loss.at()[0], lse.at()[0], ws)
+    torch.cuda.synchronize()
+    R.check(lse.x[0], want["lse"], "lse")
+    R.check(loss.x[0], want["loss"], "loss")
+    assert loss.untouched() and lse.untouched() and bool((ws_all[len(ws):] == 255).all())
+    outs = [result(*shape, dtype, lead, extra) if on else None for on, shape in zip(wanted, ((tokens, width), (vocab, width)))]
+    ws_all, ws = scratch(L.mg_vocab_loss_grad_workspace_bytes(code, *case))
+    L.mg_vocab_loss_grad(code, *case, *arguments, target, lse.at()[0], None if token_weights is None else token_weights.cuda(), *(v for o in outs for v in (o.at() if o else (None, 0))), ws)
+    torch.cuda.synchronize()
+    for name, o in zip(("dx", "dw"), outs):
+        if o is not None:
+            R.check(o.x, want[name], name)
+            assert o.untouched(), name
+    assert bool((ws_all[len(ws):] == 255).all()) and all(h.untouched() for h in held)
+    counts = (targets >= 0) & (targets < vocab)
+    if wanted[0]:
+        assert not bool(outs[0].x.cpu()[~counts].any()) and not bool(loss.x[0].cpu()[~counts].any())       # ignored tokens: exactly nothing
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("case", LOSSES, ids=lambda c: "x".join(map(str, c)))
+def test_loss(case, dtype):
+    say("loss", case, dtype)
+    run_loss(case, KINDS[dtype])
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("weights,ignored", [("mean", 0.0), ("none", 0.5), ("large", 0.1), ("zeros", 0.2), ("each", 1.0)])
+def test_weights_of_tokens(weights, ignored, dtype):
+    run_loss((40, 72, 333), KINDS[dtype], weights=weights, ignored=ignored)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("lead,extra", [(1, 0), (0, 3), (8, 8)])
+def test_loss_of_parts_of_larger_matrices(lead, extra, dtype):
+    for case in ((40, 72, 136), (21, 45, 301)):
+        run_loss(case, KINDS[dtype], lead, extra)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("wanted", [(True, False), (False, True)])
+def test_gradients_of_the_loss_that_are_wanted(wanted, dtype):
+    run_loss((40, 72, 333), KINDS[dtype], wanted=wanted)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+def test_sharp_logits(dtype):
+    """far from each other: nearly all of the probability is one token's, or the largest logit is far above zero"""
+    run_loss((33, 64, 400), KINDS[dtype], sigma=25.0, ignored=0.1)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+def test_losses_without_work(dtype):
+    kind, code = KINDS[dtype], CODES[KINDS[dtype]]
+    w = torch.zeros(64, dtype=kind, device="cuda")
+    targets = torch.tensor([0, -1, 3], device="cuda")
+    loss, lse = torch.full((3,), MARK, device="cuda"), torch.full((3,), MARK, device="cuda")
+    ws = scratch(L.mg_vocab_loss_workspace_bytes(code, 3, 4, 0))[1]
+    L.mg_vocab_loss(code, 3, 4, 0, w, 4, None, 4, targets, loss, lse, ws)
+    assert loss.tolist() == [0.0] * 3 and lse.tolist() == [-math.inf] * 3
+    ws = scratch(L.mg_vocab_loss_workspace_bytes(code, 3, 0, 7))[1]
+    L.mg_vocab_loss(code, 3, 0, 7, None, 1, None, 1, targets, loss, lse, ws)                        # all logits zero
+    assert torch.allclose(lse.cpu(), torch.full((3,), math.log(7.0))) and torch.allclose(loss.cpu(), torch.tensor([math.log(7.0), 0.0, math.log(7.0)]))
+    dx, dw = result(3, 4, kind), result(6, 4, kind, extra=1)
+    L.mg_vocab_loss_grad(code, 3, 4, 0, w, 4, None, 4, targets, lse, None, *dx.at(), None, 0)
+    L.mg_vocab_loss_grad(code, 0, 4, 6, None, 4, w, 4, None, None, None, None, 0, *dw.at())
+    assert not bool(dx.x.any()) and not bool(dw.x.any()) and dw.untouched() and dx.untouched()
+
+
+def test_tokens_that_do_not_count_may_hold_anything():
+    """infinities and NaN in ignored tokens and in tokens of weight zero stay where they are"""
+    for kind in KINDS.values():
+        x, w = normal(1, 20, 40), normal(2, 70, 40)
+        x[3], x[5, 0], x[6, 1] = math.nan, math.inf, -math.inf
+        targets = torch.randint(0, 70, (20,), generator=torch.Generator().manual_seed(1))
+        targets[3] = -100
+        weights = torch.ones(20)
+        weights[5] = weights[6] = 0.0
+        head = D.VocabLoss(w.to(kind).cuda())
+        loss = head.forward(x.to(kind).cuda(), targets.cuda())
+        dx, _ = head.backward(weights.cuda())
+        fine = torch.ones(20, dtype=torch.bool)
+        fine[[3, 5, 6]] = False
+        assert bool(loss.cpu()[fine].isfinite().all()) and float(loss[3]) == 0.0
+        assert bool(dx.cpu()[fine].isfinite().all()) and not bool(dx[[3, 5, 6]].any())
+
+
+# ---- clipping
+
+def run_clip(sizes, kinds, max_norm, place, lead=0, scale=1.0):
+    tensors = [Held((normal(i, 1, n) * scale).to(KINDS[k]), lead, around=MARK) for i, (n, k) in enumerate(zip(sizes, kinds))]
+    before = [t.host[lead:lead + n].clone() for t, n in zip(tensors, sizes)]
+    results = tensors if place == "in place" else [result(1, n, KINDS[k], lead) for n, k in zip(sizes, kinds)]
+    total = math.sqrt(sum(float(b.double().square().sum()) for b in before))
+    codes = torch.tensor([CODES[KINDS[k]] for k in kinds], dtype=torch.int32)
+    at = lambda held: torch.tensor([h.at()[0] for h in held], dtype=torch.int64)  # noqa: E731
+    norm = torch.full((1,), MARK, device="cuda")
+    ws_all, ws = scratch(L.mg_gradient_workspace_bytes(len(sizes)))
+    args = len(sizes), codes, at(tensors)
+    L.mg_gradient_norm(*args, torch.tensor(sizes), norm, ws)
+    assert abs(float(norm) - total) <= 2.0 ** -23 * total
+    norm.fill_(MARK)
+    ws_all.fill_(255)
+    limit = max_norm * total if math.isfinite(max_norm) else max_norm
+    limit = float(torch.tensor(limit))
+    L.mg_gradient_clip(*args, None if place == "in place" else at(results), torch.tensor(sizes), limit, norm, ws)
+    torch.cuda.synchronize()
+    assert abs(float(norm) - total) <= 2.0 ** -23 * total and bool((ws_all[len(ws):] == 255).all())
+    factor = torch.tensor(limit / total if limit < total else 1.0)
+    for b, r, n, k in zip(before, results, sizes, kinds):
+        got = r.x.cpu().view(-1)
+        assert r.untouched()
+        if limit >= total:
+            assert torch.equal(got, b)
+        elif n:
+            # the factor is off by a step at most (the norm's 64-bit sum has another order), the product by half of one, the result by half a step of its type
+            want = b.double() * factor.double()
+            assert bool(((got.double() - want).abs() <= 2.0 ** -22 * want.abs() + R.HALF[KINDS[k]] * want.abs() * (1 + 2.0 ** -20) + R.TINY[KINDS[k]]).all())
+
+
+@pytest.mark.parametrize("place", ["in place", "beside"])
+@pytest.mark.parametrize("max_norm", [0.25, 1.5, math.inf])
+@pytest.mark.parametrize("sizes", [(1,), (0, 3, 0), (7, 4096, 4097, 8192, 8193, 100), (100000, 1, 30000), tuple(range(130)), (300001,)], ids=lambda s: f"{len(s)}_{sum(s)}")
+def test_clip(sizes, max_norm, place):
+    kinds = [("f32", "f16", "bf16")[i % 3] for i in range(len(sizes))]
+    say("clip", len(sizes), sum(sizes), max_norm, place)
+    if sum(sizes) == 0:
+        return
+    run_clip(sizes, kinds, max_norm, place)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_clip_at_any_address(kind):
+    run_clip((5000, 33, 70001), (kind,) * 3, 0.5, "beside", lead=1)
+    run_clip((5000, 33, 70001), (kind,) * 3, 0.5, "in place", lead=3)
+
+
+def test_squares_beyond_fp32():
+    run_clip((5000, 600), ("f32", "bf16"), 0.5, "beside", scale=1e30)
+    run_clip((5000, 600), ("f32", "bf16"), 0.5, "beside", scale=1e-30)
+
+
+def test_limits_of_clipping():
+    g = torch.tensor([3.0, 4.0, 0.0], device="cuda")
+    grads = D.Gradients([g])
+    assert float(grads.norm()) == 5.0
+    assert float(grads.clip(5.0)) == 5.0 and g.tolist() == [3.0, 4.0, 0.0]              # no larger than the limit
+    assert float(grads.clip(0.0)) == 5.0 and g.tolist() == [0.0, 0.0, 0.0]
+    assert float(grads.clip(0.0)) == 0.0 and g.tolist() == [0.0, 0.0, 0.0]              # 0 / 0 is never formed
+    for bad in (math.inf, -math.inf, math.nan):
+        g.copy_(torch.tensor([1.0, bad, 2.0]))
+        n = float(grads.clip(0.5))
+        assert not math.isfinite(n) and math.isnan(n) == math.isnan(bad) and g[0] == 1.0 and g[2] == 2.0
+    none = D.Gradients([])
+    none.value.fill_(MARK)
+    assert float(none.norm()) == 0.0
+    none.value.fill_(MARK)
+    assert float(none.clip(1.0)) == 0.0
+    empty = D.Gradients([torch.empty(0, device="cuda")])
+    assert float(empty.clip(1.0)) == 0.0
+
+
+# ---- together, as a program uses them
+
+def make(dtype, tokens=150, width=96, hidden=200, vocab=500, seed=10):
+    block = D.GatedBlock(*(normal(seed + i, r, c, sigma=c ** -0.5).to(dtype).cuda() for i, (r, c) in enumerate(((hidden, width), (hidden, width), (width, hidden)))))
+    head = D.VocabLoss(normal(seed + 3, vocab, width, sigma=width ** -0.5).to(dtype).cuda())
+    x = normal(seed + 4, tokens, width).to(dtype).cuda()
+    targets = torch.randint(-1, vocab, (tokens,), generator=torch.Generator().manual_seed(seed)).cuda()
+    return block, head, x, targets
+
+
+@functools.lru_cache(None)
+def exact_step(dtype):
+    block, head, x, targets = make(dtype)
+    leaves = [t.double().cpu().requires_grad_() for t in (block.gate, block.up, block.down, head.weights)]
+    xd, t = x.double().cpu(), targets.cpu()
+    y = xd + (torch.nn.functional.silu(xd @ leaves[0].T) * (xd @ leaves[1].T)) @ leaves[2].T
+    loss = torch.nn.functional.cross_entropy(y @ leaves[3].T, t.clamp(min=0), reduction="none") * (t >= 0)
+    grads = torch.autograd.grad(loss.sum() / (t >= 0).sum(), leaves)
+    norm = math.sqrt(sum(float(g.square().sum()) for g in grads))
+    return loss.detach(), norm, [g * min(1.0, 0.05 / norm) for g in grads]
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+def test_a_training_step(dtype):
+    kind = KINDS[dtype]
+    want_loss, want_norm, want = exact_step(kind)
+    block, head, x, targets = make(kind)
+    loss, norm, grads = D.train_step(block, head, x, targets, 0.05)
+    # y and dy are rounded to the type between the block and the loss, H, dG, dU, dz and results once more: eight roundings of half a step at most, as parts of
+    # norms; each logit's rounding of y moves a probability by up to |z| / sqrt(width) half steps beside them, which doubles it
+    near = 16 * R.HALF[kind] + 1e-5
+    assert float((loss.cpu().double() - want_loss).norm()) <= near * float(want_loss.norm())
+    assert abs(float(norm) - want_norm) <= near * want_norm
+    for g, w in zip(grads, want):
+        assert float((g.cpu().double() - w).norm()) <= near * float(w.norm())
+
+
+def graph_of(fn):
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        fn()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = fn()
+    return graph, out
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+def test_a_captured_step_gives_what_an_eager_one_does(dtype):
+    """bit for bit, on every replay, with the program's own work and new inputs between them; two graphs take turns"""
+    block, head, x, targets = make(KINDS[dtype])
+    xs = [x.clone(), make(KINDS[dtype], seed=20)[2]]
+
+    def step(held):
+        y = block.forward(held)
+        loss = head.forward(y, targets)
+        dy, dhead = head.backward()
+        grads = [*block.backward(dy), dhead]
+        return [loss, Clip(grads), y, *grads]
+
+    def Clip(grads):
+        g = D.Gradients(grads)
+        lists.append(g)
+        return g.clip(1.0)
+
+    lists, eager = [], []
+    for source in xs:
+        eager.append([t.clone() for t in step(source)])
+    held = [x.clone(), x.clone()]
+    graphs = [graph_of(lambda h=h: step(h)) for h in held]
+    for turn in range(4):
+        for n, (graph, out) in enumerate(graphs):
+            which = (turn + n) % 2
+            held[n].copy_(xs[which])
+            graph.replay()
+            again = step(xs[1 - which])                       # the program's own work in between
+            torch.cuda.synchronize()
+            for k, (a, b) in enumerate(zip(out, eager[which])):
+                assert torch.equal(a, b), (turn, n, k)
+            for k, (a, b) in enumerate(zip(again, eager[1 - which])):
+                assert torch.equal(a, b), (turn, n, k)
+
+
+def test_calls_go_to_the_stream_they_are_given():
+    block, head, x, targets = make(torch.bfloat16)
+    want = [block.forward(x), head.forward(x, targets)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [block.forward(x), head.forward(x, targets)]
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_layers_take_views_and_refuse_other_types():
+    block, head, x, targets = make(torch.float16)
+    wide = torch.zeros(x.shape[0], x.shape[1] + 5, dtype=x.dtype, device="cuda")
+    wide[:, 2:-3] = x
+    want = block.forward(x)
+    assert torch.equal(block.forward(wide[:, 2:-3]), want) or float((block.forward(wide[:, 2:-3]).double() - want.double()).norm()) <= 2 ** -10 * float(want.double().norm())
+    turned = x.T.contiguous().T
+    assert torch.equal(block.forward(turned), want)
+    with pytest.raises(TypeError):
+        block.forward(x.float())
+    with pytest.raises(ValueError):
+        block.forward(x[:, :-1])
+    with pytest.raises(TypeError):
+        head.forward(x, targets.int())
+    with pytest.raises(ValueError):
+        head.forward(x, targets[:-1])
+    with pytest.raises(ValueError):
+        block.forward(x.cpu())
+    with pytest.raises(ValueError):
+        D.Gradients([x.T])
+    block.forward(x, keep=False)
+    with pytest.raises(RuntimeError):
+        block.backward(x)
+
+
+def test_example_runs(capsys):
+    D.main(tokens=96, width=64, hidden=80, vocab=200, steps=2)
+    assert "step   1" in capsys.readouterr().out
