@@ -145,29 +145,84 @@ size_t held_rows(int64_t tokens, int64_t cols) { return static_cast<size_t>(toke
 
 mg_status launched(hipError_t e) { return e == hipSuccess ? MG_OK : MG_ERR_LAUNCH; }
 
-mg_status product(const GatedProblem &p, int form, int end, LinearArgs args)
+// An operand of the caller, or its copy
+struct Operand {
+    const void *at;
+    int64_t ld;
+    bool padded;
+};
+
+// Operands that the direct-to-LDS kernels do not take as they are get a copy while the workspace has room.  `along`: the operand lies along a sum.
+// Copies read and write what a product of few tokens reads once (333 tokens: the any-address kernels would take longer by far).
+class Copies {
+  public:
+    Copies(Arena &ws, bool wanted) : ws_(ws), wanted_(wanted) {}
+    Operand operator()(const void *X, int64_t ld, int64_t rows, int64_t cols, bool along)
+    {
+        const bool fine = reinterpret_cast<uintptr_t>(X) % 16 == 0 && ld % 8 == 0 && (!along || cols % 8 == 0);
+        const size_t bytes = static_cast<size_t>(rows * padded(cols)) * 2;
+        if (fine || !wanted_ || ws_.left() < bytes) return {X, ld, false};
+        const int n = list_.count++;
+        list_.from[n] = X; list_.to[n] = ws_.take(bytes); list_.ld[n] = ld; list_.rows[n] = rows; list_.cols[n] = static_cast<int>(cols);
+        return {list_.to[n], padded(cols), true};
+    }
+    hipError_t launch(hipStream_t stream) const { return launch_linear_copies(list_, stream); }
+
+  private:
+    Arena &ws_;
+    bool wanted_;
+    LinearCopies list_{};
+};
+
+constexpr int64_t COPY_TOKENS = 128;              // from here on operands are copied
+size_t copy_bytes(int64_t rows, int64_t cols) { return (static_cast<size_t>(rows * padded(cols)) * 2 + 255) / 256 * 256; }
+
+// what dense operands need
+size_t copies_room(int64_t tokens, int64_t width, int64_t hidden, bool backward)
 {
-    args.k_per_slice = static_cast<int>(padded(args.k));
-    return launched(launch_linear_any(p.dtype, form, end, args, 1, p.stream));
+    if (tokens < COPY_TOKENS) return 0;
+    size_t room = 0;
+    if (width % 8 != 0) room += copy_bytes(tokens, width) * (backward ? 2 : 1) + 2 * copy_bytes(hidden, width);
+    if (hidden % 8 != 0) room += copy_bytes(width, hidden);
+    return room;
 }
+
+size_t forward_room(int64_t tokens, int64_t width, int64_t hidden) { return linear_room(FORM_KK, END_STORE, tokens, width, hidden); }
+size_t backward_room(int64_t tokens, int64_t width, int64_t hidden)
+{
+    size_t most = linear_room(FORM_KN, END_STORE, tokens, width, 2 * padded(hidden));
+    for (const size_t v : {linear_room(FORM_NN, END_STORE, 2 * padded(hidden), width, tokens), linear_room(FORM_NN, END_STORE, width, hidden, tokens)}) most = v > most ? v : most;
+    return most;
+}
+
+void gate(LinearArgs &a, const Operand &q) { a.Q0 = q.at; a.ldq0 = q.ld; a.q_padded = q.padded; }
+void left(LinearArgs &a, const Operand &p) { a.P = p.at; a.ldp = p.ld; a.p_padded = p.padded; }
 
 mg_status forward_16(const GatedProblem &p)
 {
     Arena ws = p.workspace;
     float *const kept = static_cast<float *>(p.kept);
     void *const H = kept != nullptr ? static_cast<char *>(p.kept) + kept_scores(p.tokens, p.hidden) : ws.take(held_rows(p.tokens, p.hidden));
+    const size_t wanted = forward_room(p.tokens, p.width, p.hidden), room_bytes = wanted < ws.left() ? wanted : ws.left();
+    void *const room = ws.take(room_bytes);
+    Copies copied(ws, p.tokens >= COPY_TOKENS);
+    const Operand x = copied(p.X, p.ldx, p.tokens, p.width, true), wg = copied(p.WG, p.ldwg, p.hidden, p.width, true), wu = copied(p.WU, p.ldwu, p.hidden, p.width, true),
+                  wd = copied(p.WD, p.ldwd, p.width, p.hidden, true);
+    if (const hipError_t e = copied.launch(p.stream)) return launched(e);
     LinearArgs a{};
-    a.P = p.X; a.ldp = p.ldx;
-    a.Q0 = p.WG; a.ldq0 = p.ldwg; a.Q1 = p.WU; a.ldq1 = p.ldwu;
+    left(a, x);
+    gate(a, wg);
+    a.Q1 = wu.at; a.ldq1 = wu.ld; a.q_padded = wg.padded && wu.padded;
     a.rows = static_cast<int>(p.tokens); a.cols = static_cast<int>(kept_blocks(p.hidden) * 32); a.k = static_cast<int>(p.width);
     a.hidden = static_cast<int>(p.hidden); a.activation = p.activation; a.kept = kept;
     a.C0 = H; a.ldc0 = padded(p.hidden);
-    if (const mg_status st = product(p, FORM_KK, END_GATED, a)) return st;
+    if (const hipError_t e = launch_linear(p.dtype, FORM_KK, END_GATED, a, nullptr, 0, p.stream)) return launched(e);
     LinearArgs b{};
-    b.P = H; b.ldp = padded(p.hidden); b.Q0 = p.WD; b.ldq0 = p.ldwd;
+    left(b, {H, padded(p.hidden), true});
+    gate(b, wd);
     b.rows = a.rows; b.cols = static_cast<int>(p.width); b.k = static_cast<int>(p.hidden);
     b.C0 = p.Y; b.ldc0 = p.ldy;
-    return product(p, FORM_KK, END_STORE, b);
+    return launched(launch_linear(p.dtype, FORM_KK, END_STORE, b, room, room_bytes, p.stream));
 }
 
 mg_status backward_16(const GatedProblem &p)
@@ -175,39 +230,52 @@ mg_status backward_16(const GatedProblem &p)
     Arena ws = p.workspace;
     const int64_t half = padded(p.hidden);
     void *const d = ws.take(held_rows(p.tokens, p.hidden) * 2);         // dG and dU, side by side
-    float *const kept = static_cast<float *>(p.kept);
+    const size_t wanted = backward_room(p.tokens, p.width, p.hidden), room_bytes = wanted < ws.left() ? wanted : ws.left();
+    void *const room = ws.take(room_bytes);
+    const bool inner = p.dX != nullptr || p.dWG != nullptr || p.dWU != nullptr, gates = p.dWG != nullptr || p.dWU != nullptr;
+    Copies copied(ws, p.tokens >= COPY_TOKENS);
+    const Operand none{nullptr, 0, false};
+    const Operand dy = copied(p.dY, p.lddy, p.tokens, p.width, inner), x = gates ? copied(p.X, p.ldx, p.tokens, p.width, false) : none,
+                  wd = inner ? copied(p.WD, p.ldwd, p.width, p.hidden, false) : none, wg = p.dX != nullptr ? copied(p.WG, p.ldwg, p.hidden, p.width, false) : none,
+                  wu = p.dX != nullptr ? copied(p.WU, p.ldwu, p.hidden, p.width, false) : none;
+    if (const hipError_t e = copied.launch(p.stream)) return launched(e);
     const int tokens = static_cast<int>(p.tokens), width = static_cast<int>(p.width), hidden = static_cast<int>(p.hidden);
-    if (p.dX != nullptr || p.dWG != nullptr || p.dWU != nullptr) {
+    const Operand both{d, 2 * half, true};
+    if (inner) {
         LinearArgs a{};
-        a.P = p.dY; a.ldp = p.lddy; a.Q0 = p.WD; a.ldq0 = p.ldwd;
+        left(a, dy);
+        gate(a, wd);
         a.rows = tokens; a.cols = hidden; a.k = width;
-        a.hidden = hidden; a.activation = p.activation; a.kept = kept;
+        a.hidden = hidden; a.activation = p.activation; a.kept = static_cast<float *>(p.kept);
         a.C0 = d; a.ldc0 = 2 * half;
-        if (const mg_status st = product(p, FORM_KN, END_GATED_GRAD, a)) return st;
+        if (const hipError_t e = launch_linear(p.dtype, FORM_KN, END_GATED_GRAD, a, nullptr, 0, p.stream)) return launched(e);
     }
     if (p.dX != nullptr) {
         LinearArgs a{};
-        a.P = d; a.ldp = 2 * half; a.Q0 = p.WG; a.ldq0 = p.ldwg; a.Q1 = p.WU; a.ldq1 = p.ldwu;
+        left(a, both);
+        gate(a, wg);
+        a.Q1 = wu.at; a.ldq1 = wu.ld;
         a.segment = static_cast<int>(half); a.lines = hidden;
         a.rows = tokens; a.cols = width; a.k = static_cast<int>(2 * half);
         a.C0 = p.dX; a.ldc0 = p.lddx;
-        if (const mg_status st = product(p, FORM_KN, END_STORE, a)) return st;
+        if (const hipError_t e = launch_linear(p.dtype, FORM_KN, END_STORE, a, room, room_bytes, p.stream)) return launched(e);
     }
-    if (p.dWG != nullptr || p.dWU != nullptr) {
+    if (gates) {
         LinearArgs a{};
-        a.P = d; a.ldp = 2 * half; a.Q0 = p.X; a.ldq0 = p.ldx;
+        left(a, both);
+        gate(a, x);
         a.rows = static_cast<int>(2 * half); a.cols = width; a.k = tokens;
         a.second = static_cast<int>(half); a.rows0 = hidden;
         a.C0 = p.dWG; a.ldc0 = p.lddwg; a.C1 = p.dWU; a.ldc1 = p.lddwu;
-        if (const mg_status st = product(p, FORM_NN, END_STORE, a)) return st;
+        if (const hipError_t e = launch_linear(p.dtype, FORM_NN, END_STORE, a, room, room_bytes, p.stream)) return launched(e);
     }
     if (p.dWD != nullptr) {
         LinearArgs a{};
-        a.P = p.dY; a.ldp = p.lddy;
-        a.Q0 = static_cast<char *>(p.kept) + kept_scores(p.tokens, p.hidden); a.ldq0 = half;
+        left(a, dy);
+        gate(a, {static_cast<char *>(p.kept) + kept_scores(p.tokens, p.hidden), half, true});
         a.rows = width; a.cols = hidden; a.k = tokens;
         a.C0 = p.dWD; a.ldc0 = p.lddwd;
-        if (const mg_status st = product(p, FORM_NN, END_STORE, a)) return st;
+        if (const hipError_t e = launch_linear(p.dtype, FORM_NN, END_STORE, a, room, room_bytes, p.stream)) return launched(e);
     }
     return MG_OK;
 }
@@ -227,6 +295,8 @@ size_t gated_workspace(int dtype, int64_t tokens, int64_t width, int64_t hidden,
         ws.take(sgemm_room(tokens, width, hidden, backward));
     } else {
         ws.take(held_rows(tokens, hidden) * (backward ? 2 : 1));
+        ws.take(backward ? backward_room(tokens, width, hidden) : forward_room(tokens, width, hidden));
+        ws.take(copies_room(tokens, width, hidden, backward));
     }
     return ws.used;
 }

@@ -31,6 +31,7 @@ struct LinearArgs {
     int segment;                // 0, or where in the sum Q1 takes over (a multiple of 64; P has zeros between `lines` and it)
     int lines;                  // with `segment`: lines that Q0 and Q1 have
     int hidden;                 // END_GATED, END_GATED_GRAD
+    bool p_padded, q_padded;    // the operand has zeros up to a whole piece behind the sum's end
     int tiles_r, tiles_c;
     int k_per_slice;            // a multiple of 64; slice z of the sum starts at z * k_per_slice
     // results
@@ -61,10 +62,38 @@ __host__ __device__ inline int64_t kept_at(int64_t row, int64_t col, int64_t hid
 enum LinearForm { FORM_KK = 0, FORM_KN = 1, FORM_NN = 2 };       // both; P along, Q across; both across
 
 // dtype MG_F16 or MG_BF16.  The launches of operands at any address (any) and of operands whose rows start on 16 bytes (dma).
+enum LinearTile { LINEAR_256 = 0, LINEAR_128 = 1, LINEAR_64 = 2, LINEAR_ANY = -1 };      // of C, square; ANY: the kernel for operands at any address
+constexpr int linear_tile_size(int tile) { return tile == LINEAR_256 ? 256 : tile == LINEAR_128 ? 128 : 64; }
+// slices: of the sum, each from z * k_per_slice on
 hipError_t launch_linear_any(int dtype, int form, int end, LinearArgs args, int slices, hipStream_t stream);
+// dtype MG_F16 or MG_BF16, operands that linear_aligned() is true for
+hipError_t launch_linear_dma_kk_store(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
+hipError_t launch_linear_dma_kk_gated(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
+hipError_t launch_linear_dma_kk_scores(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
+hipError_t launch_linear_dma_kk_scores_grad(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
+hipError_t launch_linear_dma_kn_store(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
+hipError_t launch_linear_dma_kn_gated_grad(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
+hipError_t launch_linear_dma_nn_store(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
 
 // adds the slices of END_STORE and writes C in dtype
 hipError_t launch_linear_sum(int dtype, const LinearArgs &args, int slices, hipStream_t stream);
+
+// The product on the kernel that its plan (linear_plan.h) takes, `room` for slices of its sum; scores_columns, of END_SCORES: columns that one entry of args.scores stands for
+hipError_t launch_linear(int dtype, int form, int end, LinearArgs args, void *room, size_t room_bytes, hipStream_t stream, int *scores_columns = nullptr);
+// bytes of room with which a product of aligned operands takes its preferred number of slices
+size_t linear_room(int form, int end, int64_t rows, int64_t cols, int64_t k);
+
+// Copies of 16-bit matrices whose rows do not start on 16 bytes, or end inside a piece along a sum: rows x padded(cols), zeros behind the columns
+struct LinearCopies {
+    const void *from[6];
+    void *to[6];
+    int64_t ld[6];
+    int cols[6];
+    int64_t rows[6];
+    uint32_t begin[7];               // first work-group
+    int count;
+};
+hipError_t launch_linear_copies(LinearCopies copies, hipStream_t stream);
 
 // Memory of a workspace, handed out on 256 bytes; without a base it only counts
 struct Arena {

@@ -73,8 +73,7 @@ mg_status mg_gated_forward(int dtype, int activation, int64_t tokens, int64_t wi
     const bool empty = tokens == 0 || width == 0, sums = !empty && hidden > 0;
     if (!empty && (Y == nullptr || (sums && (X == nullptr || WG == nullptr || WU == nullptr || WD == nullptr)))) return MG_ERR_NULL;
     if (sums && type_known(dtype)) {
-        const size_t need = kept != nullptr && dtype != MG_F32 ? 0 : gated_workspace(dtype, tokens, width, hidden, false);
-        if (need > 0 && (!aligned(workspace) || workspace_bytes < need)) return MG_ERR_WORKSPACE;
+        if (!aligned(workspace) || workspace_bytes < gated_workspace(dtype, tokens, width, hidden, false)) return MG_ERR_WORKSPACE;
     }
     if (!type_known(dtype)) return MG_ERR_TYPE;
     if (!activation_known(activation)) return MG_ERR_ACTIVATION;
@@ -86,7 +85,7 @@ mg_status mg_gated_forward(int dtype, int activation, int64_t tokens, int64_t wi
     p.tokens = tokens; p.width = width; p.hidden = hidden;
     p.X = X; p.ldx = ldx; p.WG = WG; p.ldwg = ldwg; p.WU = WU; p.ldwu = ldwu; p.WD = WD; p.ldwd = ldwd;
     p.Y = Y; p.ldy = ldy; p.kept = kept;
-    p.workspace = arena(workspace, aligned(workspace) ? workspace_bytes : 0);
+    p.workspace = arena(workspace, workspace_bytes);
     p.stream = static_cast<hipStream_t>(stream);
     return gated_forward(p);
 }

@@ -1,0 +1,109 @@
+// Products of 16-bit matrices: the kernel that the plan takes, copies of operands, sums of slices.
+#include "linear_plan.h"
+#include "linear_end.h"
+
+namespace mg {
+namespace {
+
+// A thread moves a piece of eight elements.
+__global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
+{
+    int m = 0;
+    while (m + 1 < c.count && blockIdx.x >= c.begin[m + 1]) ++m;
+    const int64_t piece = (blockIdx.x - c.begin[m]) * int64_t(256) + threadIdx.x;
+    const int cols = c.cols[m], per_row = static_cast<int>(padded(cols) / 8);
+    const int64_t row = piece / per_row;
+    if (row >= c.rows[m]) return;
+    const int col = static_cast<int>(piece - row * per_row) * 8;
+    const uint16_t *from = static_cast<const uint16_t *>(c.from[m]) + row * c.ld[m] + col;
+    Piece<uint16_t, 8> x;
+    if (cols - col >= 8) {
+        x = *reinterpret_cast<const Piece<uint16_t, 8> *>(from);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x.v[e] = e < cols - col ? from[e] : uint16_t(0);
+    }
+    *reinterpret_cast<end_floatx4 *>(static_cast<uint16_t *>(c.to[m]) + row * padded(cols) + col) = __builtin_bit_cast(end_floatx4, x);
+}
+
+// C = the sum of the slices, in their order.  A work-group has 1024 elements of a row.
+template <typename T> __global__ __launch_bounds__(256) void linear_sum_kernel(const LinearArgs args, int slices)
+{
+    int64_t row = blockIdx.x;
+    const int col = (blockIdx.y * 256 + threadIdx.x) * 4;
+    if (col >= args.cols) return;
+    const float *from = args.partial + row * args.partial_ld + col;      // (partial_ld is a multiple of 64)
+    T *C = static_cast<T *>(args.C0);
+    int64_t ldc = args.ldc0;
+    if (args.second > 0) {
+        if (row >= args.second) {
+            C = static_cast<T *>(args.C1);
+            ldc = args.ldc1;
+            row -= args.second;
+        }
+        if (row >= args.rows0 || C == nullptr) return;
+    }
+    const float scale = args.scale == nullptr ? 1.f : *args.scale;
+    end_floatx4 sum = *reinterpret_cast<const end_floatx4 *>(from);
+    for (int s = 1; s < slices; ++s) sum += *reinterpret_cast<const end_floatx4 *>(from + s * args.partial_stride);
+    float out[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = sum[e] * scale;
+    store_piece<T, 4>(C + row * ldc + col, args.cols - col, out);
+}
+
+}  // namespace
+
+hipError_t launch_linear_copies(LinearCopies c, hipStream_t stream)
+{
+    if (c.count == 0) return hipSuccess;
+    c.begin[0] = 0;
+    for (int m = 0; m < c.count; ++m) c.begin[m + 1] = c.begin[m] + static_cast<uint32_t>(ceil_div(c.rows[m] * (padded(c.cols[m]) / 8), 256));
+    copy_kernel<<<c.begin[c.count], 256, 0, stream>>>(c);
+    return hipGetLastError();
+}
+
+hipError_t launch_linear_sum(int dtype, const LinearArgs &args, int slices, hipStream_t stream)
+{
+    const dim3 grid(static_cast<uint32_t>(args.rows), static_cast<uint32_t>(ceil_div(args.cols, 1024)));
+    if (dtype == MG_F16) linear_sum_kernel<_Float16><<<grid, 256, 0, stream>>>(args, slices);
+    else linear_sum_kernel<bfloat><<<grid, 256, 0, stream>>>(args, slices);
+    return hipGetLastError();
+}
+
+size_t linear_room(int form, int end, int64_t rows, int64_t cols, int64_t k)
+{
+    size_t most = 0;
+    for (const bool aligned : {true, false}) {
+        const int slices = linear_plan(form, end, rows, cols, k, aligned, ~size_t(0)).slices;
+        const size_t room = slices > 1 ? static_cast<size_t>(slices) * rows * padded(cols) * sizeof(float) : 0;
+        most = room > most ? room : most;
+    }
+    return most;
+}
+
+hipError_t launch_linear(int dtype, int form, int end, LinearArgs args, void *room, size_t room_bytes, hipStream_t stream, int *scores_columns)
+{
+    const LinearPlan how = linear_plan(form, end, args.rows, args.cols, args.k, linear_aligned(form, end, args), args.partial != nullptr || room == nullptr ? 0 : room_bytes);
+    const bool sliced = how.slices > 1;
+    if (sliced) {
+        args.partial = static_cast<float *>(room);
+        args.partial_ld = padded(args.cols);
+        args.partial_stride = args.rows * args.partial_ld;
+    }
+    args.k_per_slice = how.k_per_slice;
+    if (scores_columns != nullptr) *scores_columns = linear_tile_size(how.tile);
+    hipError_t e = hipErrorInvalidValue;
+    if (how.tile == LINEAR_ANY) e = launch_linear_any(dtype, form, end, args, how.slices, stream);
+    else if (form == FORM_KK && end == END_STORE) e = launch_linear_dma_kk_store(dtype, how.tile, args, how.slices, stream);
+    else if (form == FORM_KK && end == END_GATED) e = launch_linear_dma_kk_gated(dtype, how.tile, args, how.slices, stream);
+    else if (form == FORM_KK && end == END_SCORES) e = launch_linear_dma_kk_scores(dtype, how.tile, args, how.slices, stream);
+    else if (form == FORM_KK && end == END_SCORES_GRAD) e = launch_linear_dma_kk_scores_grad(dtype, how.tile, args, how.slices, stream);
+    else if (form == FORM_KN && end == END_STORE) e = launch_linear_dma_kn_store(dtype, how.tile, args, how.slices, stream);
+    else if (form == FORM_KN && end == END_GATED_GRAD) e = launch_linear_dma_kn_gated_grad(dtype, how.tile, args, how.slices, stream);
+    else if (form == FORM_NN && end == END_STORE) e = launch_linear_dma_nn_store(dtype, how.tile, args, how.slices, stream);
+    if (e != hipSuccess || !sliced) return e;
+    return launch_linear_sum(dtype, args, how.slices, stream);
+}
+
+}  // namespace mg

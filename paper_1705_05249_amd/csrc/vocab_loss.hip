@@ -80,29 +80,30 @@ __global__ __launch_bounds__(256) void join_scores_kernel(const float2 *scores, 
     loss[row] = target >= 0 && target < vocab ? total - target_score[row] : 0.f;
 }
 
-// FP16: scale[0] = the power of two with which the largest weight becomes at most 2^14 (dz is a probability times a weight: its largest then is a
-// quarter of the largest FP16 number, probabilities down to 2^-28 of the largest weight are normal numbers); scale[1]: its inverse
-__global__ __launch_bounds__(256) void weight_scale_kernel(const float *weights, int tokens, float *scale)
+// scale[0] = most / (the largest weight), scale[1] its inverse: what dz is multiplied with while it is an operand in 16 bits, and its products with afterwards.
+// Where all weights are alike, as in a mean, dz then is p - [target] itself, whose -1 of an unlikely target is exact (1 / count is not: off by up to half a
+// step in every token, where it is the largest part of dz).  FP16: most = 2^13, an eighth of the largest number; probabilities down to 2^-27 stay normal.
+__global__ __launch_bounds__(256) void weight_scale_kernel(const float *weights, int tokens, float most, float *scale)
 {
     __shared__ uint32_t parts[4];
-    uint32_t most = weights == nullptr ? 0x3f800000u : 0u;
+    uint32_t largest = weights == nullptr ? 0x3f800000u : 0u;
     if (weights != nullptr)
         for (int t = threadIdx.x; t < tokens; t += 256) {
             const uint32_t w = __builtin_bit_cast(uint32_t, weights[t]) & 0x7fffffffu;
-            most = w < 0x7f800000u && w > most ? w : most;
+            largest = w < 0x7f800000u && w > largest ? w : largest;
         }
     for (int d = 32; d > 0; d /= 2) {
-        const uint32_t other = __shfl_xor(most, d);
-        most = other > most ? other : most;
+        const uint32_t other = __shfl_xor(largest, d);
+        largest = other > largest ? other : largest;
     }
-    if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = most;
+    if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = largest;
     __syncthreads();
     if (threadIdx.x != 0) return;
-    for (int w = 1; w < 4; ++w) most = parts[w] > most ? parts[w] : most;
-    // both the scale and its inverse have to be normal numbers
-    const int e = static_cast<int>(most >> 23) - 127, up = 13 - e < -126 ? -126 : 13 - e > 126 ? 126 : 13 - e;
-    scale[0] = most == 0 ? 1.f : power_of_two(up);
-    scale[1] = most == 0 ? 1.f : power_of_two(-up);
+    for (int w = 1; w < 4; ++w) largest = parts[w] > largest ? parts[w] : largest;
+    // (weights beyond 2^100 either way: the scale and its inverse have to be normal numbers)
+    const float w = fminf(fmaxf(__builtin_bit_cast(float, largest), 0x1p-100f), 0x1p100f);
+    scale[0] = largest == 0 ? 1.f : most / w;
+    scale[1] = largest == 0 ? 1.f : w / most;
 }
 
 struct LossMemory {
@@ -133,6 +134,8 @@ struct LossGradMemory {
     float *scale;
     float *slices;
     int64_t slice;                         // elements of one
+    void *room;                            // 16 bits: for slices of a product
+    size_t room_bytes;
     size_t left;
     void *rest;
 };
@@ -144,7 +147,13 @@ LossGradMemory loss_grad_memory(Arena &ws, int dtype, int64_t tokens, int64_t wi
     m.scale = static_cast<float *>(ws.take(2 * F));
     m.dz = ws.take(tokens * padded(columns) * (dtype == MG_F32 ? 4 : 2));
     m.slice = tokens * padded(width);
-    if (dtype != MG_F32 && count > 1) m.slices = static_cast<float *>(ws.take(count * m.slice * F));
+    if (dtype != MG_F32) {
+        if (count > 1) m.slices = static_cast<float *>(ws.take(count * m.slice * F));
+        else m.room_bytes = linear_room(FORM_KN, END_STORE, tokens, width, columns);
+        const size_t other = linear_room(FORM_NN, END_STORE, columns, width, tokens);
+        m.room_bytes = other > m.room_bytes ? other : m.room_bytes;
+        m.room = ws.take(m.room_bytes);
+    }
     m.left = ws.left();
     m.rest = ws.take(0);
     return m;
@@ -208,56 +217,86 @@ mg_status grad_f32(const LossProblem &p, const LossGradMemory &m)
     return MG_OK;
 }
 
-mg_status product(const LossProblem &p, int form, int end, LinearArgs args)
+// The caller's matrices or copies of them (see Copies in gated.hip)
+struct LossOperands {
+    const void *X, *W;
+    int64_t ldx, ldw;
+    bool padded;
+};
+
+constexpr int64_t COPY_TOKENS = 128;
+size_t copies_room(int64_t tokens, int64_t width, int64_t vocab) { return width % 8 != 0 && tokens >= COPY_TOKENS ? static_cast<size_t>((tokens + vocab) * padded(width)) * 2 + 512 : 0; }
+
+hipError_t loss_operands(const LossProblem &p, Arena &ws, LossOperands &o)
 {
-    args.k_per_slice = static_cast<int>(padded(args.k));
-    return launched(launch_linear_any(p.dtype, form, end, args, 1, p.stream));
+    LinearCopies list{};
+    o = {p.X, p.W, p.ldx, p.ldw, false};
+    const bool whole = p.width % 8 == 0;
+    bool copied[2] = {false, false};
+    for (int n = 0; n < 2; ++n) {
+        const void *&at = n == 0 ? o.X : o.W;
+        int64_t &ld = n == 0 ? o.ldx : o.ldw;
+        const int64_t rows = n == 0 ? p.tokens : p.vocab;
+        const size_t bytes = static_cast<size_t>(rows * padded(p.width)) * 2;
+        if ((whole && reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 8 == 0) || p.tokens < COPY_TOKENS || ws.left() < bytes) continue;
+        const int m = list.count++;
+        list.from[m] = at; list.to[m] = ws.take(bytes); list.ld[m] = ld; list.rows[m] = rows; list.cols[m] = static_cast<int>(p.width);
+        at = list.to[m];
+        ld = padded(p.width);
+        copied[n] = true;
+    }
+    o.padded = copied[0] && copied[1];
+    return launch_linear_copies(list, p.stream);
 }
 
-LinearArgs logits(const LossProblem &p, int64_t first, int64_t columns)
+LinearArgs logits(const LossProblem &p, const LossOperands &o, int64_t first, int64_t columns)
 {
     LinearArgs a{};
-    a.P = p.X; a.ldp = p.ldx;
-    a.Q0 = static_cast<const uint16_t *>(p.W) + first * p.ldw; a.ldq0 = p.ldw;
+    a.P = o.X; a.ldp = o.ldx; a.p_padded = a.q_padded = o.padded;
+    a.Q0 = static_cast<const uint16_t *>(o.W) + first * o.ldw; a.ldq0 = o.ldw;
     a.rows = static_cast<int>(p.tokens); a.cols = static_cast<int>(columns); a.k = static_cast<int>(p.width);
     a.first = first; a.vocab = p.vocab; a.targets = p.targets;
     return a;
 }
 
-mg_status grad_16(const LossProblem &p, const LossGradMemory &m)
+mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
 {
-    if (p.dtype == MG_F16) {
-        weight_scale_kernel<<<1, 256, 0, p.stream>>>(p.weights, static_cast<int>(p.tokens), m.scale);
+    LossOperands o;
+    if (const hipError_t e = loss_operands(p, ws, o)) return launched(e);
+    const float *scale = nullptr;
+    if (p.weights != nullptr || p.dtype == MG_F16) {
+        weight_scale_kernel<<<1, 256, 0, p.stream>>>(p.weights, static_cast<int>(p.tokens), p.dtype == MG_F16 ? 8192.f : 1.f, m.scale);
         if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
+        scale = m.scale;
     }
     const int64_t columns = piece_columns(p.dtype, p.tokens, p.vocab), lead = padded(columns);
     const int count = static_cast<int>(ceil_div(p.vocab, columns));
     LinearArgs x{};                                        // dX
-    x.P = m.dz; x.ldp = lead; x.ldq0 = p.ldw;
+    x.P = m.dz; x.ldp = lead; x.p_padded = true; x.ldq0 = o.ldw;
     x.rows = static_cast<int>(p.tokens); x.cols = static_cast<int>(p.width);
     x.C0 = p.dX; x.ldc0 = p.lddx;
-    x.scale = p.dtype == MG_F16 ? m.scale + 1 : nullptr;
+    x.scale = scale == nullptr ? nullptr : scale + 1;
     x.partial_ld = padded(p.width);
     x.partial_stride = m.slice;
     for (int64_t first = 0, n = 0; first < p.vocab; first += columns, ++n) {
         const int64_t some = p.vocab - first < columns ? p.vocab - first : columns;
-        LinearArgs z = logits(p, first, some);
-        z.lse = p.lse; z.weights = p.weights; z.weight_scale = p.dtype == MG_F16 ? m.scale : nullptr;
+        LinearArgs z = logits(p, o, first, some);
+        z.lse = p.lse; z.weights = p.weights; z.weight_scale = scale;
         z.C0 = m.dz; z.ldc0 = lead;
-        if (const mg_status st = product(p, FORM_KK, END_SCORES_GRAD, z)) return st;
+        if (const hipError_t e = launch_linear(p.dtype, FORM_KK, END_SCORES_GRAD, z, nullptr, 0, p.stream)) return launched(e);
         if (p.dX != nullptr) {
             x.Q0 = z.Q0;
             x.k = static_cast<int>(some);
             x.partial = count > 1 ? m.slices + n * m.slice : nullptr;
-            if (const mg_status st = product(p, FORM_KN, END_STORE, x)) return st;
+            if (const hipError_t e = launch_linear(p.dtype, FORM_KN, END_STORE, x, m.room, m.room_bytes, p.stream)) return launched(e);
         }
         if (p.dW != nullptr) {
             LinearArgs w{};
-            w.P = m.dz; w.ldp = lead; w.Q0 = p.X; w.ldq0 = p.ldx;
+            w.P = m.dz; w.ldp = lead; w.Q0 = o.X; w.ldq0 = o.ldx;
             w.rows = static_cast<int>(some); w.cols = static_cast<int>(p.width); w.k = static_cast<int>(p.tokens);
             w.C0 = static_cast<uint16_t *>(p.dW) + first * p.lddw; w.ldc0 = p.lddw;
             w.scale = x.scale;
-            if (const mg_status st = product(p, FORM_NN, END_STORE, w)) return st;
+            if (const hipError_t e = launch_linear(p.dtype, FORM_NN, END_STORE, w, m.room, m.room_bytes, p.stream)) return launched(e);
         }
     }
     if (p.dX != nullptr && count > 1) {
@@ -274,7 +313,7 @@ size_t loss_workspace(int dtype, int64_t tokens, int64_t width, int64_t vocab, b
     Arena ws{nullptr, 0, 0};
     if (gradient) loss_grad_memory(ws, dtype, tokens, width, vocab);
     else loss_memory(ws, dtype, tokens, vocab);
-    if (dtype == MG_F32 && vocab > 0) ws.take(sgemm_room(tokens, width, vocab, gradient));
+    if (vocab > 0) ws.take(dtype == MG_F32 ? sgemm_room(tokens, width, vocab, gradient) : copies_room(tokens, width, vocab));
     return ws.used;
 }
 
@@ -287,11 +326,14 @@ mg_status vocab_loss(const LossProblem &p)
         if (const mg_status st = loss_f32(p, m)) return st;
         tiles = static_cast<int>(ceil_div(p.vocab, piece_columns(MG_F32, p.tokens, p.vocab)));
     } else if (p.vocab > 0) {
-        LinearArgs a = logits(p, 0, p.vocab);
+        LossOperands o;
+        if (const hipError_t e = loss_operands(p, ws, o)) return launched(e);
+        LinearArgs a = logits(p, o, 0, p.vocab);
         a.scores = m.scores;
         a.target_score = m.target_score;
-        if (const mg_status st = product(p, FORM_KK, END_SCORES, a)) return st;
-        tiles = static_cast<int>(ceil_div(p.vocab, 64));
+        int columns = 0;
+        if (const hipError_t e = launch_linear(p.dtype, FORM_KK, END_SCORES, a, nullptr, 0, p.stream, &columns)) return launched(e);
+        tiles = static_cast<int>(ceil_div(p.vocab, columns));
     }
     join_scores_kernel<<<static_cast<uint32_t>(ceil_div(p.tokens, 16)), 256, 0, p.stream>>>(m.scores, tiles, static_cast<int>(p.tokens), p.vocab, p.targets, m.target_score, p.loss, p.lse);
     return launched(hipGetLastError());
@@ -301,7 +343,7 @@ mg_status vocab_loss_grad(const LossProblem &p)
 {
     Arena ws = p.workspace;
     const LossGradMemory m = loss_grad_memory(ws, p.dtype, p.tokens, p.width, p.vocab);
-    return p.dtype == MG_F32 ? grad_f32(p, m) : grad_16(p, m);
+    return p.dtype == MG_F32 ? grad_f32(p, m) : grad_16(p, m, ws);
 }
 
 }  // namespace mg

@@ -1,0 +1,62 @@
+"""The direct-to-LDS kernels of the dense layers that are built: those that some call reaches, each once; none touches a register that an LDS read is still to
+write (see test_reads_in_flight.py)."""
+import re
+import struct
+
+from paper_1705_05249_amd import gemm as G
+from tests import test_reads_in_flight as T
+
+KK, KN, NN = range(3)
+STORE, GATED, GATED_GRAD, SCORES, SCORES_GRAD = range(5)
+NAME = re.compile(rb"_ZN2mg(?:12_GLOBAL__N_1)?17linear_(dma|any)_kernelI([\w]+?)EEvNS_?\w*?Args")
+PAIRS = {(KK, STORE), (KK, GATED), (KK, SCORES), (KK, SCORES_GRAD), (KN, STORE), (KN, GATED_GRAD), (NN, STORE)}
+
+
+def code_objects():
+    data, at = open(G.LIB_PATH, "rb").read(), 0
+    while (at := data.find(T.MAGIC, at)) >= 0:
+        p = at + len(T.MAGIC) + 8
+        for _ in range(struct.unpack_from("<Q", data, at + len(T.MAGIC))[0]):
+            offset, size, length = struct.unpack_from("<QQQ", data, p)
+            target, p = data[p + 24: p + 24 + length], p + 24 + length
+            if b"gfx950" in target:
+                yield data[at + offset: at + offset + size]
+        at += 1
+
+
+def built(kind):
+    """(bfloat16, numbers) of the kernels of a kind"""
+    found = set()
+    for code in code_objects():
+        for name, arguments in NAME.findall(code):
+            if name.decode() == kind:
+                found.add((arguments.startswith(b"DF16b"), *(int(v) for v in re.findall(rb"Li(\d+)E?", arguments))))
+    return found
+
+
+def dma():
+    tiles = {(256, 256, 2, 4, 2), (128, 128, 2, 2, 2), (64, 64, 2, 2, 4)}
+    return {(kind, *pair, *tile) for kind in (False, True) for pair in PAIRS for tile in tiles}
+
+
+def test_kernels_that_are_built():
+    assert built("dma") == dma()
+    assert built("any") == {(kind, *pair) for kind in (False, True) for pair in PAIRS}
+
+
+def test_every_hand_waited_kernel_is_looked_over(tmp_path, monkeypatch):
+    monkeypatch.setattr(T, "KERNEL", re.compile(r"^[0-9a-f]+ <(_ZN2mg17linear_dma_kernelI\w+EvNS_10LinearArgsE)>:$"))
+    seen, wrong = set(), {}
+    for n, code in enumerate(code_objects()):
+        if b"linear_dma_kernel" not in code:
+            continue
+        path = tmp_path / f"{n}.co"
+        path.write_bytes(code)
+        for name, body in T.kernels(str(path)):
+            reads, touched = T.touched_in_flight(body)
+            if reads > 0:
+                seen.add((name.startswith("_ZN2mg17linear_dma_kernelIDF16b"), *(int(v) for v in re.findall(r"Li(\d+)E", name))))
+            if touched:
+                wrong[name] = sorted(touched)[:4]
+    assert seen == dma()
+    assert not wrong, wrong
