@@ -61,11 +61,17 @@ __host__ __device__ inline int64_t kept_at(int64_t row, int64_t col, int64_t hid
 // Which of P and Q lie along the sum
 enum LinearForm { FORM_KK = 0, FORM_KN = 1, FORM_NN = 2 };       // both; P along, Q across; both across
 
-// dtype MG_F16 or MG_BF16.  The launches of operands at any address (any) and of operands whose rows start on 16 bytes (dma).
-enum LinearTile { LINEAR_256 = 0, LINEAR_128 = 1, LINEAR_64 = 2, LINEAR_ANY = -1 };      // of C, square; ANY: the kernel for operands at any address
-constexpr int linear_tile_size(int tile) { return tile == LINEAR_256 ? 256 : tile == LINEAR_128 ? 128 : 64; }
+// Tiles of C, square; ANY: the kernel for operands at any address.  128_DEEP: four K-tiles in LDS instead of two, for launches that leave a compute unit one
+// work-group (2048^3: 30.2 -> 21.7 us; with two work-groups to a compute unit the other one is ahead, 4096 x 4096 x 2048: 72 against 82).
+enum LinearTile { LINEAR_256 = 0, LINEAR_128 = 1, LINEAR_64 = 2, LINEAR_128_DEEP = 3, LINEAR_FEW = 4, LINEAR_ANY = -1, LINEAR_ANY_FEW = -2 };
+constexpr int linear_tile_size(int tile) { return tile == LINEAR_256 ? 256 : tile == LINEAR_128 || tile == LINEAR_128_DEEP ? 128 : 64; }
 // slices: of the sum, each from z * k_per_slice on
 hipError_t launch_linear_any(int dtype, int form, int end, LinearArgs args, int slices, hipStream_t stream);
+// FORM_KK, few rows of P, operands at any address or on 16 bytes; columns that a work-group has there
+hipError_t launch_linear_few_any(int dtype, int end, const LinearArgs &args, hipStream_t stream);
+hipError_t launch_linear_few_dma(int dtype, int end, const LinearArgs &args, hipStream_t stream);
+constexpr int linear_few_columns(int end) { return end == END_SCORES ? 64 : end == END_GATED ? 32 : 16; }
+constexpr int LINEAR_FEW_ROWS = 32;
 // dtype MG_F16 or MG_BF16, operands that linear_aligned() is true for
 hipError_t launch_linear_dma_kk_store(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
 hipError_t launch_linear_dma_kk_gated(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);

@@ -92,9 +92,11 @@ hipError_t launch_linear(int dtype, int form, int end, LinearArgs args, void *ro
         args.partial_stride = args.rows * args.partial_ld;
     }
     args.k_per_slice = how.k_per_slice;
-    if (scores_columns != nullptr) *scores_columns = linear_tile_size(how.tile);
+    if (scores_columns != nullptr) *scores_columns = how.tile == LINEAR_FEW || how.tile == LINEAR_ANY_FEW ? linear_few_columns(end) : linear_tile_size(how.tile);
     hipError_t e = hipErrorInvalidValue;
     if (how.tile == LINEAR_ANY) e = launch_linear_any(dtype, form, end, args, how.slices, stream);
+    else if (how.tile == LINEAR_FEW) e = launch_linear_few_dma(dtype, end, args, stream);
+    else if (how.tile == LINEAR_ANY_FEW) e = launch_linear_few_any(dtype, end, args, stream);
     else if (form == FORM_KK && end == END_STORE) e = launch_linear_dma_kk_store(dtype, how.tile, args, how.slices, stream);
     else if (form == FORM_KK && end == END_GATED) e = launch_linear_dma_kk_gated(dtype, how.tile, args, how.slices, stream);
     else if (form == FORM_KK && end == END_SCORES) e = launch_linear_dma_kk_scores(dtype, how.tile, args, how.slices, stream);

@@ -134,7 +134,7 @@ __device__ inline float2 join_scores(float2 a, float2 b)
     return make_float2(m, a.y * exp_fast(a.x - from) + b.y * exp_fast(b.x - from));
 }
 
-// All wavefronts of the work-group come here, and nobody uses the LDS any more.  The wavefront's tile starts at (row0, col0) and is wavefront
+// All WR x WC wavefronts that share a tile come here, and nobody uses the LDS any more.  The wavefront's tile starts at (row0, col0) and is wavefront
 // (wr, wc) of WR x WC; region: its own; shared: WR * FN * 16 * WC float2 that no region overlaps (END_SCORES).
 template <typename T, int END, int FM, int FN, int WR, int WC>
 __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (&acc)[FN][FM], char *region, float2 *shared, int tile_row, int tile_col, int wr, int wc, int lane)
@@ -204,8 +204,9 @@ __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (
             s += __shfl_xor(s, 32);
             if (lane < 16) shared[wc * (WR * FN * 16) + wr * FN * 16 + 16 * j + lane] = make_float2(m, s);
         }
-        __syncthreads();
-        for (int r = threadIdx.x; r < WR * FN * 16; r += WR * WC * 64) {
+        if constexpr (WR * WC == 1) end_fence();
+        else __syncthreads();
+        for (int r = (wr * WC + wc) * 64 + lane; r < WR * FN * 16; r += WR * WC * 64) {
             if (tile_row + r >= args.rows) continue;
             float2 all = shared[r];
 #pragma unroll

@@ -11,20 +11,28 @@ struct LinearPlan {
     int slices, k_per_slice;
 };
 
-// What a tile takes, in us: `alone` for 64 values of the sum while a compute unit has one of its tiles, with n of them n * `each`; around the sum `start`, and
-// `more` for every round of tiles (C leaves).
+// What a tile takes, in us, measured with random bfloat16 operands: `alone` for 64 values of the sum while a compute unit has one of its tiles, with n of them
+// n * `each`; around the sum `start`, and `more` for every tile of a compute unit (C leaves).  Along / across the sum costs more reads of LDS (`form`).
+// Estimated and measured: 2048^3 on 128_DEEP 23 and 21.7, 4096 x 4096 x 2048 on 256 60 and 58, on 128 74 and 72, 8192 x 8192 x 512 on 256 79 and 84,
+// 8192 x 1024 x 1024 on 128 22 and 21.5, 512 x 2048 x 2048 on 64 11.6 and 10.9, 333 x 1001 x 1999 on 64 11.1 and 10.5.
 struct LinearCost {
     double alone, each, start, more;
 };
 inline LinearCost linear_cost(int tile, int form)
 {
-    (void)form;
+    LinearCost c{};
+    double across = 1;                     // FORM_NN; half as much more for FORM_KN
     switch (tile) {
-        case LINEAR_256: return {1.5, 1.65, 4, 6};
-        case LINEAR_128: return {0.6, 0.5, 3, 2};
-        case LINEAR_64: return {0.3, 0.17, 3, 1};
-        default: return {0.5, 0.35, 3, 1.5};
+        case LINEAR_256: c = {1.48, 1.55, 4, 6.5}; across = 1.12; break;
+        case LINEAR_128: c = {0.82, 0.5, 3, 1.6}; across = 1.08; break;
+        case LINEAR_128_DEEP: c = {0.55, 0.58, 2.5, 2}; across = 1.08; break;
+        case LINEAR_64: c = {0.3, 0.21, 1.5, 0.5}; across = 1.2; break;
+        default: c = {0.5, 0.35, 3, 1.5}; across = 1.5; break;
     }
+    const double factor = form == FORM_NN ? across : form == FORM_KN ? (1 + across) / 2 : 1;
+    c.alone *= factor;
+    c.each *= factor;
+    return c;
 }
 
 // The least of the estimates.  Slices cost a launch that reads what they wrote; no slice gets fewer than four pieces of 64.
@@ -33,7 +41,14 @@ inline LinearPlan linear_plan(int form, int end, int64_t rows, int64_t cols, int
     LinearPlan best{LINEAR_ANY, 1, static_cast<int>(padded(k > 0 ? k : 1))};
     const double pieces = static_cast<double>(ceil_div(k > 0 ? k : 1, LAYER_PIECE)), one = static_cast<double>(rows) * padded(cols) * 4;
     double least = 0;
-    for (const int tile : {int(LINEAR_256), int(LINEAR_128), int(LINEAR_64), int(LINEAR_ANY)}) {
+    if (form == FORM_KK && end != END_SCORES_GRAD && rows <= LINEAR_FEW_ROWS) {
+        // Few rows: whatever the other sizes.  One row, 4096 x 8192: 14.6 us, 64 x 64 tiles in four slices 12.2 and 4.5 for their sum; 24 rows: 2048 x 4096 6.7 and 10.2,
+        // gate and up weights of 4096 x 2048 8.0 and 12.8; 8 rows, 512 x 8192: 7.1 and 12.8.  One row, gate and up weights of 8192 x 4096, out of the last-level cache 25 and
+        // 21.5, but out of memory, where a model of some layers has them, a block's call takes 41 us and 49 with the tiles in it.
+        best.tile = aligned ? LINEAR_FEW : LINEAR_ANY_FEW;
+        return best;
+    }
+    for (const int tile : {int(LINEAR_256), int(LINEAR_128), int(LINEAR_128_DEEP), int(LINEAR_64), int(LINEAR_ANY)}) {
         if (aligned != (tile != LINEAR_ANY)) continue;
         const int64_t size = linear_tile_size(tile), tiles = ceil_div(rows, size) * ceil_div(cols, size);
         const LinearCost c = linear_cost(tile, form);

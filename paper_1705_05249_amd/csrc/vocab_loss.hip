@@ -11,12 +11,12 @@ namespace mg {
 namespace {
 
 constexpr int64_t F = sizeof(float);
-constexpr int64_t PIECE_ELEMENTS = int64_t(1) << 27;              // of dz in 16 bits (256 MB, what the last-level cache holds); FP32: logits, half as many
+constexpr int64_t PIECE_ELEMENTS = int64_t(1) << 28;              // of dz in 16 bits; FP32: logits, a quarter as many
 
 // columns of a piece: a multiple of 256, or the vocabulary
 int64_t piece_columns(int dtype, int64_t tokens, int64_t vocab)
 {
-    const int64_t most = (dtype == MG_F32 ? PIECE_ELEMENTS / 2 : PIECE_ELEMENTS) / tokens / 256 * 256;
+    const int64_t most = (dtype == MG_F32 ? PIECE_ELEMENTS / 4 : PIECE_ELEMENTS) / tokens / 256 * 256;
     const int64_t columns = most < 256 ? 256 : most;
     return columns < vocab ? columns : vocab;
 }
@@ -61,19 +61,22 @@ __global__ __launch_bounds__(256) void scores_grad_kernel(float *Z, int64_t ldz,
     for (int c = threadIdx.x; c < cols; c += 256) z[c] = w != 0.f ? w * (expf(z[c] - l) - (first + c == target ? 1.f : 0.f)) : 0.f;
 }
 
-// 16 tokens a work-group, 16 lanes a token: joins the tiles' scores in a fixed order
-__global__ __launch_bounds__(256) void join_scores_kernel(const float2 *scores, int tiles, int tokens, int64_t vocab, const int64_t *targets, const float *target_score, float *loss,
-                                                          float *lse)
+// Joins the tiles' scores in a fixed order: TOKENS tokens a work-group, 256 / TOKENS lanes a token.
+template <int TOKENS> __global__ __launch_bounds__(256) void join_scores_kernel(const float2 *scores, int tiles, int tokens, int64_t vocab, const int64_t *targets, const float *target_score,
+                                                                                float *loss, float *lse)
 {
-    const int row = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
+    constexpr int LANES = 256 / TOKENS;
+    const int row = blockIdx.x * TOKENS + threadIdx.x % TOKENS, part = threadIdx.x / TOKENS;
     __shared__ float2 parts[256];
     float2 all = make_float2(-__builtin_inff(), 0.f);
     if (row < tokens)
-        for (int t = part; t < tiles; t += 16) all = join_scores(all, scores[static_cast<int64_t>(t) * tokens + row]);
+        for (int t = part; t < tiles; t += LANES) all = join_scores(all, scores[static_cast<int64_t>(t) * tokens + row]);
     parts[threadIdx.x] = all;
-    __syncthreads();
+    for (int d = LANES / 2; d > 0; d /= 2) {
+        __syncthreads();
+        if (part < d) parts[threadIdx.x] = all = join_scores(all, parts[threadIdx.x + d * TOKENS]);
+    }
     if (part != 0 || row >= tokens) return;
-    for (int p = 1; p < 16; ++p) all = join_scores(all, parts[16 * p + threadIdx.x]);
     const float total = all.x + logf(all.y);
     const int64_t target = targets[row];
     lse[row] = total;
@@ -83,12 +86,12 @@ __global__ __launch_bounds__(256) void join_scores_kernel(const float2 *scores, 
 // scale[0] = most / (the largest weight), scale[1] its inverse: what dz is multiplied with while it is an operand in 16 bits, and its products with afterwards.
 // Where all weights are alike, as in a mean, dz then is p - [target] itself, whose -1 of an unlikely target is exact (1 / count is not: off by up to half a
 // step in every token, where it is the largest part of dz).  FP16: most = 2^13, an eighth of the largest number; probabilities down to 2^-27 stay normal.
-__global__ __launch_bounds__(256) void weight_scale_kernel(const float *weights, int tokens, float most, float *scale)
+__global__ __launch_bounds__(1024) void weight_scale_kernel(const float *weights, int tokens, float most, float *scale)
 {
-    __shared__ uint32_t parts[4];
+    __shared__ uint32_t parts[16];
     uint32_t largest = weights == nullptr ? 0x3f800000u : 0u;
     if (weights != nullptr)
-        for (int t = threadIdx.x; t < tokens; t += 256) {
+        for (int t = threadIdx.x; t < tokens; t += 1024) {
             const uint32_t w = __builtin_bit_cast(uint32_t, weights[t]) & 0x7fffffffu;
             largest = w < 0x7f800000u && w > largest ? w : largest;
         }
@@ -99,7 +102,7 @@ __global__ __launch_bounds__(256) void weight_scale_kernel(const float *weights,
     if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = largest;
     __syncthreads();
     if (threadIdx.x != 0) return;
-    for (int w = 1; w < 4; ++w) largest = parts[w] > largest ? parts[w] : largest;
+    for (int w = 1; w < 16; ++w) largest = parts[w] > largest ? parts[w] : largest;
     // (weights beyond 2^100 either way: the scale and its inverse have to be normal numbers)
     const float w = fminf(fmaxf(__builtin_bit_cast(float, largest), 0x1p-100f), 0x1p100f);
     scale[0] = largest == 0 ? 1.f : most / w;
@@ -265,7 +268,7 @@ mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
     if (const hipError_t e = loss_operands(p, ws, o)) return launched(e);
     const float *scale = nullptr;
     if (p.weights != nullptr || p.dtype == MG_F16) {
-        weight_scale_kernel<<<1, 256, 0, p.stream>>>(p.weights, static_cast<int>(p.tokens), p.dtype == MG_F16 ? 8192.f : 1.f, m.scale);
+        weight_scale_kernel<<<1, 1024, 0, p.stream>>>(p.weights, static_cast<int>(p.tokens), p.dtype == MG_F16 ? 8192.f : 1.f, m.scale);
         if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
         scale = m.scale;
     }
@@ -335,7 +338,14 @@ mg_status vocab_loss(const LossProblem &p)
         if (const hipError_t e = launch_linear(p.dtype, FORM_KK, END_SCORES, a, nullptr, 0, p.stream, &columns)) return launched(e);
         tiles = static_cast<int>(ceil_div(p.vocab, columns));
     }
-    join_scores_kernel<<<static_cast<uint32_t>(ceil_div(p.tokens, 16)), 256, 0, p.stream>>>(m.scores, tiles, static_cast<int>(p.tokens), p.vocab, p.targets, m.target_score, p.loss, p.lse);
+    auto join = [&](auto each) {
+        constexpr int TOKENS = decltype(each)::value;
+        join_scores_kernel<TOKENS><<<static_cast<uint32_t>(ceil_div(p.tokens, TOKENS)), 256, 0, p.stream>>>(m.scores, tiles, static_cast<int>(p.tokens), p.vocab, p.targets, m.target_score, p.loss,
+                                                                                                          p.lse);
+    };
+    // (few tokens: a work-group each, 16 tokens of 512 tiles 11.9 us otherwise)
+    if (p.tokens <= 512) join(std::integral_constant<int, 1>{});
+    else join(std::integral_constant<int, 16>{});
     return launched(hipGetLastError());
 }
 

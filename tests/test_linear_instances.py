@@ -3,6 +3,8 @@ write (see test_reads_in_flight.py)."""
 import re
 import struct
 
+import pytest
+
 from paper_1705_05249_amd import gemm as G
 from tests import test_reads_in_flight as T
 
@@ -35,7 +37,7 @@ def built(kind):
 
 
 def dma():
-    tiles = {(256, 256, 2, 4, 2), (128, 128, 2, 2, 2), (64, 64, 2, 2, 4)}
+    tiles = {(256, 256, 2, 4, 2), (128, 128, 2, 2, 2), (128, 128, 2, 2, 4), (64, 64, 2, 2, 4)}
     return {(kind, *pair, *tile) for kind in (False, True) for pair in PAIRS for tile in tiles}
 
 
@@ -44,19 +46,26 @@ def test_kernels_that_are_built():
     assert built("any") == {(kind, *pair) for kind in (False, True) for pair in PAIRS}
 
 
-def test_every_hand_waited_kernel_is_looked_over(tmp_path, monkeypatch):
-    monkeypatch.setattr(T, "KERNEL", re.compile(r"^[0-9a-f]+ <(_ZN2mg17linear_dma_kernelI\w+EvNS_10LinearArgsE)>:$"))
+def few():
+    """bfloat16, end, blocks of 16 columns and rows, wavefronts, stages, weights pass the caches by"""
+    kernels = {(STORE, 1, 1, 8, 4), (STORE, 1, 2, 8, 3), (GATED, 2, 1, 4, 2), (GATED, 2, 2, 4, 3), (SCORES, 4, 1, 4, 2), (SCORES, 4, 2, 4, 3)}
+    return {(kind, *kernel, once) for kind in (False, True) for kernel in kernels for once in (0, 1)}
+
+
+@pytest.mark.parametrize("start,wanted", [("_ZN2mg17linear_dma_kernelI", dma), ("_ZN2mg12_GLOBAL__N_121linear_few_dma_kernelI", few)])
+def test_every_hand_waited_kernel_is_looked_over(tmp_path, monkeypatch, start, wanted):
+    monkeypatch.setattr(T, "KERNEL", re.compile(r"^[0-9a-f]+ <(" + start + r"\w+E+vNS\w*?10LinearArgsE)>:$"))
     seen, wrong = set(), {}
     for n, code in enumerate(code_objects()):
-        if b"linear_dma_kernel" not in code:
+        if start.encode() not in code:
             continue
         path = tmp_path / f"{n}.co"
         path.write_bytes(code)
         for name, body in T.kernels(str(path)):
             reads, touched = T.touched_in_flight(body)
             if reads > 0:
-                seen.add((name.startswith("_ZN2mg17linear_dma_kernelIDF16b"), *(int(v) for v in re.findall(r"Li(\d+)E", name))))
+                seen.add((name.startswith(start + "DF16b"), *(int(v) for v in re.findall(r"L[ib](\d+)E", name))))
             if touched:
                 wrong[name] = sorted(touched)[:4]
-    assert seen == dma()
+    assert seen == wanted()
     assert not wrong, wrong
