@@ -107,12 +107,12 @@ def loss(x, w, targets, dtype, weights=None, gradient=False):
     weights = torch.ones_like(lse) if weights is None else weights.double()
     wt = torch.where(counts, weights, 0.0)[:, None]
     here = torch.zeros_like(z)
-    here[torch.arange(len(targets)), at] = 1.0
+    here[torch.arange(len(targets), device=z.device), at] = 1.0
     dz = wt * (p - here)
     # (the lse that the gradient is given was rounded to FP32 and is off as above)
     ep = p * (ez + elog[:, None] + STEP * (3 + far)) * 1.01 + 2 * STEP * (p + here)
     edz = wt.abs() * ep + 4 * STEP * dz.abs()
-    largest = weights.abs().max() if weights.numel() else torch.tensor(1.0)
+    largest = weights.abs().max()
     edz = edz + HALF[dtype] * (dz.abs() + edz) + TINY[dtype] * largest * 2.0 ** -13 * (wt != 0)
     dx, dw = product(dz, edz, w, zero(w)), product(dz.T, edz.T, x, zero(x))
     pieces = 2 * STEP * (1 + vocab // 256)                         # pieces of the vocabulary are added in FP32
@@ -124,7 +124,7 @@ def loss(x, w, targets, dtype, weights=None, gradient=False):
 def check(got, want, name):
     """got (on any device) is within its bound"""
     value, bound = want
-    got = got.double().cpu()
+    got = got.to(value.device).double()
     assert got.shape == value.shape, (name, got.shape, value.shape)
     if not got.numel():
         return

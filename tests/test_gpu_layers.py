@@ -65,7 +65,8 @@ def run_block(case, act, dtype, lead=0, extra=0, keep=True, backward=True, wante
     code, kind = CODES[dtype], D.ACTIVATIONS[act]
     x, wg, wu, wd, dy = (t.to(dtype) for t in (normal(1, tokens, width), normal(2, hidden, width, sigma=width ** -0.5), normal(3, hidden, width, sigma=width ** -0.5),
                                                 normal(4, width, hidden, sigma=hidden ** -0.5), normal(5, tokens, width)))
-    want = R.block(x, wg, wu, wd, act, dtype, dy)
+    where = "cuda" if tokens * width * hidden > 1 << 24 else "cpu"
+    want = R.block(*(t.to(where) for t in (x, wg, wu, wd)), act, dtype, dy.to(where))
     held = [Held(t, lead, extra) for t in (x, wg, wu, wd)]
     arguments = [v for h in held for v in h.at()]
     y = result(tokens, width, dtype, lead, extra)
@@ -153,7 +154,8 @@ def run_loss(case, dtype, lead=0, extra=0, weights="each", ignored=0.3, wanted=(
     targets[out] = torch.tensor([-100, -1, vocab, 1 << 40, -(1 << 33)])[torch.arange(tokens) % 5][out]
     token_weights = {"each": torch.rand(tokens, generator=gen) * 2 - 0.5, "mean": torch.full((tokens,), 1.0 / 7001), "none": None, "large": torch.full((tokens,), 1024.0),
                      "zeros": torch.where(torch.arange(tokens) % 2 == 0, 0.0, 1.0)}[weights]
-    want = R.loss(x, w, targets, dtype, token_weights, gradient=True)
+    where = "cuda" if tokens * width * vocab > 1 << 24 else "cpu"
+    want = R.loss(x.to(where), w.to(where), targets.to(where), dtype, None if token_weights is None else token_weights.to(where), gradient=True)
     held = [Held(t, lead, extra) for t in (x, w)]
     arguments = [v for h in held for v in h.at()]
     target = targets.cuda()
@@ -244,6 +246,27 @@ def test_tokens_that_do_not_count_may_hold_anything():
         fine[[3, 5, 6]] = False
         assert bool(loss.cpu()[fine].isfinite().all()) and float(loss[3]) == 0.0
         assert bool(dx.cpu()[fine].isfinite().all()) and not bool(dx[[3, 5, 6]].any())
+
+
+# sizes at which the large tiles are taken (tests/test_linear_plan.py says which by which product)
+LARGE_BLOCKS = [(3999, 520, 4000), (4000, 4008, 520), (520, 4000, 2000), (3970, 515, 4001), (1500, 1032, 1000)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("case", LARGE_BLOCKS, ids=lambda c: "x".join(map(str, c)))
+def test_large_blocks(case, dtype):
+    say("block", case, dtype)
+    run_block(case, R.ACTS[sum(case) % 4], KINDS[dtype])
+
+
+LARGE_LOSSES = [(4000, 520, 4000), (3970, 515, 4061), (1111, 1032, 2100)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("case", LARGE_LOSSES, ids=lambda c: "x".join(map(str, c)))
+def test_large_losses(case, dtype):
+    say("loss", case, dtype)
+    run_loss(case, KINDS[dtype])
 
 
 # ---- clipping

@@ -10,7 +10,7 @@ from tests import test_reads_in_flight as T
 
 KK, KN, NN = range(3)
 STORE, GATED, GATED_GRAD, SCORES, SCORES_GRAD = range(5)
-NAME = re.compile(rb"_ZN2mg(?:12_GLOBAL__N_1)?17linear_(dma|any)_kernelI([\w]+?)EEvNS_?\w*?Args")
+NAME = re.compile(rb"_ZN2mg(?:12_GLOBAL__N_1)?1[67]linear_(dma|any|pp)_kernelI([\w]+?)EEvNS_?\w*?Args")
 PAIRS = {(KK, STORE), (KK, GATED), (KK, SCORES), (KK, SCORES_GRAD), (KN, STORE), (KN, GATED_GRAD), (NN, STORE)}
 
 
@@ -37,12 +37,18 @@ def built(kind):
 
 
 def dma():
-    tiles = {(256, 256, 2, 4, 2), (128, 128, 2, 2, 2), (128, 128, 2, 2, 4), (64, 64, 2, 2, 4)}
-    return {(kind, *pair, *tile) for kind in (False, True) for pair in PAIRS for tile in tiles}
+    tiles = {(128, 128, 2, 2, 2), (128, 128, 2, 2, 4), (64, 64, 2, 2, 4)}
+    return {(kind, *pair, *tile) for kind in (False, True) for pair in PAIRS for tile in tiles | ({(256, 256, 2, 4, 2)} if pair[0] == NN else set())}
+
+
+def pp():
+    """the 256 x 256 tile of operands that lie along the sum, P at least"""
+    return {(kind, *pair) for kind in (False, True) for pair in PAIRS if pair[0] != NN}
 
 
 def test_kernels_that_are_built():
     assert built("dma") == dma()
+    assert built("pp") == pp()
     assert built("any") == {(kind, *pair) for kind in (False, True) for pair in PAIRS}
 
 
@@ -52,7 +58,7 @@ def few():
     return {(kind, *kernel, once) for kind in (False, True) for kernel in kernels for once in (0, 1)}
 
 
-@pytest.mark.parametrize("start,wanted", [("_ZN2mg17linear_dma_kernelI", dma), ("_ZN2mg12_GLOBAL__N_121linear_few_dma_kernelI", few)])
+@pytest.mark.parametrize("start,wanted", [("_ZN2mg17linear_dma_kernelI", dma), ("_ZN2mg16linear_pp_kernelI", pp), ("_ZN2mg12_GLOBAL__N_121linear_few_dma_kernelI", few)])
 def test_every_hand_waited_kernel_is_looked_over(tmp_path, monkeypatch, start, wanted):
     monkeypatch.setattr(T, "KERNEL", re.compile(r"^[0-9a-f]+ <(" + start + r"\w+E+vNS\w*?10LinearArgsE)>:$"))
     seen, wrong = set(), {}

@@ -1,0 +1,54 @@
+"""The choice of the kernel for a product of 16-bit matrices, on the host: every kernel is taken somewhere in the GPU tests, slices fit their room and cover the sum."""
+import random
+
+from tests.linear_choice import choices
+
+
+def padded(v):
+    return -(-v // 64) * 64
+
+
+def block(tokens, width, hidden):
+    both = 2 * padded(hidden)
+    return [("kk", "gated", tokens, -(-hidden // 16) * 32, width), ("kk", "store", tokens, width, hidden), ("kn", "gated_grad", tokens, hidden, width), ("kn", "store", tokens, width, both),
+            ("nn", "store", both, width, tokens), ("nn", "store", width, hidden, tokens)]
+
+
+def loss(tokens, width, vocab):
+    return [("kk", "scores", tokens, vocab, width), ("kk", "scores_grad", tokens, vocab, width), ("kn", "store", tokens, width, vocab), ("nn", "store", vocab, width, tokens)]
+
+
+def test_the_gpu_tests_reach_every_kernel():
+    from tests import test_gpu_layers as G
+    asked = [p for c in G.BLOCKS + G.LARGE_BLOCKS for p in block(*c)] + [p for c in G.LOSSES + G.LARGE_LOSSES for p in loss(*c)]
+    taken = {(form, end, kernel) for (form, end, *_), (kernel, _, _) in zip(asked, choices(asked))}
+    pairs = {(form, end) for form, end, *_ in asked}
+    assert {(*pair, tile) for pair in pairs for tile in ("256", "64")} <= taken, {(*pair, tile) for pair in pairs for tile in ("256", "64")} - taken
+    for tile in ("128", "128 deep"):
+        assert sum(t[2] == tile for t in taken) >= 3, (tile, taken)
+    assert {("kk", end, "few") for end in ("store", "gated", "scores")} <= taken
+
+
+def test_slices_cover_the_sum_and_fit_their_room():
+    rng = random.Random(1)
+    asked = []
+    for _ in range(3000):
+        size = lambda most: int(round(most ** rng.random()))  # noqa: E731
+        form = rng.choice(("kk", "kn", "nn"))
+        end = rng.choice({"kk": ("store", "gated", "scores", "scores_grad"), "kn": ("store", "gated_grad"), "nn": ("store",)}[form])
+        asked.append((form, end, size(20000), size(70000), size(70000), rng.random() < 0.7, rng.choice((0, 1 << 20, 1 << 24, 1 << 28, 1 << 40))))
+    split = 0
+    for (form, end, rows, cols, k, aligned, room), (kernel, slices, each) in zip(asked, choices(asked)):
+        assert each % 64 == 0 and (slices - 1) * each < k <= slices * each
+        assert aligned == (kernel not in ("any", "any few"))
+        assert slices == 1 or (end == "store" and slices * rows * padded(cols) * 4 <= room)
+        assert kernel not in ("few", "any few") or (form == "kk" and rows <= 32)
+        split += slices > 1
+    assert split > 100
+
+
+def test_measured_choices():
+    """both sides were measured: 2048^3 30.2 us on 128, 21.7 on 128 deep; 4096 x 4096 x 2048 76 and 57 on 256; 8192 x 1024 x 1024 28 on 256, 21.5 on 128; 512 x 2048 x 2048
+    20 on 128 deep, 10.9 on 64; 256 x 256 x 8192 39 in one slice of 64, 13 in eight and more"""
+    got = choices([("kk", "store", 2048, 2048, 2048), ("kk", "store", 4096, 4096, 2048), ("kk", "store", 8192, 1024, 1024), ("kk", "store", 512, 2048, 2048), ("nn", "store", 256, 256, 8192)])
+    assert [g[0] for g in got] == ["128 deep", "256", "128", "64", "64"] and got[4][1] >= 8 and [g[1] for g in got[:4]] == [1] * 4
