@@ -3,7 +3,9 @@
 // Tensors are cut into chunks of 16 KB; a work-group has a range of consecutive chunks, whatever tensors they are of, so that many small tensors cost what one
 // large one does.  A launch takes a table of tensors among its arguments.  First pass: every work-group's sum of squares, in 64 bits (a square of a
 // bfloat16 does not fit FP32, and sums of 10^9 squares lose nothing that way); second pass: every work-group adds all work-groups' sums in the same order,
-// so that no launch stands between the passes, and scales.  Bound by memory: read once, read again and written.
+// so that no launch stands between the passes, and scales.  Bound by memory: read once, read again and written.  The second pass goes from the last chunks to
+// the first, which it finds in the last-level cache while they are, and large results pass that by: 800 MB of 300 tensors 633 -> 495 us (the first
+// pass at 3.9 TB/s, the second at 5.6).
 #include "layers.h"
 #include "internal.h"
 
@@ -11,9 +13,19 @@ namespace mg {
 namespace {
 
 constexpr int TENSORS = 120;                 // of a launch: 3.4 KB of arguments
-constexpr int MOST_GROUPS = 1024;            // work-groups of a launch: four for every compute unit
+constexpr int MOST_GROUPS = 1280;            // work-groups of a launch: five for every compute unit (four 2.5 % slower, three and six 8)
 constexpr int MOST_SUMS = 8192;              // of all launches, unless there are more launches than that
 constexpr int CHUNK_BYTES = 16384;
+constexpr int64_t PAST_CACHES = int64_t(128) << 20;      // results of so many bytes do not stay in the last-level cache (256 MB) for their reader
+
+// 16 bytes at the alignment of an element of SIZE bytes
+template <int SIZE> struct ClipPiece;
+template <> struct ClipPiece<4> {
+    typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <> struct ClipPiece<2> {
+    typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2)));
+};
 
 struct ClipTable {
     const void *source[TENSORS];
@@ -26,24 +38,25 @@ struct ClipTable {
 
 __host__ __device__ inline int64_t chunk_elements(int type) { return CHUNK_BYTES / (type == MG_F32 ? 4 : 2); }
 
-// calls fn(tensor, first element, elements) for the work-group's chunks
-template <typename Fn> __device__ inline void for_chunks(const ClipTable &t, Fn &&fn)
+// calls fn(tensor, first element, elements) for the work-group's chunks, BACK from the last one on
+template <bool BACK, typename Fn> __device__ inline void for_chunks(const ClipTable &t, Fn &&fn)
 {
-    const uint32_t total = t.begin[t.count];
-    uint32_t chunk = blockIdx.x * t.per_group;
-    const uint32_t end = chunk + t.per_group < total ? chunk + t.per_group : total;
-    if (chunk >= end) return;
-    int low = 0, high = t.count - 1;         // the tensor with begin <= chunk < the next one's
-    while (low < high) {
-        const int mid = (low + high + 1) / 2;
-        if (t.begin[mid] <= chunk) low = mid;
+    const uint32_t total = t.begin[t.count], start = blockIdx.x * t.per_group, end = start + t.per_group < total ? start + t.per_group : total;
+    if (start >= end) return;
+    uint32_t chunk = BACK ? end - 1 : start;
+    int at = 0, high = t.count - 1;          // the tensor with begin <= chunk < the next one's
+    while (at < high) {
+        const int mid = (at + high + 1) / 2;
+        if (t.begin[mid] <= chunk) at = mid;
         else high = mid - 1;
     }
-    for (; chunk < end; ++chunk) {
-        while (chunk >= t.begin[low + 1]) ++low;
-        const int type = static_cast<int>(t.size_type[low] & 3);
-        const int64_t size = t.size_type[low] >> 2, each = chunk_elements(type), first = (chunk - t.begin[low]) * each;
-        fn(low, type, first, size - first < each ? static_cast<int>(size - first) : static_cast<int>(each));
+    for (uint32_t n = end - start; n > 0; --n) {
+        if (BACK) while (chunk < t.begin[at]) --at;
+        else while (chunk >= t.begin[at + 1]) ++at;
+        const int type = static_cast<int>(t.size_type[at] & 3);
+        const int64_t size = t.size_type[at] >> 2, each = chunk_elements(type), first = (chunk - t.begin[at]) * each;
+        fn(at, type, first, size - first < each ? static_cast<int>(size - first) : static_cast<int>(each));
+        chunk += BACK ? -1 : 1;
     }
 }
 
@@ -77,7 +90,7 @@ __global__ __launch_bounds__(256) void squares_kernel(const ClipTable t, double 
 {
     __shared__ double parts[4];
     double sum = 0.0;
-    for_chunks(t, [&](int tensor, int type, int64_t first, int count) {
+    for_chunks<false>(t, [&](int tensor, int type, int64_t first, int count) {
         if (type == MG_F32) sum += squares(static_cast<const float *>(t.source[tensor]) + first, count);
         else if (type == MG_F16) sum += squares(static_cast<const _Float16 *>(t.source[tensor]) + first, count);
         else sum += squares(static_cast<const bfloat *>(t.source[tensor]) + first, count);
@@ -100,7 +113,8 @@ __global__ __launch_bounds__(256) void norm_kernel(const double *sums, int count
     if (threadIdx.x == 0) norm[0] = static_cast<float>(n);
 }
 
-template <typename T> __device__ inline void scale_chunk(const T *from, T *to, int count, float factor)
+// PASS: the results pass the caches by
+template <typename T, bool PASS> __device__ inline void scale_chunk(const T *from, T *to, int count, float factor)
 {
     constexpr int PER = 16 / static_cast<int>(sizeof(T));
     float v[4][PER];
@@ -114,22 +128,31 @@ template <typename T> __device__ inline void scale_chunk(const T *from, T *to, i
         const int e = (i * 256 + static_cast<int>(threadIdx.x)) * PER;
 #pragma unroll
         for (int k = 0; k < PER; ++k) v[i][k] *= factor;
+        if constexpr (PASS) {
+            if (count - e >= PER) {
+                Piece<T, PER> x;
+#pragma unroll
+                for (int k = 0; k < PER; ++k) x.v[k] = static_cast<T>(v[i][k]);
+                __builtin_nontemporal_store(__builtin_bit_cast(typename ClipPiece<sizeof(T)>::type, x), reinterpret_cast<typename ClipPiece<sizeof(T)>::type *>(to + e));
+                continue;
+            }
+        }
         store_piece<T, PER>(to + e, count - e > 0 ? count - e : 0, v[i]);
     }
 }
 
 // factor 1 does not touch what is scaled in place and copies what is not, infinities and NaN among it
-__global__ __launch_bounds__(256) void clip_kernel(const ClipTable t, const double *sums, int count, double max_norm, float *norm)
+template <bool PASS> __global__ __launch_bounds__(256) void clip_kernel(const ClipTable t, const double *sums, int count, double max_norm, float *norm)
 {
     __shared__ double parts[4];
     const double n = norm_of(sums, count, parts);
     if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = static_cast<float>(n);
     const float factor = n > max_norm && n < __builtin_inf() ? static_cast<float>(max_norm / n) : 1.f;
-    for_chunks(t, [&](int tensor, int type, int64_t first, int some) {
+    for_chunks<true>(t, [&](int tensor, int type, int64_t first, int some) {
         if (factor == 1.f && t.source[tensor] == t.result[tensor]) return;
-        if (type == MG_F32) scale_chunk(static_cast<const float *>(t.source[tensor]) + first, static_cast<float *>(t.result[tensor]) + first, some, factor);
-        else if (type == MG_F16) scale_chunk(static_cast<const _Float16 *>(t.source[tensor]) + first, static_cast<_Float16 *>(t.result[tensor]) + first, some, factor);
-        else scale_chunk(static_cast<const bfloat *>(t.source[tensor]) + first, static_cast<bfloat *>(t.result[tensor]) + first, some, factor);
+        if (type == MG_F32) scale_chunk<float, PASS>(static_cast<const float *>(t.source[tensor]) + first, static_cast<float *>(t.result[tensor]) + first, some, factor);
+        else if (type == MG_F16) scale_chunk<_Float16, PASS>(static_cast<const _Float16 *>(t.source[tensor]) + first, static_cast<_Float16 *>(t.result[tensor]) + first, some, factor);
+        else scale_chunk<bfloat, PASS>(static_cast<const bfloat *>(t.source[tensor]) + first, static_cast<bfloat *>(t.result[tensor]) + first, some, factor);
     });
 }
 
@@ -165,6 +188,9 @@ size_t clip_workspace(int64_t count) { return static_cast<size_t>(launches(count
 hipError_t launch_clip(const ClipProblem &p)
 {
     double *const sums = static_cast<double *>(p.workspace);
+    int64_t bytes = 0;
+    for (int64_t i = 0; i < p.count; ++i) bytes += p.sizes[i] * (p.types[i] == MG_F32 ? 4 : 2);
+    const bool past = bytes >= PAST_CACHES;
     ClipTable t;
     int written = 0;
     for (int64_t first = 0; first < p.count; first += TENSORS) {
@@ -176,10 +202,11 @@ hipError_t launch_clip(const ClipProblem &p)
     }
     bool told = false;
     if (p.scales)
-        for (int64_t first = 0; first < p.count; first += TENSORS) {
+        for (int64_t first = (p.count - 1) / TENSORS * TENSORS; first >= 0; first -= TENSORS) {
             const uint32_t groups = fill(t, p, first);
             if (groups == 0) continue;
-            clip_kernel<<<groups, 256, 0, p.stream>>>(t, sums, written, static_cast<double>(p.max_norm), told ? nullptr : p.norm);
+            auto kernel = past ? clip_kernel<true> : clip_kernel<false>;
+            kernel<<<groups, 256, 0, p.stream>>>(t, sums, written, static_cast<double>(p.max_norm), told ? nullptr : p.norm);
             told = true;
             if (const hipError_t e = hipGetLastError()) return e;
         }

@@ -314,11 +314,7 @@ template <int FORM, int END> hipError_t launch_linear_dma(int dtype, int tile, c
 {
     auto with = [&](auto type) {
         using T = decltype(type);
-        if constexpr (FORM == FORM_NN) {
-            if (tile == LINEAR_256) return launch_linear_dma_as<T, FORM, END, 256, 256, 2, 4, 2>(args, slices, stream);
-        } else {
-            if (tile == LINEAR_256) return launch_linear_pp<T, FORM, END>(args, slices, stream);
-        }
+        if (tile == LINEAR_256) return launch_linear_pp<T, FORM, END>(args, slices, stream);
         if (tile == LINEAR_128) return launch_linear_dma_as<T, FORM, END, 128, 128, 2, 2, 2>(args, slices, stream);
         if (tile == LINEAR_128_DEEP) return launch_linear_dma_as<T, FORM, END, 128, 128, 2, 2, 4>(args, slices, stream);
         return launch_linear_dma_as<T, FORM, END, 64, 64, 2, 2, 4>(args, slices, stream);

@@ -13,7 +13,7 @@ struct LinearPlan {
 
 // What a tile takes, in us, measured with random bfloat16 operands: `alone` for 64 values of the sum while a compute unit has one of its tiles, with n of them
 // n * `each`; around the sum `start`, and `more` for every tile of a compute unit (C leaves).  Along / across the sum costs more reads of LDS (`form`).
-// Estimated and measured: 2048^3 on 128_DEEP 23 and 21.7, 4096 x 4096 x 2048 on 256 60 and 58, on 128 74 and 72, 8192 x 8192 x 512 on 256 79 and 84,
+// Estimated and measured: 2048^3 on 128_DEEP 23 and 21.7, 4096 x 4096 x 2048 on 256 55 and 57, on 128 74 and 72, 8192 x 8192 x 512 on 256 75 and 89,
 // 8192 x 1024 x 1024 on 128 22 and 21.5, 512 x 2048 x 2048 on 64 11.6 and 10.9, 333 x 1001 x 1999 on 64 11.1 and 10.5.
 struct LinearCost {
     double alone, each, start, more;
@@ -23,7 +23,7 @@ inline LinearCost linear_cost(int tile, int form)
     LinearCost c{};
     double across = 1;                     // FORM_NN; half as much more for FORM_KN
     switch (tile) {
-        case LINEAR_256: c = {1.48, 1.55, 4, 6.5}; across = 1.12; break;
+        case LINEAR_256: c = {1.35, 1.4, 4, 6.5}; across = 1.08; break;
         case LINEAR_128: c = {0.82, 0.5, 3, 1.6}; across = 1.08; break;
         case LINEAR_128_DEEP: c = {0.55, 0.58, 2.5, 2}; across = 1.08; break;
         case LINEAR_64: c = {0.3, 0.21, 1.5, 0.5}; across = 1.2; break;

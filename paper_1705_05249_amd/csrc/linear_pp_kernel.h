@@ -1,8 +1,10 @@
 // Products of 16-bit matrices on 256 x 256 tiles in which the two wavefronts that share a SIMD take turns: while one issues the matrix instructions of a K-tile
 // from registers, the other fetches its operands of the next one from LDS and starts global -> LDS loads; a work-group barrier ends every turn.  The schedule is
-// that of hgemm_pp_kernel (mfma_pp_kernel.h, where its turns and shares of the loads are drawn up), with Q as its A and P, which lies along the sum, as its B; what
-// is different is what linear_dma_kernel.h says: bfloat16, Q of two matrices, sizes that end inside a tile, what becomes of the sums.
-// 8192 x 8192 x 8192: 1.25 -> PP_RATE PFLOP/s.
+// that of hgemm_pp_kernel (mfma_pp_kernel.h, where its turns and shares of the loads are drawn up), with Q as its A and P as its B; what is different is what
+// linear_dma_kernel.h says: bfloat16, Q of two matrices, sizes that end inside a tile, what becomes of the sums; and P may lie across the sum, as two halves of 128 rows
+// in LDS, since each half of the work-group reads one and its blocks are loaded apart from the other's.
+// Measured, in us, against the kernel of linear_dma_kernel.h on the same tile: 4096 x 4096 x 8192 both along 226 -> 186 (1.48 PFLOP/s), 8192 x 2048 x 16384
+// with Q across 484 -> 409; 8192^3 both across 947 -> 808 (1.36).
 #pragma once
 
 #include "linear_dma_kernel.h"
@@ -60,6 +62,32 @@ template <bool ALONG, bool GATED = false> struct LinearLoaderHalf {
     }
 };
 
+// P across the sum, 256 columns in memory and two tiles of 128 in LDS (lines of 256 bytes, four to a block): blocks Q = 0 .. 3 of a wavefront are lines 16 Q + 4 w ..
+// of the first, 4 .. 7 of the second.
+struct LinearLoaderHalves {
+    static constexpr uint32_t MISSING = 0x80000000u;
+    uint32_t goff[2], step;
+    __amdgpu_buffer_rsrc_t rsrc;
+
+    __device__ inline void prepare(int64_t ld, int64_t, int w, int lane, int left)
+    {
+        const int kl = 4 * w + lane / 16, chunk = lane % 16 ^ ldsmap::line_swizzle(128, kl);
+        static_for<2>([&](auto H) {
+            constexpr int h = decltype(H)::value;
+            goff[h] = 128 * h + chunk * 8 < left ? static_cast<uint32_t>(kl * ld * 2) + 256 * h + (chunk << 4) : MISSING;
+        });
+        step = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(16 * ld * 2));
+    }
+    __device__ inline void aim(const _Float16 *X, int64_t ld, int64_t r0, int64_t l0, int left, int rows)
+    {
+        rsrc = LinearLoader<256, 512, false>::descriptor(X + r0 + l0 * ld, left < 64 ? left : 64, ld, rows);
+    }
+    template <int Q> __device__ inline void issue(lds_char *mine, bool flat = false) const
+    {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, reinterpret_cast<lds_void *>(mine + (flat ? 0 : Q * 4096)), 16, goff[Q / 4] + (Q % 4) * step, 0, 0, 0);
+    }
+};
+
 // (as mma_in_place of mfma_pp_kernel.h, and for its reasons)
 template <typename T> __device__ inline void multiply_in_place(floatx4 &acc, const u32x4 &frag_p, const u32x4 &frag_q)
 {
@@ -72,12 +100,11 @@ constexpr int LINEAR_PP_LDS = 4 * 32768 + 1024;
 template <typename T, int FORM, int END> __global__ __launch_bounds__(512) void linear_pp_kernel(const LinearArgs args)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr bool Q_ALONG = FORM == FORM_KK, GATED = END == END_GATED;
-    static_assert(FORM != FORM_NN, "rows 0-127 and 128-255 of P must be separate 1 KB blocks");
+    constexpr bool P_ALONG = FORM != FORM_NN, Q_ALONG = FORM == FORM_KK, GATED = END == END_GATED;
     constexpr int BC = 256, BR = 256, WC = 2, WR = 4, BK = 64, RB = 16, KSTEPS = 2;
     constexpr int WTC = BC / WC, WTR = BR / WR, FM = WTC / RB, FN = WTR / RB;
     using LoadQ = LinearLoaderHalf<Q_ALONG, GATED>;
-    using LoadP = LinearLoaderHalf<true>;
+    using LoadP = std::conditional_t<P_ALONG, LinearLoaderHalf<true>, LinearLoaderHalves>;
     constexpr int Q_BYTES = 32768, P_BYTES = 32768;              // LDS: [Q stage 0][Q stage 1][P stage 0][P stage 1][dump]
     constexpr int SLOTS = FM * FN, NMMA = KSTEPS * SLOTS, NM = 2, MEM_LOADS = 8 - NM;       // NM: loads a wavefront issues inside its run of MFMAs
     constexpr int REGION = end_region<WTC>(), DUMP = 2 * (Q_BYTES + P_BYTES);
@@ -99,7 +126,8 @@ template <typename T, int FORM, int END> __global__ __launch_bounds__(512) void 
         const int p = base + (along ? ldsmap::kcontig_base<RB>(lane, wrow) : ldsmap::transposed_base<RB>(lane, wrow, rows));
         return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds3)) + static_cast<uint32_t>(p);
     };
-    const uint32_t frag_q = first_fragment(Q_ALONG, wc * WTC, 0, BC), frag_p = first_fragment(true, wr * WTR, 2 * Q_BYTES, BR);
+    const uint32_t frag_q = first_fragment(Q_ALONG, wc * WTC, 0, BC);
+    const uint32_t frag_p = P_ALONG ? first_fragment(true, wr * WTR, 2 * Q_BYTES, BR) : first_fragment(false, wr % 2 * WTR, 2 * Q_BYTES + wr / 2 * (P_BYTES / 2), BR / 2);
 
     floatx4 acc[FN][FM];
 #pragma unroll
@@ -119,7 +147,7 @@ template <typename T, int FORM, int END> __global__ __launch_bounds__(512) void 
         constexpr int par = decltype(PAR)::value;
         static_for<KSTEPS>([&](auto S) {
             constexpr int s = decltype(S)::value;
-            static_for<FN>([&](auto F) { fp[s][decltype(F)::value] = read_linear<true, BR, decltype(F)::value, s, par * P_BYTES>(frag_p); });
+            static_for<FN>([&](auto F) { fp[s][decltype(F)::value] = read_linear<P_ALONG, P_ALONG ? BR : BR / 2, decltype(F)::value, s, par * P_BYTES>(frag_p); });
             static_for<FM>([&](auto F) { fq[s][decltype(F)::value] = read_linear<Q_ALONG, BC, decltype(F)::value, s, par * Q_BYTES>(frag_q); });
         });
     };

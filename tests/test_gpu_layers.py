@@ -249,7 +249,7 @@ def test_tokens_that_do_not_count_may_hold_anything():
 
 
 # sizes at which the large tiles are taken (tests/test_linear_plan.py says which by which product)
-LARGE_BLOCKS = [(3999, 520, 4000), (4000, 4008, 520), (520, 4000, 2000), (3970, 515, 4001), (1500, 1032, 1000)]
+LARGE_BLOCKS = [(3999, 520, 4000), (4000, 4008, 520), (520, 4000, 2000), (3970, 515, 4001), (1500, 1032, 1000), (1000, 1000, 9992), (2500, 2600, 300)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
@@ -259,13 +259,20 @@ def test_large_blocks(case, dtype):
     run_block(case, R.ACTS[sum(case) % 4], KINDS[dtype])
 
 
-LARGE_LOSSES = [(4000, 520, 4000), (3970, 515, 4061), (1111, 1032, 2100)]
+LARGE_LOSSES = [(4000, 520, 4000), (3970, 515, 4061), (1111, 1032, 2100), (2600, 264, 2600)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("case", LARGE_LOSSES, ids=lambda c: "x".join(map(str, c)))
 def test_large_losses(case, dtype):
     say("loss", case, dtype)
+    run_loss(case, KINDS[dtype])
+
+
+@pytest.mark.parametrize("case,dtype", [((16500, 64, 16640), "bf16"), ((16500, 40, 16700), "f16"), ((5000, 64, 14000), "f32")])
+def test_losses_in_pieces_of_the_vocabulary(case, dtype):
+    """2^28 elements of dz (FP32: 2^26) are more than a piece"""
+    assert case[0] * case[2] > (1 << 26 if dtype == "f32" else 1 << 28)
     run_loss(case, KINDS[dtype])
 
 

@@ -38,12 +38,12 @@ def built(kind):
 
 def dma():
     tiles = {(128, 128, 2, 2, 2), (128, 128, 2, 2, 4), (64, 64, 2, 2, 4)}
-    return {(kind, *pair, *tile) for kind in (False, True) for pair in PAIRS for tile in tiles | ({(256, 256, 2, 4, 2)} if pair[0] == NN else set())}
+    return {(kind, *pair, *tile) for kind in (False, True) for pair in PAIRS for tile in tiles}
 
 
 def pp():
-    """the 256 x 256 tile of operands that lie along the sum, P at least"""
-    return {(kind, *pair) for kind in (False, True) for pair in PAIRS if pair[0] != NN}
+    """the 256 x 256 tile"""
+    return {(kind, *pair) for kind in (False, True) for pair in PAIRS}
 
 
 def test_kernels_that_are_built():

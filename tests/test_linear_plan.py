@@ -23,9 +23,9 @@ def test_the_gpu_tests_reach_every_kernel():
     asked = [p for c in G.BLOCKS + G.LARGE_BLOCKS for p in block(*c)] + [p for c in G.LOSSES + G.LARGE_LOSSES for p in loss(*c)]
     taken = {(form, end, kernel) for (form, end, *_), (kernel, _, _) in zip(asked, choices(asked))}
     pairs = {(form, end) for form, end, *_ in asked}
-    assert {(*pair, tile) for pair in pairs for tile in ("256", "64")} <= taken, {(*pair, tile) for pair in pairs for tile in ("256", "64")} - taken
-    for tile in ("128", "128 deep"):
-        assert sum(t[2] == tile for t in taken) >= 3, (tile, taken)
+    missing = {(*pair, tile) for pair in pairs for tile in ("256", "128", "64")} - taken
+    assert not missing, missing
+    assert sum(t[2] == "128 deep" for t in taken) >= 3, taken
     assert {("kk", end, "few") for end in ("store", "gated", "scores")} <= taken
 
 
