@@ -11,27 +11,28 @@ struct LinearPlan {
     int slices, k_per_slice;
 };
 
-// What a tile takes, in us, measured with random bfloat16 operands: `alone` for 64 values of the sum while a compute unit has one of its tiles, with n of them
-// n * `each`; around the sum `start`, and `more` for every tile of a compute unit (C leaves).  Along / across the sum costs more reads of LDS (`form`).
-// Estimated and measured: 2048^3 on 128_DEEP 23 and 21.7, 4096 x 4096 x 2048 on 256 55 and 57, on 128 74 and 72, 8192 x 8192 x 512 on 256 75 and 89,
-// 8192 x 1024 x 1024 on 128 22 and 21.5, 512 x 2048 x 2048 on 64 11.6 and 10.9, 333 x 1001 x 1999 on 64 11.1 and 10.5.
+// What a tile takes, in us, measured with random bfloat16 operands: `alone` for 64 values of the sum while a compute unit has one of its tiles, `pair` while it has two
+// at a time (LDS has room for two of 128 or 64); around the sum `start`, and `more` for every tile of a compute unit (C leaves).  Operands across the sum cost more
+// reads of LDS (`form`).  Estimated and measured: 2048^3 on 128_DEEP 23 and 21.7, 4096 x 4096 x 2048 on 256 55 and 57, on 128 74 and 72, 8192 x 8192 x 512 on 256
+// 75 and 89, 1000 x 9999 x 1001 on 128 37 and 36, on 256 33 and 31, 8192 x 1024 x 1024 on 128 22 and 21.5, 512 x 2048 x 2048 on 64 11.6 and 10.9,
+// 333 x 1001 x 1999 on 64 11.6 and 10.5.
 struct LinearCost {
-    double alone, each, start, more;
+    double alone, pair, start, more;
 };
 inline LinearCost linear_cost(int tile, int form)
 {
     LinearCost c{};
     double across = 1;                     // FORM_NN; half as much more for FORM_KN
     switch (tile) {
-        case LINEAR_256: c = {1.35, 1.4, 4, 6.5}; across = 1.08; break;
-        case LINEAR_128: c = {0.82, 0.5, 3, 1.6}; across = 1.08; break;
-        case LINEAR_128_DEEP: c = {0.55, 0.58, 2.5, 2}; across = 1.08; break;
-        case LINEAR_64: c = {0.3, 0.21, 1.5, 0.5}; across = 1.2; break;
-        default: c = {0.5, 0.35, 3, 1.5}; across = 1.5; break;
+        case LINEAR_256: c = {1.4, 2.8, 4, 6.5}; across = 1.08; break;
+        case LINEAR_128: c = {0.82, 1.0, 3, 1.6}; across = 1.08; break;
+        case LINEAR_128_DEEP: c = {0.57, 1.14, 2.5, 2}; across = 1.08; break;
+        case LINEAR_64: c = {0.3, 0.42, 1.5, 0.5}; across = 1.2; break;
+        default: c = {0.5, 0.7, 3, 1.5}; across = 1.5; break;
     }
     const double factor = form == FORM_NN ? across : form == FORM_KN ? (1 + across) / 2 : 1;
     c.alone *= factor;
-    c.each *= factor;
+    c.pair *= factor;
     return c;
 }
 
@@ -55,8 +56,8 @@ inline LinearPlan linear_plan(int form, int end, int64_t rows, int64_t cols, int
         for (int s = 1; s <= 64; s *= 2) {
             if (s > 1 && (end != END_STORE || pieces / s < 4 || one * s > static_cast<double>(room) || tiles * s > 1024)) break;
             const double per_unit = static_cast<double>(ceil_div(tiles * s, 256));
-            const double piece = c.each * per_unit > c.alone ? c.each * per_unit : c.alone;
-            const double us = c.start + c.more * per_unit + pieces / s * piece + (s > 1 ? 4 + one * (s + 1) / 4e6 : 0);
+            const double pairs = static_cast<double>(ceil_div(tiles * s, 256) / 2), piece = pairs * c.pair + (per_unit - 2 * pairs) * c.alone;
+            const double us = c.start + c.more * per_unit + pieces / s * piece + (s > 1 ? 6 + one * (s + 1) / 4e6 : 0);
             if (least == 0 || us < least) {
                 least = us;
                 best.tile = tile;

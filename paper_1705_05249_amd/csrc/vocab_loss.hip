@@ -23,14 +23,26 @@ int64_t piece_columns(int dtype, int64_t tokens, int64_t vocab)
 
 mg_status launched(hipError_t e) { return e == hipSuccess ? MG_OK : MG_ERR_LAUNCH; }
 
-// FP32: (largest, sum of exponentials) of a row of a piece of logits, and the target's logit.  A work-group a row; z is read twice, the second time from L2.
+constexpr int CHUNK = 4096;             // logits of a row that a work-group of the FP32 kernels has, 16 in a thread
+
+// FP32: (largest, sum of exponentials) of a chunk of a row of logits, and the target's logit.  z is read once.
 __global__ __launch_bounds__(256) void scores_kernel(const float *Z, int64_t ldz, int cols, int64_t first, int tokens, const int64_t *targets, float2 *scores, float *target_score)
 {
     __shared__ float parts[4];
-    const int row = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const float *z = Z + row * ldz;
-    float m = -__builtin_inff();
-    for (int c = threadIdx.x; c < cols; c += 256) m = fmaxf(m, z[c]);
+    const int row = blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64, start = blockIdx.y * CHUNK;
+    const float *z = Z + row * ldz + start;
+    const int here = cols - start < CHUNK ? cols - start : CHUNK;
+    float v[4][4], m = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = (i * 256 + static_cast<int>(threadIdx.x)) * 4;
+        load_piece<float, 4>(z + c, here - c > 0 ? here - c : 0, v[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e >= here) v[i][e] = -__builtin_inff();
+            m = fmaxf(m, v[i][e]);
+        }
+    }
     for (int d = 32; d > 0; d /= 2) m = fmaxf(m, __shfl_xor(m, d));
     if (lane == 0) parts[wave] = m;
     __syncthreads();
@@ -38,27 +50,37 @@ __global__ __launch_bounds__(256) void scores_kernel(const float *Z, int64_t ldz
     __syncthreads();
     const float from = m == -__builtin_inff() ? 0.f : m;
     float s = 0.f;
-    for (int c = threadIdx.x; c < cols; c += 256) s += expf(z[c] - from);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += expf(v[i][e] - from);
     for (int d = 32; d > 0; d /= 2) s += __shfl_xor(s, d);
     if (lane == 0) parts[wave] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
-        scores[row] = make_float2(m, (parts[0] + parts[1]) + (parts[2] + parts[3]));
-        const int64_t t = targets[row] - first;
-        if (t >= 0 && t < cols) target_score[row] = z[t];
+        scores[static_cast<int64_t>(blockIdx.y) * tokens + row] = make_float2(m, (parts[0] + parts[1]) + (parts[2] + parts[3]));
+        const int64_t t = targets[row] - first - start;
+        if (t >= 0 && t < here) target_score[row] = z[t];
     }
-    (void)tokens;
 }
 
 // FP32: dz in the place of z
 __global__ __launch_bounds__(256) void scores_grad_kernel(float *Z, int64_t ldz, int cols, int64_t first, int64_t vocab, const int64_t *targets, const float *lse,
                                                           const float *weights)
 {
-    const int row = blockIdx.x;
-    const int64_t target = targets[row];
+    const int row = blockIdx.x, start = blockIdx.y * CHUNK, here = cols - start < CHUNK ? cols - start : CHUNK;
+    const int64_t target = targets[row], at = target - first - start;
     const float w = target >= 0 && target < vocab ? weights == nullptr ? 1.f : weights[row] : 0.f, l = lse[row];
-    float *z = Z + row * ldz;
-    for (int c = threadIdx.x; c < cols; c += 256) z[c] = w != 0.f ? w * (expf(z[c] - l) - (first + c == target ? 1.f : 0.f)) : 0.f;
+    float *z = Z + row * ldz + start;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = (i * 256 + static_cast<int>(threadIdx.x)) * 4, left = here - c > 0 ? here - c : 0;
+        float v[4];
+        load_piece<float, 4>(z + c, left, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = w != 0.f ? w * (expf(v[e] - l) - (c + e == at ? 1.f : 0.f)) : 0.f;
+        store_piece<float, 4>(z + c, left, v);
+    }
 }
 
 // Joins the tiles' scores in a fixed order: TOKENS tokens a work-group, 256 / TOKENS lanes a token.
@@ -109,6 +131,9 @@ __global__ __launch_bounds__(1024) void weight_scale_kernel(const float *weights
     scale[1] = largest == 0 ? 1.f : w / most;
 }
 
+// FP32: how many scores a token has when the vocabulary goes in pieces
+int64_t score_chunks(int64_t vocab, int64_t columns) { return vocab / columns * ceil_div(columns, CHUNK) + ceil_div(vocab % columns, CHUNK); }
+
 struct LossMemory {
     float2 *scores;
     float *target_score, *pieces;          // pieces: FP32 logits
@@ -122,7 +147,7 @@ LossMemory loss_memory(Arena &ws, int dtype, int64_t tokens, int64_t vocab)
     const int64_t columns = vocab > 0 ? piece_columns(dtype, tokens, vocab) : 0;
     m.target_score = static_cast<float *>(ws.take(tokens * F));
     if (dtype == MG_F32) {
-        m.scores = static_cast<float2 *>(ws.take(vocab > 0 ? ceil_div(vocab, columns) * tokens * 8 : 0));
+        m.scores = static_cast<float2 *>(ws.take(vocab > 0 ? score_chunks(vocab, columns) * tokens * 8 : 0));
         m.pieces = static_cast<float *>(ws.take(tokens * columns * F));
     } else {
         m.scores = static_cast<float2 *>(ws.take(ceil_div(vocab, 64) * tokens * 8));
@@ -186,14 +211,16 @@ const float *row_of(const void *X, int64_t row, int64_t ld) { return static_cast
 mg_status loss_f32(const LossProblem &p, const LossMemory &m)
 {
     const int64_t columns = piece_columns(MG_F32, p.tokens, p.vocab);
-    for (int64_t first = 0, n = 0; first < p.vocab; first += columns, ++n) {
-        const int64_t some = p.vocab - first < columns ? p.vocab - first : columns;
+    int64_t done = 0;
+    for (int64_t first = 0; first < p.vocab; first += columns) {
+        const int64_t some = p.vocab - first < columns ? p.vocab - first : columns, chunks = ceil_div(some, CHUNK);
         const mg_status st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_TRANS, p.tokens, some, p.width, 1.f, static_cast<const float *>(p.X), p.ldx, row_of(p.W, first, p.ldw), p.ldw, 0.f,
                                       m.pieces, columns, m.rest, m.left, p.stream);
         if (st != MG_OK) return st;
-        scores_kernel<<<static_cast<uint32_t>(p.tokens), 256, 0, p.stream>>>(m.pieces, columns, static_cast<int>(some), first, static_cast<int>(p.tokens), p.targets, m.scores + n * p.tokens,
-                                                                             m.target_score);
+        scores_kernel<<<dim3(static_cast<uint32_t>(p.tokens), static_cast<uint32_t>(chunks)), 256, 0, p.stream>>>(m.pieces, columns, static_cast<int>(some), first, static_cast<int>(p.tokens),
+                                                                                                                 p.targets, m.scores + done * p.tokens, m.target_score);
         if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
+        done += chunks;
     }
     return MG_OK;
 }
@@ -207,7 +234,7 @@ mg_status grad_f32(const LossProblem &p, const LossGradMemory &m)
         const float *W = row_of(p.W, first, p.ldw), *X = static_cast<const float *>(p.X);
         mg_status st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_TRANS, p.tokens, some, p.width, 1.f, X, p.ldx, W, p.ldw, 0.f, Z, columns, m.rest, m.left, p.stream);
         if (st != MG_OK) return st;
-        scores_grad_kernel<<<static_cast<uint32_t>(p.tokens), 256, 0, p.stream>>>(Z, columns, static_cast<int>(some), first, p.vocab, p.targets, p.lse, p.weights);
+        scores_grad_kernel<<<dim3(static_cast<uint32_t>(p.tokens), static_cast<uint32_t>(ceil_div(some, CHUNK))), 256, 0, p.stream>>>(Z, columns, static_cast<int>(some), first, p.vocab, p.targets, p.lse, p.weights);
         if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
         if (p.dX != nullptr)
             st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_NO_TRANS, p.tokens, p.width, some, 1.f, Z, columns, W, p.ldw, first > 0 ? 1.f : 0.f, static_cast<float *>(p.dX), p.lddx, m.rest,
@@ -327,7 +354,7 @@ mg_status vocab_loss(const LossProblem &p)
     int tiles = 0;
     if (p.vocab > 0 && p.dtype == MG_F32) {
         if (const mg_status st = loss_f32(p, m)) return st;
-        tiles = static_cast<int>(ceil_div(p.vocab, piece_columns(MG_F32, p.tokens, p.vocab)));
+        tiles = static_cast<int>(score_chunks(p.vocab, piece_columns(MG_F32, p.tokens, p.vocab)));
     } else if (p.vocab > 0) {
         LossOperands o;
         if (const hipError_t e = loss_operands(p, ws, o)) return launched(e);
