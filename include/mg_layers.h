@@ -9,8 +9,8 @@
  * all matrices of a call.  Results do not depend on timing: the same call gives the same bits.  A result may not overlap what the call reads.
  *
  * Sums are in FP32 (MG_F32: as mg_sgemm's).  With 16-bit types a number is rounded to dtype where it becomes an operand of the next product
- * (H, dG and dU of a block, dz of the loss) and where it is a result, and nowhere else; activations, exponentials and what a block keeps
- * for its backward pass are in FP32.
+ * (H, dG and dU of a block, dz of the loss) and where it is a result; activations and exponentials are in FP32, and so is what a block keeps for its
+ * backward pass, but for MG_BF16, where that has 11 bits and exponents of its own.
  *
  * Workspaces: 256-byte aligned, at least the bytes that the query of the call answers (MG_ERR_WORKSPACE otherwise), which is 0 for sizes that
  * the call refuses.  With 16-bit types, operands whose rows start on 16 bytes (pointer and leading dimension) and are whole 16-byte pieces
@@ -45,7 +45,7 @@ enum {
  *   g / 2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3)));  MG_ACT_RELU2 max(g, 0)^2. */
 typedef enum { MG_ACT_SILU = 171, MG_ACT_GELU = 172, MG_ACT_GELU_TANH = 173, MG_ACT_RELU2 = 174 } mg_activation;
 
-/* kept: what mg_gated_backward reads of this forward pass (G, U and H, in an order of their own), 256-byte aligned, at least
+/* kept: what mg_gated_backward reads of this forward pass (act(G), U act'(G) and H, in an order of their own), 256-byte aligned, at least
  * mg_gated_kept_bytes() bytes; NULL where no backward pass will come (tokens that are served).  Calls of few tokens without it read the
  * weights once, at the memory's rate.
  * Errors: MG_ERR_DIM, MG_ERR_LDA (ldx), MG_ERR_LDB (a weight matrix's), MG_ERR_LDC (ldy), MG_ERR_NULL, MG_ERR_WORKSPACE, MG_ERR_TYPE,
@@ -59,7 +59,7 @@ size_t mg_gated_kept_bytes(int dtype, int64_t tokens, int64_t width, int64_t hid
 /* Gradients for dY (tokens x width), from the same X and weights and what the forward pass of the same dtype, activation and sizes kept:
  *     dH = dY WD,  dU = dH * act(G),  dG = dH * U * act'(G)
  *     dX = dG WG + dU WU,  dWG = dG^T X,  dWU = dU^T X,  dWD = dY^T H
- * Each of the four results may be NULL.  `kept` is not changed: the call can be made again.  No tokens: the weights' gradients become zero.
+ * The activation's slope is in what was kept; `activation` is checked, nothing else.  Each of the four results may be NULL.  `kept` is not changed: the call can be made again.  No tokens: the weights' gradients become zero.
  * Errors: as above, MG_ERR_LDA also for lddy, MG_ERR_LDC for a result's. */
 mg_status mg_gated_backward(int dtype, int activation, int64_t tokens, int64_t width, int64_t hidden, const void *X, int64_t ldx,
                             const void *WG, int64_t ldwg, const void *WU, int64_t ldwu, const void *WD, int64_t ldwd, const void *dY, int64_t lddy,

@@ -1,7 +1,8 @@
 // Gated feed-forward blocks: which products a call is made of, and the elementwise kernels between the products of FP32.
 //
 // Forward, 16 bits: one product with gate and up weights as one matrix, 16 rows of each in turn, so that a lane holds g and u of the same element and
-// H leaves the kernel (6 tokens width hidden operations in two launches); then Y.  Backward: dH never exists in memory, dG and dU leave its product;
+// H leaves the kernel (6 tokens width hidden operations in two launches); then Y.  Backward: dH never exists in memory, dG and dU leave its product, made of what
+// the forward pass kept without another look at the activation;
 // dX is one sum over 2 hidden, dG's half and dU's; the gradients of gate and up weights are one product with twice the rows.
 // FP32: products as mg_sgemm makes them, with G and U in memory.
 #include "linear_end.h"
@@ -12,41 +13,47 @@ namespace {
 
 constexpr int64_t F = sizeof(float);
 
-// H = act(G) * U
-template <int ACT> __global__ __launch_bounds__(256) void gated_act_kernel(const float *G, const float *U, float *H, int64_t count)
-{
-    const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
-    if (at >= count) return;
-    float g[4], u[4], h[4], slope;
-    load_piece<float, 4>(G + at, static_cast<int>(count - at < 4 ? count - at : 4), g);
-    load_piece<float, 4>(U + at, static_cast<int>(count - at < 4 ? count - at : 4), u);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        activation_of<ACT, true>(g[e], h[e], slope);
-        h[e] *= u[e];
-    }
-    store_piece<float, 4>(H + at, static_cast<int>(count - at < 4 ? count - at : 4), h);
-}
-
-// dG (where dH is) and dU
-template <int ACT> __global__ __launch_bounds__(256) void gated_grad_kernel(const float *G, const float *U, float *dH, float *dU, int64_t count)
+// H = act(G) * U; KEEP: act(G) and U act'(G) take the places of G and U
+template <int ACT, bool KEEP> __global__ __launch_bounds__(256) void gated_act_kernel(float *G, float *U, float *H, int64_t count)
 {
     const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
     if (at >= count) return;
     const int valid = static_cast<int>(count - at < 4 ? count - at : 4);
-    float g[4], u[4], d[4], other[4];
+    float g[4], u[4], h[4];
     load_piece<float, 4>(G + at, valid, g);
     load_piece<float, 4>(U + at, valid, u);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float a, slope;
+        activation_of<ACT, true>(g[e], a, slope);
+        h[e] = a * u[e];
+        g[e] = a;
+        u[e] *= slope;
+    }
+    store_piece<float, 4>(H + at, valid, h);
+    if (KEEP) {
+        store_piece<float, 4>(G + at, valid, g);
+        store_piece<float, 4>(U + at, valid, u);
+    }
+}
+
+// dG = dH b (where dH is) and dU = dH a, from what the forward pass kept
+__global__ __launch_bounds__(256) void gated_grad_kernel(const float *A, const float *B, float *dH, float *dU, int64_t count)
+{
+    const int64_t at = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (at >= count) return;
+    const int valid = static_cast<int>(count - at < 4 ? count - at : 4);
+    float a[4], b[4], d[4];
+    load_piece<float, 4>(A + at, valid, a);
+    load_piece<float, 4>(B + at, valid, b);
     load_piece<float, 4>(dH + at, valid, d);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        float h, slope;
-        activation_of<ACT, true>(g[e], h, slope);
-        other[e] = d[e] * h;
-        d[e] = d[e] * u[e] * slope;
+        a[e] *= d[e];
+        b[e] *= d[e];
     }
-    store_piece<float, 4>(dH + at, valid, d);
-    store_piece<float, 4>(dU + at, valid, other);
+    store_piece<float, 4>(dH + at, valid, b);
+    store_piece<float, 4>(dU + at, valid, a);
 }
 
 uint32_t pieces(int64_t count) { return static_cast<uint32_t>(ceil_div(count, 1024)); }
@@ -61,7 +68,7 @@ template <typename Fn> hipError_t with_activation(int act, Fn &&fn)
     return hipGetLastError();
 }
 
-// what a forward pass of FP32 keeps, tokens x hidden each
+// what a forward pass of FP32 keeps, tokens x hidden each: act(G) and U act'(G), where G and U were, and H
 struct KeptF32 {
     float *G, *U, *H;
     KeptF32(void *at, int64_t tokens, int64_t hidden) : G(static_cast<float *>(at)), U(G + tokens * hidden), H(U + tokens * hidden) {}
@@ -102,7 +109,9 @@ mg_status forward_f32(const GatedProblem &p)
     if (const mg_status st = product(X, p.ldx, p.WU, p.ldwu, p.hidden, p.width, kept.U, p.hidden)) return st;
     const int64_t count = p.tokens * p.hidden;
     const hipError_t e = with_activation(p.activation, [&](auto act) {
-        gated_act_kernel<decltype(act)::value><<<pieces(count), 256, 0, p.stream>>>(kept.G, kept.U, kept.H, count);
+        constexpr int ACT = decltype(act)::value;
+        if (p.kept != nullptr) gated_act_kernel<ACT, true><<<pieces(count), 256, 0, p.stream>>>(kept.G, kept.U, kept.H, count);
+        else gated_act_kernel<ACT, false><<<pieces(count), 256, 0, p.stream>>>(kept.G, kept.U, kept.H, count);
     });
     if (e != hipSuccess) return MG_ERR_LAUNCH;
     return product(kept.H, p.hidden, p.WD, p.ldwd, p.width, p.hidden, static_cast<float *>(p.Y), p.ldy);
@@ -124,10 +133,8 @@ mg_status backward_f32(const GatedProblem &p)
     if (p.dX != nullptr || p.dWG != nullptr || p.dWU != nullptr) {
         st = product(MG_NO_TRANS, p.tokens, p.hidden, p.width, p.dY, p.lddy, p.WD, p.ldwd, 0.f, dG, p.hidden);
         if (st != MG_OK) return st;
-        const hipError_t e = with_activation(p.activation, [&](auto act) {
-            gated_grad_kernel<decltype(act)::value><<<pieces(count), 256, 0, p.stream>>>(kept.G, kept.U, dG, dU, count);
-        });
-        if (e != hipSuccess) return MG_ERR_LAUNCH;
+        gated_grad_kernel<<<pieces(count), 256, 0, p.stream>>>(kept.G, kept.U, dG, dU, count);
+        if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
     }
     if (p.dX != nullptr) {
         st = product(MG_NO_TRANS, p.tokens, p.width, p.hidden, dG, p.hidden, p.WG, p.ldwg, 0.f, p.dX, p.lddx);
@@ -139,8 +146,8 @@ mg_status backward_f32(const GatedProblem &p)
     return st;
 }
 
-// G and U in front of H
-size_t kept_scores(int64_t tokens, int64_t hidden) { return static_cast<size_t>(kept_at((tokens + 15) / 16 * 16, 0, hidden)) * F; }
+// 16 bits: a and b in front of H
+size_t kept_front(int dtype, int64_t tokens, int64_t hidden) { return static_cast<size_t>(kept_block((tokens + 15) / 16 * 16, 0, hidden) * kept_block_bytes(dtype) + 255) / 256 * 256; }
 size_t held_rows(int64_t tokens, int64_t cols) { return static_cast<size_t>(tokens * padded(cols)) * 2; }
 
 mg_status launched(hipError_t e) { return e == hipSuccess ? MG_OK : MG_ERR_LAUNCH; }
@@ -201,8 +208,7 @@ void left(LinearArgs &a, const Operand &p) { a.P = p.at; a.ldp = p.ld; a.p_padde
 mg_status forward_16(const GatedProblem &p)
 {
     Arena ws = p.workspace;
-    float *const kept = static_cast<float *>(p.kept);
-    void *const H = kept != nullptr ? static_cast<char *>(p.kept) + kept_scores(p.tokens, p.hidden) : ws.take(held_rows(p.tokens, p.hidden));
+    void *const H = p.kept != nullptr ? static_cast<char *>(p.kept) + kept_front(p.dtype, p.tokens, p.hidden) : ws.take(held_rows(p.tokens, p.hidden));
     const size_t wanted = forward_room(p.tokens, p.width, p.hidden), room_bytes = wanted < ws.left() ? wanted : ws.left();
     void *const room = ws.take(room_bytes);
     Copies copied(ws, p.tokens >= COPY_TOKENS);
@@ -214,7 +220,7 @@ mg_status forward_16(const GatedProblem &p)
     gate(a, wg);
     a.Q1 = wu.at; a.ldq1 = wu.ld; a.q_padded = wg.padded && wu.padded;
     a.rows = static_cast<int>(p.tokens); a.cols = static_cast<int>(kept_blocks(p.hidden) * 32); a.k = static_cast<int>(p.width);
-    a.hidden = static_cast<int>(p.hidden); a.activation = p.activation; a.kept = kept;
+    a.hidden = static_cast<int>(p.hidden); a.activation = p.activation; a.kept = p.kept;
     a.C0 = H; a.ldc0 = padded(p.hidden);
     if (const hipError_t e = launch_linear(p.dtype, FORM_KK, END_GATED, a, nullptr, 0, p.stream)) return launched(e);
     LinearArgs b{};
@@ -246,7 +252,7 @@ mg_status backward_16(const GatedProblem &p)
         left(a, dy);
         gate(a, wd);
         a.rows = tokens; a.cols = hidden; a.k = width;
-        a.hidden = hidden; a.activation = p.activation; a.kept = static_cast<float *>(p.kept);
+        a.hidden = hidden; a.kept = p.kept;
         a.C0 = d; a.ldc0 = 2 * half;
         if (const hipError_t e = launch_linear(p.dtype, FORM_KN, END_GATED_GRAD, a, nullptr, 0, p.stream)) return launched(e);
     }
@@ -272,7 +278,7 @@ mg_status backward_16(const GatedProblem &p)
     if (p.dWD != nullptr) {
         LinearArgs a{};
         left(a, dy);
-        gate(a, {static_cast<char *>(p.kept) + kept_scores(p.tokens, p.hidden), half, true});
+        gate(a, {static_cast<char *>(p.kept) + kept_front(p.dtype, p.tokens, p.hidden), half, true});
         a.rows = width; a.cols = hidden; a.k = tokens;
         a.C0 = p.dWD; a.ldc0 = p.lddwd;
         if (const hipError_t e = launch_linear(p.dtype, FORM_NN, END_STORE, a, room, room_bytes, p.stream)) return launched(e);
@@ -284,7 +290,7 @@ mg_status backward_16(const GatedProblem &p)
 
 size_t gated_kept(int dtype, int64_t tokens, int64_t hidden)
 {
-    return dtype == MG_F32 ? static_cast<size_t>(3 * tokens * hidden) * F : kept_scores(tokens, hidden) + held_rows(tokens, hidden);
+    return dtype == MG_F32 ? static_cast<size_t>(3 * tokens * hidden) * F : kept_front(dtype, tokens, hidden) + held_rows(tokens, hidden);
 }
 
 size_t gated_workspace(int dtype, int64_t tokens, int64_t width, int64_t hidden, bool backward)

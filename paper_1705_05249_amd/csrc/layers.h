@@ -16,7 +16,7 @@ __host__ __device__ inline int64_t padded(int64_t v) { return (v + LAYER_PIECE -
 // What becomes of the sums
 enum LinearEnd {
     END_STORE = 0,          // C in the operands' type, its rows in one matrix or two, or slices of FP32 sums
-    END_GATED = 1,          // Q is gate and up weights, 16 rows of each in turn: H = act(G) * U, and G and U for the backward pass
+    END_GATED = 1,          // Q is gate and up weights, 16 rows of each in turn: H = act(G) * U, and what the backward pass needs of G and U
     END_GATED_GRAD = 2,     // the sums are dH: dG and dU beside each other
     END_SCORES = 3,         // the sums are logits: largest one and sum of exponentials of a tile's columns, the target's logit
     END_SCORES_GRAD = 4     // the sums are logits: dz
@@ -42,7 +42,7 @@ struct LinearArgs {
     int64_t partial_ld, partial_stride;
     const float *scale;         // END_STORE: device scalar that every result is multiplied with; null: 1
     int activation;
-    float *kept;                // END_GATED (null: nothing is kept), END_GATED_GRAD: see kept_at
+    void *kept;                 // END_GATED (null: nothing is kept), END_GATED_GRAD: see kept_block
     // END_SCORES, END_SCORES_GRAD: columns are the vocabulary's from `first` on
     int64_t first, vocab;
     const int64_t *targets;
@@ -53,10 +53,13 @@ struct LinearArgs {
     const float *weight_scale;  // device scalar beside the weights; null: 1
 };
 
-// G and U as a block keeps them: 16 x 16 blocks in the order in which a matrix instruction leaves them (lane l: row l % 16, columns 4 (l / 16) .. + 3),
-// G's block in front of U's.  A wavefront moves a block as 1 KB on end.
+// What a block keeps of 16-bit types for its backward pass: a = act(G) and b = U act'(G), of which dU = dH a and dG = dH b, in blocks of 16 x 16 in the order in which a
+// matrix instruction leaves them (lane l: row l % 16, columns 4 (l / 16) .. + 3): a wavefront moves a block on end.  FP16: FP32 numbers.  bfloat16: FP16
+// numbers with a power of two for every four of a row, which have 11 bits, three more than dG and dU are rounded to afterwards, whatever the range (bfloat16 would
+// add as much error as that rounding), in 1152 bytes instead of 2048.
 __host__ __device__ inline int64_t kept_blocks(int64_t hidden) { return (hidden + 15) / 16; }
-__host__ __device__ inline int64_t kept_at(int64_t row, int64_t col, int64_t hidden) { return ((row / 16) * kept_blocks(hidden) + col / 16) * 512; }
+__host__ __device__ inline int64_t kept_block(int64_t row, int64_t col, int64_t hidden) { return (row / 16) * kept_blocks(hidden) + col / 16; }
+constexpr int kept_block_bytes(int dtype) { return dtype == MG_BF16 ? 1024 + 128 : 2048; }
 
 // Which of P and Q lie along the sum
 enum LinearForm { FORM_KK = 0, FORM_KN = 1, FORM_NN = 2 };       // both; P along, Q across; both across

@@ -56,74 +56,121 @@ template <typename T> __device__ inline void end_stage(char *at, float a, float 
     else *reinterpret_cast<Four<T> *>(at) = Four<T>{{static_cast<T>(a), static_cast<T>(b), static_cast<T>(c), static_cast<T>(d)}};
 }
 
-// Whether the activation's derivative is formed
-template <int ACT, typename T, bool GRAD, int FM, int FN>
-__device__ __forceinline__ void end_gated(const LinearArgs &args, const end_floatx4 (&acc)[FN][FM], char *region, int row0, int col0, int lane)
+// A block of a and b of what is kept (kept_block), this lane's four of each.  bfloat16: 16 bytes a lane, then the lanes' exponents.
+template <typename T> __device__ inline void keep(void *kept, int64_t block, int lane, const float (&a)[4], const float (&b)[4])
 {
-    const int held = (args.hidden + 15) / 16 * 16;              // columns of H, dG and dU that are written: zeros from `hidden` on
-    T *const C = static_cast<T *>(args.C0);
-    if constexpr (!GRAD) {
-        constexpr int HALF = FM / 2, ROWB = HALF * 32 + 16;
-        const int out0 = col0 / 2;
+    if constexpr (std::is_same_v<T, bfloat>) {
+        char *const at = static_cast<char *>(kept) + block * kept_block_bytes(MG_BF16);
+        // the largest of four goes to 2^14 .. 2^15 (an infinity stays one)
+        auto shift = [](const float (&v)[4]) {
+            const int e = __builtin_amdgcn_frexp_expf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+            return 15 - e < 126 ? 15 - e : 126;
+        };
+        const int ka = shift(a), kb = shift(b);
+        Four<_Float16> x, y;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int row = row0 + 16 * j;
-            end_fence();
+        for (int e = 0; e < 4; ++e) {
+            x.v[e] = static_cast<_Float16>(ldexpf(a[e], ka));
+            y.v[e] = static_cast<_Float16>(ldexpf(b[e], kb));
+        }
+        const uint64_t both[2] = {__builtin_bit_cast(uint64_t, x), __builtin_bit_cast(uint64_t, y)};
+        *reinterpret_cast<end_floatx4 *>(at + 16 * lane) = __builtin_bit_cast(end_floatx4, both);
+        *reinterpret_cast<uint16_t *>(at + 1024 + 2 * lane) = static_cast<uint16_t>((ka & 0xff) | (kb & 0xff) << 8);
+    } else {
+        float *const at = reinterpret_cast<float *>(static_cast<char *>(kept) + block * kept_block_bytes(MG_F16)) + 4 * lane;
+        *reinterpret_cast<end_floatx4 *>(at) = end_floatx4{a[0], a[1], a[2], a[3]};
+        *reinterpret_cast<end_floatx4 *>(at + 256) = end_floatx4{b[0], b[1], b[2], b[3]};
+    }
+}
+template <typename T> __device__ inline void recall(const void *kept, int64_t block, int lane, float (&a)[4], float (&b)[4])
+{
+    if constexpr (std::is_same_v<T, bfloat>) {
+        const char *const at = static_cast<const char *>(kept) + block * kept_block_bytes(MG_BF16);
+        struct Both {
+            Four<_Float16> x, y;
+        };
+        const Both v = __builtin_bit_cast(Both, *reinterpret_cast<const end_floatx4 *>(at + 16 * lane));
+        const uint16_t k = *reinterpret_cast<const uint16_t *>(at + 1024 + 2 * lane);
+        const int ka = static_cast<int8_t>(k & 0xff), kb = static_cast<int8_t>(k >> 8);
 #pragma unroll
-            for (int i = 0; i < HALF; ++i) {
-                const end_floatx4 g = acc[j][2 * i], u = acc[j][2 * i + 1];
-                if (args.kept != nullptr && row < args.rows && out0 + 16 * i < held) {
-                    float *const to = args.kept + kept_at(row, out0 + 16 * i, args.hidden) + 4 * lane;
-                    *reinterpret_cast<end_floatx4 *>(to) = g;
-                    *reinterpret_cast<end_floatx4 *>(to + 256) = u;
-                }
-                float h[4], slope;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    activation_of<ACT>(g[e], h[e], slope);
-                    h[e] *= u[e];
-                }
-                end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, h[0], h[1], h[2], h[3]);
-            }
-            end_fence();
-            end_drain<T, HALF * 16>(region, ROWB, row, out0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
+        for (int e = 0; e < 4; ++e) {
+            a[e] = ldexpf(static_cast<float>(v.x.v[e]), -ka);
+            b[e] = ldexpf(static_cast<float>(v.y.v[e]), -kb);
         }
     } else {
-        constexpr int ROWB = FM * 32 + 16;
-        const int64_t beside = args.ldc0 / 2;                   // dU's columns behind dG's
+        const float *const at = reinterpret_cast<const float *>(static_cast<const char *>(kept) + block * kept_block_bytes(MG_F16)) + 4 * lane;
+        const end_floatx4 x = *reinterpret_cast<const end_floatx4 *>(at), y = *reinterpret_cast<const end_floatx4 *>(at + 256);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int row = row0 + 16 * j;
-            Four<T> du[FM];
-            end_fence();
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const int col = col0 + 16 * i;
-                float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-                if (row < args.rows && col < held) {
-                    const float *const from = args.kept + kept_at(row, col, args.hidden) + 4 * lane;
-                    const end_floatx4 g = *reinterpret_cast<const end_floatx4 *>(from), u = *reinterpret_cast<const end_floatx4 *>(from + 256);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float h, slope;
-                        activation_of<ACT>(g[e], h, slope);
-                        // (columns behind the last one are sums of whatever lies behind the rows of WD)
-                        const bool there = col + 4 * (lane / 16) + e < args.hidden;
-                        a[e] = there ? acc[j][i][e] * u[e] * slope : 0.f;
-                        b[e] = there ? acc[j][i][e] * h : 0.f;
-                    }
-                }
-                end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, a[0], a[1], a[2], a[3]);
-                du[i] = Four<T>{{static_cast<T>(b[0]), static_cast<T>(b[1]), static_cast<T>(b[2]), static_cast<T>(b[3])}};
-            }
-            end_fence();
-            end_drain<T, FM * 16>(region, ROWB, row, col0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
-            end_fence();
-#pragma unroll
-            for (int i = 0; i < FM; ++i) *reinterpret_cast<Four<T> *>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8) = du[i];
-            end_fence();
-            end_drain<T, FM * 16>(region, ROWB, row, col0, args.rows, held, lane, [&](int r) { return C + beside + r * args.ldc0; });
+        for (int e = 0; e < 4; ++e) {
+            a[e] = x[e];
+            b[e] = y[e];
         }
+    }
+}
+
+// Columns of H, dG and dU that are written: zeros from `hidden` on
+__device__ inline int held_columns(int hidden) { return (hidden + 15) / 16 * 16; }
+
+template <int ACT, typename T, int FM, int FN> __device__ __forceinline__ void end_gated(const LinearArgs &args, const end_floatx4 (&acc)[FN][FM], char *region, int row0, int col0, int lane)
+{
+    constexpr int HALF = FM / 2, ROWB = HALF * 32 + 16;
+    const int out0 = col0 / 2, held = held_columns(args.hidden);
+    T *const C = static_cast<T *>(args.C0);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int row = row0 + 16 * j;
+        end_fence();
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) {
+            const end_floatx4 g = acc[j][2 * i], u = acc[j][2 * i + 1];
+            float a[4], b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float slope;
+                activation_of<ACT>(g[e], a[e], slope);
+                b[e] = u[e] * slope;
+            }
+            if (args.kept != nullptr && row < args.rows && out0 + 16 * i < held) keep<T>(args.kept, kept_block(row, out0 + 16 * i, args.hidden), lane, a, b);
+            end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, a[0] * u[0], a[1] * u[1], a[2] * u[2], a[3] * u[3]);
+        }
+        end_fence();
+        end_drain<T, HALF * 16>(region, ROWB, row, out0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
+    }
+}
+
+template <typename T, int FM, int FN> __device__ __forceinline__ void end_gated_grad(const LinearArgs &args, const end_floatx4 (&acc)[FN][FM], char *region, int row0, int col0, int lane)
+{
+    constexpr int ROWB = FM * 32 + 16;
+    const int held = held_columns(args.hidden);
+    T *const C = static_cast<T *>(args.C0);
+    const int64_t beside = args.ldc0 / 2;                   // dU's columns behind dG's
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+        const int row = row0 + 16 * j;
+        Four<T> du[FM];
+        end_fence();
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int col = col0 + 16 * i;
+            float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
+            if (row < args.rows && col < held) recall<T>(args.kept, kept_block(row, col, args.hidden), lane, a, b);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // (columns behind the last one are sums of whatever lies behind the rows of WD)
+                const bool there = col + 4 * (lane / 16) + e < args.hidden;
+                a[e] = there ? acc[j][i][e] * a[e] : 0.f;
+                b[e] = there ? acc[j][i][e] * b[e] : 0.f;
+            }
+            end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, b[0], b[1], b[2], b[3]);
+            du[i] = Four<T>{{static_cast<T>(a[0]), static_cast<T>(a[1]), static_cast<T>(a[2]), static_cast<T>(a[3])}};
+        }
+        end_fence();
+        end_drain<T, FM * 16>(region, ROWB, row, col0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
+        end_fence();
+#pragma unroll
+        for (int i = 0; i < FM; ++i) *reinterpret_cast<Four<T> *>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8) = du[i];
+        end_fence();
+        end_drain<T, FM * 16>(region, ROWB, row, col0, args.rows, held, lane, [&](int r) { return C + beside + r * args.ldc0; });
     }
 }
 
@@ -171,12 +218,13 @@ __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (
                 if ((other ? args.C1 : args.C0) != nullptr) end_drain<T, FM * 16>(region, ROWB, row, col0, rows, args.cols, lane, [&](int r) { return C + r * ldc; });
             }
         }
-    } else if constexpr (END == END_GATED || END == END_GATED_GRAD) {
-        constexpr bool GRAD = END == END_GATED_GRAD;
-        if (args.activation == MG_ACT_SILU) end_gated<MG_ACT_SILU, T, GRAD>(args, acc, region, row0, col0, lane);
-        else if (args.activation == MG_ACT_GELU) end_gated<MG_ACT_GELU, T, GRAD>(args, acc, region, row0, col0, lane);
-        else if (args.activation == MG_ACT_GELU_TANH) end_gated<MG_ACT_GELU_TANH, T, GRAD>(args, acc, region, row0, col0, lane);
-        else end_gated<MG_ACT_RELU2, T, GRAD>(args, acc, region, row0, col0, lane);
+    } else if constexpr (END == END_GATED) {
+        if (args.activation == MG_ACT_SILU) end_gated<MG_ACT_SILU, T>(args, acc, region, row0, col0, lane);
+        else if (args.activation == MG_ACT_GELU) end_gated<MG_ACT_GELU, T>(args, acc, region, row0, col0, lane);
+        else if (args.activation == MG_ACT_GELU_TANH) end_gated<MG_ACT_GELU_TANH, T>(args, acc, region, row0, col0, lane);
+        else end_gated<MG_ACT_RELU2, T>(args, acc, region, row0, col0, lane);
+    } else if constexpr (END == END_GATED_GRAD) {
+        end_gated_grad<T>(args, acc, region, row0, col0, lane);
     } else if constexpr (END == END_SCORES) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {

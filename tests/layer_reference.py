@@ -65,8 +65,12 @@ def block(x, wg, wu, wd, kind, dtype, dy=None):
     dy = dy.double()
     dh, edh = product(dy, zero(dy), wd, zero(wd))
     es = curve * eg + fine * (1 + g.abs()) * (slope.abs() + 0.1)
-    dg, du = dh * u * slope, dh * a
-    edg = edh * (u * slope).abs() + (dh.abs() + edh) * (eu * slope.abs() + (u.abs() + eu) * es) + 3 * STEP * dg.abs()
+    b = u * slope
+    eb = eu * slope.abs() + (u.abs() + eu) * es + 2 * STEP * b.abs()
+    if dtype == torch.bfloat16:                                   # kept with 11 bits, and an exponent for four
+        ea, eb = (e + 2.0 ** -11 * (v.abs() + e) + 2.0 ** -38 * (v.abs() + e).amax() for v, e in ((a, ea), (b, eb)))
+    dg, du = dh * b, dh * a
+    edg = edh * b.abs() + (dh.abs() + edh) * eb + 3 * STEP * dg.abs()
     edu = edh * a.abs() + (dh.abs() + edh) * ea + 3 * STEP * du.abs()
     edg, edu = rounded(dg, edg, dtype), rounded(du, edu, dtype)
     d, ed = torch.cat((dg, du), 1), torch.cat((edg, edu), 1)
