@@ -6,7 +6,8 @@
  * host or synchronised, every call only enqueues kernels on `stream`, arguments are checked on the host before any GPU work, errors are
  * negative status codes, the errors of smaller magnitude come first.  Matrices are row-major: element (r, c) at X[r*ld + c]; any address
  * that is a multiple of an element's size and any leading dimension that holds a row will do.  dtype is MG_F32, MG_F16 or MG_BF16, for
- * all matrices of a call.  Results do not depend on timing: the same call gives the same bits.  A result may not overlap what the call reads.
+ * all matrices of a call.  Results do not depend on timing: the same call gives the same bits.  A result may not
+ * overlap what the call reads, nor another result.
  *
  * Sums are in FP32 (MG_F32: as mg_sgemm's).  With 16-bit types a number is rounded to dtype where it becomes an operand of the next product
  * (H, dG and dU of a block, dz of the loss) and where it is a result; activations and exponentials are in FP32, and so is what a block keeps for its
@@ -80,9 +81,10 @@ size_t mg_vocab_loss_workspace_bytes(int dtype, int64_t tokens, int64_t width, i
 /* Gradients of sum over t of weights[t] * loss[t], from the lse that mg_vocab_loss wrote:
  *     dz(t, v) = weights[t] * (exp(z(t, v) - lse[t]) - (v == targets[t])),  0 for ignored targets
  *     dX = dz W,  dW = dz^T X
- * weights: FP32 device array of tokens (a mean over `count` tokens has 1/count in it, and a loss scale; a token of weight zero adds nothing), NULL: 1.
+ * weights: FP32 device array of tokens (a mean over `count` tokens has 1/count in it, and a loss scale), NULL: 1.  A token that is ignored or has weight zero adds
+ * nothing, whatever its row of X holds, infinities and NaN among it; its row of dX is zero.
  * dz exists for a piece of the vocabulary at a time, in the workspace.  dX or dW may be NULL.  No tokens: dW becomes zero; vocab == 0: dX.
- * MG_F16: dz is scaled by a power of two that the largest weight gives, so that small probabilities keep their bits.
+ * 16 bits: dz is rounded in units of the largest weight (MG_F16: of 2^-13 of it), so that equal weights cost no bits and small probabilities keep theirs.
  * Errors: as above, MG_ERR_LDC (lddx, lddw). */
 mg_status mg_vocab_loss_grad(int dtype, int64_t tokens, int64_t width, int64_t vocab, const void *X, int64_t ldx, const void *W, int64_t ldw,
                              const int64_t *targets, const float *lse, const float *weights, void *dX, int64_t lddx, void *dW, int64_t lddw,

@@ -160,7 +160,6 @@ struct Operand {
 };
 
 // Operands that the direct-to-LDS kernels do not take as they are get a copy while the workspace has room.  `along`: the operand lies along a sum.
-// Copies read and write what a product of few tokens reads once (333 tokens: the any-address kernels would take longer by far).
 class Copies {
   public:
     Copies(Arena &ws, bool wanted) : ws_(ws), wanted_(wanted) {}
@@ -181,13 +180,15 @@ class Copies {
     LinearCopies list_{};
 };
 
-constexpr int64_t COPY_TOKENS = 128;              // from here on operands are copied
+// A forward pass of few tokens reads its weights once, wherever their rows start; all else is faster with copies (width 1000, hidden 2000, rows at odd elements, without and
+// with copies: 33 tokens forward 38 and 25 us, backward 75 and 45; 1024 tokens 73 and 38, 232 and 77).
+bool copies_pay(int64_t tokens, bool backward) { return backward || tokens > LINEAR_FEW_ROWS; }
 size_t copy_bytes(int64_t rows, int64_t cols) { return (static_cast<size_t>(rows * padded(cols)) * 2 + 255) / 256 * 256; }
 
 // what dense operands need
 size_t copies_room(int64_t tokens, int64_t width, int64_t hidden, bool backward)
 {
-    if (tokens < COPY_TOKENS) return 0;
+    if (!copies_pay(tokens, backward)) return 0;
     size_t room = 0;
     if (width % 8 != 0) room += copy_bytes(tokens, width) * (backward ? 2 : 1) + 2 * copy_bytes(hidden, width);
     if (hidden % 8 != 0) room += copy_bytes(width, hidden);
@@ -211,7 +212,7 @@ mg_status forward_16(const GatedProblem &p)
     void *const H = p.kept != nullptr ? static_cast<char *>(p.kept) + kept_front(p.dtype, p.tokens, p.hidden) : ws.take(held_rows(p.tokens, p.hidden));
     const size_t wanted = forward_room(p.tokens, p.width, p.hidden), room_bytes = wanted < ws.left() ? wanted : ws.left();
     void *const room = ws.take(room_bytes);
-    Copies copied(ws, p.tokens >= COPY_TOKENS);
+    Copies copied(ws, copies_pay(p.tokens, false));
     const Operand x = copied(p.X, p.ldx, p.tokens, p.width, true), wg = copied(p.WG, p.ldwg, p.hidden, p.width, true), wu = copied(p.WU, p.ldwu, p.hidden, p.width, true),
                   wd = copied(p.WD, p.ldwd, p.width, p.hidden, true);
     if (const hipError_t e = copied.launch(p.stream)) return launched(e);
@@ -239,7 +240,7 @@ mg_status backward_16(const GatedProblem &p)
     const size_t wanted = backward_room(p.tokens, p.width, p.hidden), room_bytes = wanted < ws.left() ? wanted : ws.left();
     void *const room = ws.take(room_bytes);
     const bool inner = p.dX != nullptr || p.dWG != nullptr || p.dWU != nullptr, gates = p.dWG != nullptr || p.dWU != nullptr;
-    Copies copied(ws, p.tokens >= COPY_TOKENS);
+    Copies copied(ws, copies_pay(p.tokens, true));
     const Operand none{nullptr, 0, false};
     const Operand dy = copied(p.dY, p.lddy, p.tokens, p.width, inner), x = gates ? copied(p.X, p.ldx, p.tokens, p.width, false) : none,
                   wd = inner ? copied(p.WD, p.ldwd, p.width, p.hidden, false) : none, wg = p.dX != nullptr ? copied(p.WG, p.ldwg, p.hidden, p.width, false) : none,

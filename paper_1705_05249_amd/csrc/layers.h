@@ -92,7 +92,7 @@ hipError_t launch_linear(int dtype, int form, int end, LinearArgs args, void *ro
 // bytes of room with which a product of aligned operands takes its preferred number of slices
 size_t linear_room(int form, int end, int64_t rows, int64_t cols, int64_t k);
 
-// Copies of 16-bit matrices whose rows do not start on 16 bytes, or end inside a piece along a sum: rows x padded(cols), zeros behind the columns
+// Copies of matrices of 16-bit units whose rows do not start on 16 bytes, or end inside a piece along a sum: rows x padded(cols), zeros behind the columns
 struct LinearCopies {
     const void *from[6];
     void *to[6];
@@ -101,6 +101,12 @@ struct LinearCopies {
     int64_t rows[6];
     uint32_t begin[7];               // first work-group
     int count;
+    // the gradient of the loss (targets null: other callers): rows of matrix 0 are tokens, and zeros where the token's target is no row of the vocabulary or its weight
+    // is zero; scale (or null): what dz is scaled with, see weight_scale
+    const int64_t *targets;
+    int64_t vocab;
+    const float *weights;
+    float most, *scale;
 };
 hipError_t launch_linear_copies(LinearCopies copies, hipStream_t stream);
 

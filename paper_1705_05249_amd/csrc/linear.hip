@@ -5,9 +5,44 @@
 namespace mg {
 namespace {
 
-// A thread moves a piece of eight elements.
+// scale[0] = most / (the largest weight), scale[1] its inverse: what dz is multiplied with while it is an operand in 16 bits, and its products with afterwards.
+// Where all weights are alike, as in a mean, dz then is p - [target] itself, whose -1 of an unlikely target is exact (1 / count is not: off by up to half a
+// step in every token, where it is the largest part of dz).  FP16: most = 2^13, an eighth of the largest number; probabilities down to 2^-27 stay normal.
+__device__ inline void weight_scale(const float *weights, int64_t tokens, float most, float *scale)
+{
+    __shared__ uint32_t parts[4];
+    uint32_t largest = weights == nullptr ? 0x3f800000u : 0u;
+    if (weights != nullptr) {
+        // (eight at a time: a load behind the other would be 0.5 us each)
+        for (int64_t t = threadIdx.x; t < tokens; t += 8 * 256) {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = t + 256 * e < tokens ? __builtin_bit_cast(uint32_t, weights[t + 256 * e]) & 0x7fffffffu : 0u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) largest = w[e] < 0x7f800000u && w[e] > largest ? w[e] : largest;
+        }
+    }
+    for (int d = 32; d > 0; d /= 2) {
+        const uint32_t other = __shfl_xor(largest, d);
+        largest = other > largest ? other : largest;
+    }
+    if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = largest;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < 4; ++w) largest = parts[w] > largest ? parts[w] : largest;
+    // (weights beyond 2^100 either way: the scale and its inverse have to be normal numbers)
+    const float w = fminf(fmaxf(__builtin_bit_cast(float, largest), 0x1p-100f), 0x1p100f);
+    scale[0] = largest == 0 ? 1.f : most / w;
+    scale[1] = largest == 0 ? 1.f : w / most;
+}
+
+// A thread moves a piece of eight elements; the work-group behind the last matrix makes the scale.
 __global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
 {
+    if (blockIdx.x >= c.begin[c.count]) {
+        weight_scale(c.weights, c.rows[0], c.most, c.scale);
+        return;
+    }
     int m = 0;
     while (m + 1 < c.count && blockIdx.x >= c.begin[m + 1]) ++m;
     const int64_t piece = (blockIdx.x - c.begin[m]) * int64_t(256) + threadIdx.x;
@@ -15,13 +50,19 @@ __global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
     const int64_t row = piece / per_row;
     if (row >= c.rows[m]) return;
     const int col = static_cast<int>(piece - row * per_row) * 8;
+    int left = cols - col;
+    if (m == 0 && c.targets != nullptr) {
+        // nothing times an infinity is no number: a token that does not count must not reach the sums over tokens
+        const int64_t target = c.targets[row];
+        if (target < 0 || target >= c.vocab || (c.weights != nullptr && c.weights[row] == 0.f)) left = 0;
+    }
     const uint16_t *from = static_cast<const uint16_t *>(c.from[m]) + row * c.ld[m] + col;
     Piece<uint16_t, 8> x;
-    if (cols - col >= 8) {
+    if (left >= 8) {
         x = *reinterpret_cast<const Piece<uint16_t, 8> *>(from);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x.v[e] = e < cols - col ? from[e] : uint16_t(0);
+        for (int e = 0; e < 8; ++e) x.v[e] = e < left ? from[e] : uint16_t(0);
     }
     *reinterpret_cast<end_floatx4 *>(static_cast<uint16_t *>(c.to[m]) + row * padded(cols) + col) = __builtin_bit_cast(end_floatx4, x);
 }
@@ -59,7 +100,7 @@ hipError_t launch_linear_copies(LinearCopies c, hipStream_t stream)
     if (c.count == 0) return hipSuccess;
     c.begin[0] = 0;
     for (int m = 0; m < c.count; ++m) c.begin[m + 1] = c.begin[m] + static_cast<uint32_t>(ceil_div(c.rows[m] * (padded(c.cols[m]) / 8), 256));
-    copy_kernel<<<c.begin[c.count], 256, 0, stream>>>(c);
+    copy_kernel<<<c.begin[c.count] + (c.scale != nullptr ? 1 : 0), 256, 0, stream>>>(c);
     return hipGetLastError();
 }
 

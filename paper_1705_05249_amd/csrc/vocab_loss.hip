@@ -105,32 +105,6 @@ template <int TOKENS> __global__ __launch_bounds__(256) void join_scores_kernel(
     loss[row] = target >= 0 && target < vocab ? total - target_score[row] : 0.f;
 }
 
-// scale[0] = most / (the largest weight), scale[1] its inverse: what dz is multiplied with while it is an operand in 16 bits, and its products with afterwards.
-// Where all weights are alike, as in a mean, dz then is p - [target] itself, whose -1 of an unlikely target is exact (1 / count is not: off by up to half a
-// step in every token, where it is the largest part of dz).  FP16: most = 2^13, an eighth of the largest number; probabilities down to 2^-27 stay normal.
-__global__ __launch_bounds__(1024) void weight_scale_kernel(const float *weights, int tokens, float most, float *scale)
-{
-    __shared__ uint32_t parts[16];
-    uint32_t largest = weights == nullptr ? 0x3f800000u : 0u;
-    if (weights != nullptr)
-        for (int t = threadIdx.x; t < tokens; t += 1024) {
-            const uint32_t w = __builtin_bit_cast(uint32_t, weights[t]) & 0x7fffffffu;
-            largest = w < 0x7f800000u && w > largest ? w : largest;
-        }
-    for (int d = 32; d > 0; d /= 2) {
-        const uint32_t other = __shfl_xor(largest, d);
-        largest = other > largest ? other : largest;
-    }
-    if (threadIdx.x % 64 == 0) parts[threadIdx.x / 64] = largest;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 1; w < 16; ++w) largest = parts[w] > largest ? parts[w] : largest;
-    // (weights beyond 2^100 either way: the scale and its inverse have to be normal numbers)
-    const float w = fminf(fmaxf(__builtin_bit_cast(float, largest), 0x1p-100f), 0x1p100f);
-    scale[0] = largest == 0 ? 1.f : most / w;
-    scale[1] = largest == 0 ? 1.f : w / most;
-}
-
 // FP32: how many scores a token has when the vocabulary goes in pieces
 int64_t score_chunks(int64_t vocab, int64_t columns) { return vocab / columns * ceil_div(columns, CHUNK) + ceil_div(vocab % columns, CHUNK); }
 
@@ -158,6 +132,8 @@ LossMemory loss_memory(Arena &ws, int dtype, int64_t tokens, int64_t vocab)
 }
 
 struct LossGradMemory {
+    void *x;                               // X without the tokens that do not count, rows of x_lead elements
+    int64_t x_lead;
     void *dz;                              // a piece
     float *scale;
     float *slices;
@@ -173,6 +149,9 @@ LossGradMemory loss_grad_memory(Arena &ws, int dtype, int64_t tokens, int64_t wi
     LossGradMemory m{};
     const int64_t columns = piece_columns(dtype, tokens, vocab), count = ceil_div(vocab, columns);
     m.scale = static_cast<float *>(ws.take(2 * F));
+    const int64_t units = dtype == MG_F32 ? 2 : 1;               // of 16 bits
+    m.x = ws.take(tokens * padded(width * units) * 2);
+    m.x_lead = padded(width * units) / units;
     m.dz = ws.take(tokens * padded(columns) * (dtype == MG_F32 ? 4 : 2));
     m.slice = tokens * padded(width);
     if (dtype != MG_F32) {
@@ -208,6 +187,43 @@ size_t sgemm_room(int64_t tokens, int64_t width, int64_t vocab, bool gradient)
 
 const float *row_of(const void *X, int64_t row, int64_t ld) { return static_cast<const float *>(X) + row * ld; }
 
+// The loss alone reads W once; where it has rows at odd elements, copying it pays from about 192 tokens on (vocabulary of 32768, width 2048, without and with copies: 128 tokens
+// 75 and 74 us, 256 tokens 151 and 88).  The gradient reads it twice more: 33 tokens 210 and 154 us.
+bool copies_pay(int64_t tokens, bool gradient) { return gradient || tokens >= 192; }
+size_t copies_room(int64_t tokens, int64_t width, int64_t vocab, bool gradient)
+{
+    return width % 8 != 0 && copies_pay(tokens, gradient) ? static_cast<size_t>(((gradient ? 0 : tokens) + vocab) * padded(width)) * 2 + 512 : 0;
+}
+
+// The caller's matrices or copies of them
+struct LossOperands {
+    const void *X, *W;
+    int64_t ldx, ldw;
+    bool x_padded, w_padded;
+};
+
+// adds a copy to the list, where the direct-to-LDS kernels do not take a matrix along the sum as it is and there is room
+bool copy_of(LinearCopies &list, Arena &ws, const void *&at, int64_t &ld, int64_t rows, int64_t width)
+{
+    const size_t bytes = static_cast<size_t>(rows * padded(width)) * 2;
+    if ((width % 8 == 0 && reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 8 == 0) || ws.left() < bytes) return false;
+    const int m = list.count++;
+    list.from[m] = at; list.to[m] = ws.take(bytes); list.ld[m] = ld; list.rows[m] = rows; list.cols[m] = static_cast<int>(width);
+    at = list.to[m];
+    ld = padded(width);
+    return true;
+}
+
+// the copy of X without the tokens that do not count, first in a list; the scale
+void masked_copy(LinearCopies &list, const LossProblem &p, const LossGradMemory &m, float most, float *scale)
+{
+    const int units = p.dtype == MG_F32 ? 2 : 1;
+    list.count = 1;
+    list.from[0] = p.X; list.to[0] = m.x; list.ld[0] = p.ldx * units; list.rows[0] = p.tokens; list.cols[0] = static_cast<int>(p.width) * units;
+    list.targets = p.targets; list.vocab = p.vocab; list.weights = p.weights;
+    list.most = most; list.scale = scale;
+}
+
 mg_status loss_f32(const LossProblem &p, const LossMemory &m)
 {
     const int64_t columns = piece_columns(MG_F32, p.tokens, p.vocab);
@@ -229,10 +245,14 @@ mg_status grad_f32(const LossProblem &p, const LossGradMemory &m)
 {
     const int64_t columns = piece_columns(MG_F32, p.tokens, p.vocab);
     float *const Z = static_cast<float *>(m.dz);
+    const float *const X = static_cast<const float *>(m.x);
+    LinearCopies list{};
+    masked_copy(list, p, m, 1.f, nullptr);
+    if (const hipError_t e = launch_linear_copies(list, p.stream)) return launched(e);
     for (int64_t first = 0; first < p.vocab; first += columns) {
         const int64_t some = p.vocab - first < columns ? p.vocab - first : columns;
-        const float *W = row_of(p.W, first, p.ldw), *X = static_cast<const float *>(p.X);
-        mg_status st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_TRANS, p.tokens, some, p.width, 1.f, X, p.ldx, W, p.ldw, 0.f, Z, columns, m.rest, m.left, p.stream);
+        const float *W = row_of(p.W, first, p.ldw);
+        mg_status st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_TRANS, p.tokens, some, p.width, 1.f, X, m.x_lead, W, p.ldw, 0.f, Z, columns, m.rest, m.left, p.stream);
         if (st != MG_OK) return st;
         scores_grad_kernel<<<dim3(static_cast<uint32_t>(p.tokens), static_cast<uint32_t>(ceil_div(some, CHUNK))), 256, 0, p.stream>>>(Z, columns, static_cast<int>(some), first, p.vocab, p.targets, p.lse, p.weights);
         if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
@@ -240,49 +260,17 @@ mg_status grad_f32(const LossProblem &p, const LossGradMemory &m)
             st = mg_sgemm(MG_ROW_MAJOR, MG_NO_TRANS, MG_NO_TRANS, p.tokens, p.width, some, 1.f, Z, columns, W, p.ldw, first > 0 ? 1.f : 0.f, static_cast<float *>(p.dX), p.lddx, m.rest,
                           m.left, p.stream);
         if (st == MG_OK && p.dW != nullptr)
-            st = mg_sgemm(MG_ROW_MAJOR, MG_TRANS, MG_NO_TRANS, some, p.width, p.tokens, 1.f, Z, columns, X, p.ldx, 0.f, static_cast<float *>(p.dW) + first * p.lddw, p.lddw, m.rest, m.left,
+            st = mg_sgemm(MG_ROW_MAJOR, MG_TRANS, MG_NO_TRANS, some, p.width, p.tokens, 1.f, Z, columns, X, m.x_lead, 0.f, static_cast<float *>(p.dW) + first * p.lddw, p.lddw, m.rest, m.left,
                           p.stream);
         if (st != MG_OK) return st;
     }
     return MG_OK;
 }
 
-// The caller's matrices or copies of them (see Copies in gated.hip)
-struct LossOperands {
-    const void *X, *W;
-    int64_t ldx, ldw;
-    bool padded;
-};
-
-constexpr int64_t COPY_TOKENS = 128;
-size_t copies_room(int64_t tokens, int64_t width, int64_t vocab) { return width % 8 != 0 && tokens >= COPY_TOKENS ? static_cast<size_t>((tokens + vocab) * padded(width)) * 2 + 512 : 0; }
-
-hipError_t loss_operands(const LossProblem &p, Arena &ws, LossOperands &o)
-{
-    LinearCopies list{};
-    o = {p.X, p.W, p.ldx, p.ldw, false};
-    const bool whole = p.width % 8 == 0;
-    bool copied[2] = {false, false};
-    for (int n = 0; n < 2; ++n) {
-        const void *&at = n == 0 ? o.X : o.W;
-        int64_t &ld = n == 0 ? o.ldx : o.ldw;
-        const int64_t rows = n == 0 ? p.tokens : p.vocab;
-        const size_t bytes = static_cast<size_t>(rows * padded(p.width)) * 2;
-        if ((whole && reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 8 == 0) || p.tokens < COPY_TOKENS || ws.left() < bytes) continue;
-        const int m = list.count++;
-        list.from[m] = at; list.to[m] = ws.take(bytes); list.ld[m] = ld; list.rows[m] = rows; list.cols[m] = static_cast<int>(p.width);
-        at = list.to[m];
-        ld = padded(p.width);
-        copied[n] = true;
-    }
-    o.padded = copied[0] && copied[1];
-    return launch_linear_copies(list, p.stream);
-}
-
 LinearArgs logits(const LossProblem &p, const LossOperands &o, int64_t first, int64_t columns)
 {
     LinearArgs a{};
-    a.P = o.X; a.ldp = o.ldx; a.p_padded = a.q_padded = o.padded;
+    a.P = o.X; a.ldp = o.ldx; a.p_padded = o.x_padded; a.q_padded = o.w_padded;
     a.Q0 = static_cast<const uint16_t *>(o.W) + first * o.ldw; a.ldq0 = o.ldw;
     a.rows = static_cast<int>(p.tokens); a.cols = static_cast<int>(columns); a.k = static_cast<int>(p.width);
     a.first = first; a.vocab = p.vocab; a.targets = p.targets;
@@ -291,14 +279,12 @@ LinearArgs logits(const LossProblem &p, const LossOperands &o, int64_t first, in
 
 mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
 {
-    LossOperands o;
-    if (const hipError_t e = loss_operands(p, ws, o)) return launched(e);
-    const float *scale = nullptr;
-    if (p.weights != nullptr || p.dtype == MG_F16) {
-        weight_scale_kernel<<<1, 1024, 0, p.stream>>>(p.weights, static_cast<int>(p.tokens), p.dtype == MG_F16 ? 8192.f : 1.f, m.scale);
-        if (hipGetLastError() != hipSuccess) return MG_ERR_LAUNCH;
-        scale = m.scale;
-    }
+    LossOperands o{m.x, p.W, m.x_lead, p.ldw, true, false};
+    LinearCopies list{};
+    float *const scale = p.weights != nullptr || p.dtype == MG_F16 ? m.scale : nullptr;
+    masked_copy(list, p, m, p.dtype == MG_F16 ? 8192.f : 1.f, scale);
+    if (copies_pay(p.tokens, true)) o.w_padded = copy_of(list, ws, o.W, o.ldw, p.vocab, p.width);
+    if (const hipError_t e = launch_linear_copies(list, p.stream)) return launched(e);
     const int64_t columns = piece_columns(p.dtype, p.tokens, p.vocab), lead = padded(columns);
     const int count = static_cast<int>(ceil_div(p.vocab, columns));
     LinearArgs x{};                                        // dX
@@ -343,7 +329,7 @@ size_t loss_workspace(int dtype, int64_t tokens, int64_t width, int64_t vocab, b
     Arena ws{nullptr, 0, 0};
     if (gradient) loss_grad_memory(ws, dtype, tokens, width, vocab);
     else loss_memory(ws, dtype, tokens, vocab);
-    if (vocab > 0) ws.take(dtype == MG_F32 ? sgemm_room(tokens, width, vocab, gradient) : copies_room(tokens, width, vocab));
+    if (vocab > 0) ws.take(dtype == MG_F32 ? sgemm_room(tokens, width, vocab, gradient) : copies_room(tokens, width, vocab, gradient));
     return ws.used;
 }
 
@@ -356,8 +342,13 @@ mg_status vocab_loss(const LossProblem &p)
         if (const mg_status st = loss_f32(p, m)) return st;
         tiles = static_cast<int>(score_chunks(p.vocab, piece_columns(MG_F32, p.tokens, p.vocab)));
     } else if (p.vocab > 0) {
-        LossOperands o;
-        if (const hipError_t e = loss_operands(p, ws, o)) return launched(e);
+        LossOperands o{p.X, p.W, p.ldx, p.ldw, false, false};
+        LinearCopies list{};
+        if (copies_pay(p.tokens, false)) {
+            o.x_padded = copy_of(list, ws, o.X, o.ldx, p.tokens, p.width);
+            o.w_padded = copy_of(list, ws, o.W, o.ldw, p.vocab, p.width);
+        }
+        if (const hipError_t e = launch_linear_copies(list, p.stream)) return launched(e);
         LinearArgs a = logits(p, o, 0, p.vocab);
         a.scores = m.scores;
         a.target_score = m.target_score;

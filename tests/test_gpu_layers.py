@@ -241,11 +241,16 @@ def test_tokens_that_do_not_count_may_hold_anything():
         weights[5] = weights[6] = 0.0
         head = D.VocabLoss(w.to(kind).cuda())
         loss = head.forward(x.to(kind).cuda(), targets.cuda())
-        dx, _ = head.backward(weights.cuda())
+        dx, dw = head.backward(weights.cuda())
         fine = torch.ones(20, dtype=torch.bool)
         fine[[3, 5, 6]] = False
         assert bool(loss.cpu()[fine].isfinite().all()) and float(loss[3]) == 0.0
         assert bool(dx.cpu()[fine].isfinite().all()) and not bool(dx[[3, 5, 6]].any())
+        # the same as without them
+        x[[3, 5, 6]] = 0.0
+        head.forward(x.to(kind).cuda(), targets.cuda())
+        same_x, same_w = head.backward(weights.cuda())
+        assert torch.equal(dx, same_x) and torch.equal(dw, same_w)
 
 
 # sizes at which the large tiles are taken (tests/test_linear_plan.py says which by which product)
