@@ -4,6 +4,8 @@
 // (element (r, l) at P[r*ld + l]) or across it (at P[l*ld + r]); the results stay in registers until they have become what the operator stores.
 #pragma once
 
+#include <atomic>
+
 #include "experts.h"
 #include "../../include/mg_layers.h"
 
@@ -155,7 +157,7 @@ struct LossProblem {
 };
 size_t loss_workspace(int dtype, int64_t tokens, int64_t width, int64_t vocab, bool gradient);
 mg_status vocab_loss(const LossProblem &p);              // vocab may be zero, tokens not
-mg_status vocab_loss_grad(const LossProblem &p);         // sizes above zero but for width
+mg_status vocab_loss_grad(const LossProblem &p);         // sizes above zero
 
 struct ClipProblem {
     int64_t count;
@@ -171,6 +173,21 @@ struct ClipProblem {
 };
 size_t clip_workspace(int64_t count);
 hipError_t launch_clip(const ClipProblem &p);
+
+// Devices on which a kernel may take more than 64 KB of LDS: the limit belongs to a kernel on a device
+struct RaisedLds {
+    std::atomic<uint64_t> devices{0};
+    hipError_t operator()(const void *kernel, int bytes)
+    {
+        int device = 0;
+        if (const hipError_t e = hipGetDevice(&device)) return e;
+        const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+        if ((devices.load(std::memory_order_relaxed) & bit) != 0) return hipSuccess;
+        const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);      // (raising it twice is harmless)
+        if (e == hipSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
+        return e;
+    }
+};
 
 // zeros in a matrix (rows x cols elements of `size` bytes)
 hipError_t launch_zero_rows(void *X, int64_t rows, int64_t cols, int64_t ld, int size, hipStream_t stream);

@@ -34,7 +34,6 @@ bool loss_fits(int64_t tokens, int64_t width, int64_t vocab)
 
 Arena arena(void *workspace, size_t bytes) { return Arena{static_cast<char *>(workspace), bytes, 0}; }
 
-// what all gradients need: no tokens (or nothing behind the sum) makes zeros
 mg_status check_clip(const ClipProblem &p, size_t workspace_bytes)
 {
     if (p.count < 0 || p.count > MOST_TENSORS) return MG_ERR_DIM;

@@ -36,16 +36,19 @@ __device__ inline void weight_scale(const float *weights, int64_t tokens, float 
     scale[1] = largest == 0 ? 1.f : w / most;
 }
 
+constexpr uint32_t COPY_GROUPS = uint32_t(1) << 22;           // along x: a launch has fewer than 2^32 threads there, five matrices of 2^34 elements more pieces
+
 // A thread moves a piece of eight elements; the work-group behind the last matrix makes the scale.
 __global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
 {
-    if (blockIdx.x >= c.begin[c.count]) {
-        weight_scale(c.weights, c.rows[0], c.most, c.scale);
+    const uint32_t group = blockIdx.y * gridDim.x + blockIdx.x;
+    if (group >= c.begin[c.count]) {
+        if (group == c.begin[c.count] && c.scale != nullptr) weight_scale(c.weights, c.rows[0], c.most, c.scale);
         return;
     }
     int m = 0;
-    while (m + 1 < c.count && blockIdx.x >= c.begin[m + 1]) ++m;
-    const int64_t piece = (blockIdx.x - c.begin[m]) * int64_t(256) + threadIdx.x;
+    while (m + 1 < c.count && group >= c.begin[m + 1]) ++m;
+    const int64_t piece = (group - c.begin[m]) * int64_t(256) + threadIdx.x;
     const int cols = c.cols[m], per_row = static_cast<int>(padded(cols) / 8);
     const int64_t row = piece / per_row;
     if (row >= c.rows[m]) return;
@@ -100,7 +103,8 @@ hipError_t launch_linear_copies(LinearCopies c, hipStream_t stream)
     if (c.count == 0) return hipSuccess;
     c.begin[0] = 0;
     for (int m = 0; m < c.count; ++m) c.begin[m + 1] = c.begin[m] + static_cast<uint32_t>(ceil_div(c.rows[m] * (padded(c.cols[m]) / 8), 256));
-    copy_kernel<<<c.begin[c.count] + (c.scale != nullptr ? 1 : 0), 256, 0, stream>>>(c);
+    const uint32_t groups = c.begin[c.count] + (c.scale != nullptr ? 1 : 0), wide = groups < COPY_GROUPS ? groups : COPY_GROUPS;
+    copy_kernel<<<dim3(wide, (groups + wide - 1) / wide), 256, 0, stream>>>(c);
     return hipGetLastError();
 }
 

@@ -80,6 +80,7 @@ template <int ROWS, int NT, bool ALONG, bool GATED = false, bool ONCE = false> s
             rsrc = descriptor(X + r0 + l0 * ld, left < 64 ? left : 64, ld, rows);
             now[0] = second ? other[0] : goff[0];
             now[1] = second ? other[1] : goff[1];
+            step = static_cast<uint32_t>(4 * ld * 2);                               // (the matrices' rows need not be equally far apart)
         }
     }
     __device__ inline void aim_gated(const _Float16 *gate, int64_t ldg, const _Float16 *upper, int64_t ldu, int64_t feature, int64_t l0, int left, int features)
@@ -294,13 +295,9 @@ template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STA
 {
     constexpr int LDS = linear_dma_lds<BC, BR, WC, WR, STAGES>();
     static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
-    static bool raised = false;                   // raising the limit twice is harmless
+    static RaisedLds raised;
     auto kernel = linear_dma_kernel<T, FORM, END, BC, BR, WC, WR, STAGES>;
-    if (!raised) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-        if (e != hipSuccess) return e;
-        raised = true;
-    }
+    if (const hipError_t e = raised(reinterpret_cast<const void *>(kernel), LDS)) return e;
     args.tiles_c = (args.cols + BC - 1) / BC;
     args.tiles_r = (args.rows + BR - 1) / BR;
     kernel<<<dim3(static_cast<uint32_t>(args.tiles_c) * args.tiles_r, 1, slices), WC * WR * 64, LDS, stream>>>(args);

@@ -61,9 +61,12 @@ template <typename T> __device__ inline void keep(void *kept, int64_t block, int
 {
     if constexpr (std::is_same_v<T, bfloat>) {
         char *const at = static_cast<char *>(kept) + block * kept_block_bytes(MG_BF16);
-        // the largest of four goes to 2^14 .. 2^15 (an infinity stays one)
+        // the largest finite one of four goes to 2^14 .. 2^15 (infinities stay what they are)
         auto shift = [](const float (&v)[4]) {
-            const int e = __builtin_amdgcn_frexp_expf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+            float largest = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) largest = fmaxf(largest, fabsf(v[i]) < __builtin_inff() ? fabsf(v[i]) : 0.f);
+            const int e = __builtin_amdgcn_frexp_expf(largest);
             return 15 - e < 126 ? 15 - e : 126;
         };
         const int ka = shift(a), kb = shift(b);

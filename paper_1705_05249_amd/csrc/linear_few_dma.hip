@@ -109,13 +109,9 @@ template <typename T, int END, int FM, int FN, int W, int S, bool ONCE> hipError
 {
     constexpr int LDS = few_lds<FM, FN, W, S>();
     static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
-    static bool raised = false;                   // raising the limit twice is harmless
+    static RaisedLds raised;
     auto kernel = linear_few_dma_kernel<T, END, FM, FN, W, S, ONCE>;
-    if (!raised) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-        if (e != hipSuccess) return e;
-        raised = true;
-    }
+    if (const hipError_t e = raised(reinterpret_cast<const void *>(kernel), LDS)) return e;
     kernel<<<static_cast<uint32_t>(ceil_div(args.cols, FM * 16)), W * 64, LDS, stream>>>(args);
     return hipGetLastError();
 }

@@ -301,13 +301,9 @@ template <typename T, int FORM, int END> __global__ __launch_bounds__(512) void 
 
 template <typename T, int FORM, int END> hipError_t launch_linear_pp(LinearArgs args, int slices, hipStream_t stream)
 {
-    static bool raised = false;                   // raising the limit twice is harmless
+    static RaisedLds raised;
     auto kernel = linear_pp_kernel<T, FORM, END>;
-    if (!raised) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LINEAR_PP_LDS);
-        if (e != hipSuccess) return e;
-        raised = true;
-    }
+    if (const hipError_t e = raised(reinterpret_cast<const void *>(kernel), LINEAR_PP_LDS)) return e;
     args.tiles_c = (args.cols + 255) / 256;
     args.tiles_r = (args.rows + 255) / 256;
     kernel<<<dim3(static_cast<uint32_t>(args.tiles_c) * args.tiles_r, 1, slices), 512, LINEAR_PP_LDS, stream>>>(args);

@@ -7,7 +7,7 @@
 trains a block under a loss on tokens that another model has labelled, with clipped gradients, and prints loss, norm and the time of a step.  In the
 manner of expert_layer.py: outside autograd, `backward` gives the gradients; PyTorch holds the memory and makes the update, everything else runs in the
 library's kernels.  All buffers are allocated by the layers, on their weights' device, none by the library; the calls go to torch's current stream, so
-that device has to be the current one.
+that device has to be the current one.  What `forward` keeps (its inputs as they are, not copies of them) belongs to its stream: `backward` goes to the same one.
 """
 import sys
 
@@ -27,6 +27,8 @@ def _checked(name, tensor, shape, device, types):
         raise ValueError(f"{name}: shape {tuple(tensor.shape)}, expected {tuple(shape)}")
     if tensor.device != device or not tensor.is_cuda:
         raise ValueError(f"{name}: on {tensor.device}, expected on {device if device.type == 'cuda' else 'the GPU'}")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {device}, but the current device is cuda:{torch.cuda.current_device()}")
     tensor = tensor.detach()
     if tensor.dim() == 2 and tensor.numel() and (tensor.stride(1) != 1 or tensor.stride(0) < tensor.shape[1]):
         return tensor.contiguous()
@@ -101,7 +103,7 @@ class VocabLoss:
         x = _checked("x", x, (x.shape[0], self.width), w.device, (w.dtype,))
         targets = _checked("targets", targets, x.shape[:1], w.device, (torch.int64,))
         size = TYPES[w.dtype], x.shape[0], self.width, self.vocab
-        loss, lse = (torch.empty(x.shape[0], device=x.device) for _ in range(2))
+        loss, lse = (torch.empty(x.shape[0], dtype=torch.float32, device=x.device) for _ in range(2))
         L.mg_vocab_loss(*size, *_at(x), *_at(w), targets, loss, lse, _scratch(L.mg_vocab_loss_workspace_bytes(*size), x.device))
         self.kept = (x, targets, lse) if keep else None
         return loss
@@ -132,12 +134,17 @@ class Gradients:
                 raise ValueError(f"tensor {i}: on {t.device}, expected on {self.tensors[0].device if self.tensors[0].is_cuda else 'the GPU'}")
             if not t.is_contiguous():
                 raise ValueError(f"tensor {i}: not dense")
+        # (scaled in place, a number that is listed twice would be scaled twice)
+        places = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i) for i, t in enumerate(self.tensors) if t.numel())
+        for (_, end, i), (start, _, j) in zip(places, places[1:]):
+            if start < end:
+                raise ValueError(f"tensors {min(i, j)} and {max(i, j)} share memory")
         self.count = len(self.tensors)
         device = self.tensors[0].device if self.tensors else "cuda"
-        self.types = torch.tensor([TYPES[t.dtype] for t in self.tensors], dtype=torch.int32)
-        self.addresses = torch.tensor([t.data_ptr() for t in self.tensors], dtype=torch.int64)
-        self.sizes = torch.tensor([t.numel() for t in self.tensors], dtype=torch.int64)
-        self.value = torch.empty(1, device=device)
+        self.types = torch.tensor([TYPES[t.dtype] for t in self.tensors], dtype=torch.int32, device="cpu")
+        self.addresses = torch.tensor([t.data_ptr() for t in self.tensors], dtype=torch.int64, device="cpu")
+        self.sizes = torch.tensor([t.numel() for t in self.tensors], dtype=torch.int64, device="cpu")
+        self.value = torch.empty(1, dtype=torch.float32, device=device)
         self.workspace = _scratch(L.mg_gradient_workspace_bytes(self.count), device)
 
     def norm(self):
@@ -156,7 +163,7 @@ def train_step(block, head, x, targets, max_norm):
     y = x + block.forward(x)
     loss = head.forward(y, targets)
     counted = ((targets >= 0) & (targets < head.vocab)).sum().clamp(min=1)
-    dy, dhead = head.backward(torch.ones(len(loss), device=x.device) / counted)
+    dy, dhead = head.backward(torch.ones_like(loss) / counted)
     _, dgate, dup, ddown = block.backward(dy)
     grads = [dgate, dup, ddown, dhead]
     return loss, Gradients(grads).clip(max_norm), grads

@@ -60,18 +60,20 @@ BLOCKS = [(1, 1, 1), (1, 8, 16), (2, 64, 15), (3, 200, 129), (17, 33, 100), (64,
           (33, 96, 300), (5, 2056, 40)]
 
 
-def run_block(case, act, dtype, lead=0, extra=0, keep=True, backward=True, wanted=(True,) * 4, room="all"):
+def run_block(case, act, dtype, lead=0, extra=0, keep=True, backward=True, wanted=(True,) * 4, room=0):
+    """lead, extra: of every matrix, or one for each of X, WG, WU, WD, Y, dY and the four results; room: bytes of workspace beyond what the queries answer"""
     tokens, width, hidden = case
+    leads, extras = (v if isinstance(v, tuple) else (v,) * 10 for v in (lead, extra))
     code, kind = CODES[dtype], D.ACTIVATIONS[act]
     x, wg, wu, wd, dy = (t.to(dtype) for t in (normal(1, tokens, width), normal(2, hidden, width, sigma=width ** -0.5), normal(3, hidden, width, sigma=width ** -0.5),
                                                 normal(4, width, hidden, sigma=hidden ** -0.5), normal(5, tokens, width)))
     where = "cuda" if tokens * width * hidden > 1 << 24 else "cpu"
     want = R.block(*(t.to(where) for t in (x, wg, wu, wd)), act, dtype, dy.to(where))
-    held = [Held(t, lead, extra) for t in (x, wg, wu, wd)]
+    held = [Held(t, *at) for t, *at in zip((x, wg, wu, wd), leads, extras)]
     arguments = [v for h in held for v in h.at()]
-    y = result(tokens, width, dtype, lead, extra)
+    y = result(tokens, width, dtype, leads[4], extras[4])
     kept_all, kept = scratch(L.mg_gated_kept_bytes(code, *case)) if keep else (None, None)
-    ws_all, ws = scratch(L.mg_gated_forward_workspace_bytes(code, *case))
+    ws_all, ws = scratch(L.mg_gated_forward_workspace_bytes(code, *case) + room)
     L.mg_gated_forward(code, kind, *case, *arguments, *y.at(), kept, ws)
     torch.cuda.synchronize()
     R.check(y.x, want["y"], "y")
@@ -80,9 +82,10 @@ def run_block(case, act, dtype, lead=0, extra=0, keep=True, backward=True, wante
     if not backward:
         return
     before = kept.clone()
-    d = Held(dy, lead, extra)
-    outs = [result(*shape, dtype, lead, extra) if on else None for on, shape in zip(wanted, ((tokens, width), (hidden, width), (hidden, width), (width, hidden)))]
-    ws_all, ws = scratch(L.mg_gated_backward_workspace_bytes(code, *case))
+    d = Held(dy, leads[5], extras[5])
+    shapes = (tokens, width), (hidden, width), (hidden, width), (width, hidden)
+    outs = [result(*shape, dtype, *at) if on else None for on, shape, *at in zip(wanted, shapes, leads[6:], extras[6:])]
+    ws_all, ws = scratch(L.mg_gated_backward_workspace_bytes(code, *case) + room)
     L.mg_gated_backward(code, kind, *case, *arguments, *d.at(), kept, *(v for o in outs for v in (o.at() if o else (None, 0))), ws)
     torch.cuda.synchronize()
     for name, o in zip(("dx", "dwg", "dwu", "dwd"), outs):
@@ -111,6 +114,78 @@ def test_activations(act, dtype):
 @pytest.mark.parametrize("case", [(40, 72, 136), (33, 61, 75), (3, 264, 72)], ids=lambda c: "x".join(map(str, c)))
 def test_block_of_parts_of_larger_matrices(case, lead, extra, dtype):
     run_block(case, "gelu_tanh", KINDS[dtype], lead, extra)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("case", [(40, 72, 136), (300, 264, 520), (5, 136, 72)], ids=lambda c: "x".join(map(str, c)))
+def test_blocks_whose_matrices_lie_differently(case, dtype):
+    """every matrix has rows of its own distance, some of them off 16 bytes; with the workspace that the queries answer and with room for copies"""
+    for lead, extra in ((0, (8, 24, 16, 40, 64, 32, 72, 80, 8, 48)), ((0, 3, 0, 8, 1, 0, 5, 0, 2, 0), (8, 24, 3, 40, 1, 32, 72, 5, 8, 48))):
+        for room in (0, 1 << 22):
+            run_block(case, "silu", KINDS[dtype], lead, extra, room=room)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_large_blocks_whose_matrices_lie_differently(dtype):
+    """gate and up weights at different distances, on every tile that reads both in one sum"""
+    for case in ((1000, 1000, 2000), (2100, 4000, 520), (4000, 1500, 700), (1500, 2000, 1000)):
+        run_block(case, "gelu", KINDS[dtype], 0, (8, 24, 16, 40, 64, 32, 72, 80, 8, 48))
+
+
+@pytest.mark.parametrize("dtype,ld", [("bf16", 1 << 20), ("f16", (1 << 21) + 8), ("bf16", (1 << 20) + 1), ("f32", 1 << 20)])
+def test_rows_far_apart(dtype, ld):
+    """operands and results whose last rows are more than 2^32 bytes behind the first"""
+    kind = KINDS[dtype]
+    tokens, width, hidden, code = 2100, 2064, 2072, CODES[kind]
+    assert min(tokens, width, hidden) * ld * 2 > 1 << 32
+
+    def far(x):
+        room = torch.empty(x.shape[0] * ld, dtype=kind, device="cuda").view(-1, ld)[:, :x.shape[1]]
+        room.copy_(x)
+        return room
+    data = [normal(i, r, c, sigma=1.0 if i in (1, 5) else c ** -0.5).to(kind) for i, (r, c) in enumerate(((tokens, width), (hidden, width), (hidden, width), (width, hidden), (tokens, width)), 1)]
+    want = R.block(*(t.cuda() for t in data[:4]), "silu", kind, data[4].cuda())
+    x, wg, wu, wd, dy = (far(t) for t in data)
+    operands = [v for t in (x, wg, wu, wd) for v in (t.data_ptr(), ld)]
+    zeros = lambda rows, cols: far(torch.zeros(rows, cols, dtype=kind))  # noqa: E731
+    y = zeros(tokens, width)
+    size = code, tokens, width, hidden
+    kept = scratch(L.mg_gated_kept_bytes(*size))[1]
+    L.mg_gated_forward(code, L.MG_ACT_SILU, *size[1:], *operands, y, ld, kept, scratch(L.mg_gated_forward_workspace_bytes(*size))[1])
+    R.check(y, want["y"], "y")
+    outs = [zeros(*t.shape) for t in (x, wg, wu, wd)]
+    L.mg_gated_backward(code, L.MG_ACT_SILU, *size[1:], *operands, dy, ld, kept, *(v for o in outs for v in (o, ld)), scratch(L.mg_gated_backward_workspace_bytes(*size))[1])
+    for name, o in zip(("dx", "dwg", "dwu", "dwd"), outs):
+        R.check(o, want[name], name)
+    del want
+    targets = torch.randint(-1, hidden, (tokens,), generator=torch.Generator().manual_seed(3))
+    want = R.loss(data[0].cuda(), data[1].cuda(), targets.cuda(), kind, None, gradient=True)
+    loss, lse, target = torch.empty(tokens, device="cuda"), torch.empty(tokens, device="cuda"), targets.cuda()
+    for o in outs[:2]:
+        o.zero_()
+    L.mg_vocab_loss(*size, *operands[:4], target, loss, lse, scratch(L.mg_vocab_loss_workspace_bytes(*size))[1])
+    L.mg_vocab_loss_grad(*size, *operands[:4], target, lse, None, *(v for o in outs[:2] for v in (o, ld)), scratch(L.mg_vocab_loss_grad_workspace_bytes(*size))[1])
+    for name, o in (("loss", loss), ("lse", lse), ("dx", outs[0]), ("dw", outs[1])):
+        R.check(o, want[name], name)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+def test_infinities_stay_in_their_feature(dtype):
+    """what a block keeps of one feature does not depend on what another one's is"""
+    kind = KINDS[dtype]
+    x, dy = (normal(1, 20, 16).abs() * 2).to(kind), normal(2, 20, 16, sigma=0.1).to(kind)
+    weights = [normal(3, 40, 16).to(kind), normal(4, 40, 16).to(kind), normal(5, 16, 40).to(kind)]
+    grads = []
+    for largest in (False, True):
+        if largest:
+            weights[1][5] = torch.finfo(kind).max
+        block = D.GatedBlock(*(w.cuda() for w in weights))
+        block.forward(x.cuda())
+        grads.append([g.cpu() for g in block.backward(dy.cuda())])
+    others = torch.arange(40) != 5
+    (_, gate, up, down), (_, gate2, up2, down2) = grads
+    assert torch.equal(up, up2) and torch.equal(gate[others], gate2[others]) and torch.equal(down[:, others], down2[:, others])
+    assert not bool(gate2[5].isfinite().all()) and bool(gate.isfinite().all())
 
 
 @pytest.mark.parametrize("dtype", KINDS)
@@ -144,8 +219,10 @@ def test_blocks_without_work(dtype):
 LOSSES = [(1, 1, 1), (1, 8, 100), (2, 64, 65), (3, 33, 1000), (16, 256, 513), (17, 100, 64), (64, 72, 300), (70, 136, 1029), (130, 65, 200), (300, 264, 520), (257, 64, 257), (5, 1032, 4100)]
 
 
-def run_loss(case, dtype, lead=0, extra=0, weights="each", ignored=0.3, wanted=(True, True), sigma=2.0):
+def run_loss(case, dtype, lead=0, extra=0, weights="each", ignored=0.3, wanted=(True, True), sigma=2.0, room=0):
+    """lead, extra: of every matrix, or one for each of X, W, dX and dW"""
     tokens, width, vocab = case
+    leads, extras = (v if isinstance(v, tuple) else (v,) * 4 for v in (lead, extra))
     code = CODES[dtype]
     x, w = normal(1, tokens, width).to(dtype), normal(2, vocab, width, sigma=sigma * width ** -0.5).to(dtype)
     gen = torch.Generator().manual_seed(3)
@@ -156,18 +233,18 @@ def run_loss(case, dtype, lead=0, extra=0, weights="each", ignored=0.3, wanted=(
                      "zeros": torch.where(torch.arange(tokens) % 2 == 0, 0.0, 1.0)}[weights]
     where = "cuda" if tokens * width * vocab > 1 << 24 else "cpu"
     want = R.loss(x.to(where), w.to(where), targets.to(where), dtype, None if token_weights is None else token_weights.to(where), gradient=True)
-    held = [Held(t, lead, extra) for t in (x, w)]
+    held = [Held(t, *at) for t, *at in zip((x, w), leads, extras)]
     arguments = [v for h in held for v in h.at()]
     target = targets.cuda()
     loss, lse = (result(1, tokens, torch.float32) for _ in range(2))
-    ws_all, ws = scratch(L.mg_vocab_loss_workspace_bytes(code, *case))
+    ws_all, ws = scratch(L.mg_vocab_loss_workspace_bytes(code, *case) + room)
     L.mg_vocab_loss(code, *case, *arguments, target, loss.at()[0], lse.at()[0], ws)
     torch.cuda.synchronize()
     R.check(lse.x[0], want["lse"], "lse")
     R.check(loss.x[0], want["loss"], "loss")
     assert loss.untouched() and lse.untouched() and bool((ws_all[len(ws):] == 255).all())
-    outs = [result(*shape, dtype, lead, extra) if on else None for on, shape in zip(wanted, ((tokens, width), (vocab, width)))]
-    ws_all, ws = scratch(L.mg_vocab_loss_grad_workspace_bytes(code, *case))
+    outs = [result(*shape, dtype, *at) if on else None for on, shape, *at in zip(wanted, ((tokens, width), (vocab, width)), leads[2:], extras[2:])]
+    ws_all, ws = scratch(L.mg_vocab_loss_grad_workspace_bytes(code, *case) + room)
     L.mg_vocab_loss_grad(code, *case, *arguments, target, lse.at()[0], None if token_weights is None else token_weights.cuda(), *(v for o in outs for v in (o.at() if o else (None, 0))), ws)
     torch.cuda.synchronize()
     for name, o in zip(("dx", "dw"), outs):
@@ -198,6 +275,33 @@ def test_weights_of_tokens(weights, ignored, dtype):
 def test_loss_of_parts_of_larger_matrices(lead, extra, dtype):
     for case in ((40, 72, 136), (21, 45, 301)):
         run_loss(case, KINDS[dtype], lead, extra)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("case", [(40, 72, 136), (250, 264, 520)], ids=lambda c: "x".join(map(str, c)))
+def test_losses_whose_matrices_lie_differently(case, dtype):
+    for lead, extra in ((0, (8, 24, 16, 40)), ((0, 3, 5, 0), (8, 5, 3, 40)), ((2, 0, 0, 1), (8, 16, 3, 40))):
+        for room in (0, 1 << 22):
+            run_loss(case, KINDS[dtype], lead, extra, room=room)
+
+
+@pytest.mark.parametrize("dtype", KINDS)
+def test_weights_of_all_sizes(dtype):
+    """an infinite weight makes its own token's gradients no numbers and no other token's; tiny and huge ones are as exact as ordinary ones"""
+    kind = KINDS[dtype]
+    x, w, targets = normal(1, 40, 32).to(kind).cuda(), normal(2, 50, 32, sigma=0.2).to(kind).cuda(), (torch.arange(40) % 50).cuda()
+    head = D.VocabLoss(w)
+    head.forward(x, targets)
+    ones = head.backward(torch.ones(40, device="cuda"))
+    for scale in (2.0 ** -90, 2.0 ** 14):
+        dx, dw = head.backward(torch.full((40,), scale, device="cuda"))
+        if kind != torch.float16:                                    # (results are rounded to the type, whose range is what it is)
+            assert all(torch.equal(a.double(), b.double() * scale) for a, b in zip((dx, dw), ones))
+    some = torch.ones(40, device="cuda")
+    some[7] = math.inf
+    dx = head.backward(some)[0]
+    others = torch.arange(40) != 7
+    assert torch.equal(dx.cpu()[others], ones[0].cpu()[others]) and not bool(dx[7].isfinite().any())
 
 
 @pytest.mark.parametrize("dtype", KINDS)
@@ -476,6 +580,44 @@ def test_layers_take_views_and_refuse_other_types():
     block.forward(x, keep=False)
     with pytest.raises(RuntimeError):
         block.backward(x)
+
+
+def test_two_streams_at_once():
+    """calls that overlap, a workspace each, give what they give one after the other"""
+    models = [make(torch.bfloat16, tokens=600, width=520, hidden=1000, vocab=3000, seed=s) for s in (30, 40)]
+    want = [[t.clone() for t in D.train_step(block, head, x, targets, 0.05)[2]] for block, head, x, targets in models]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in models]
+    got = [[], []]
+    for _ in range(5):
+        for n, (stream, model) in enumerate(zip(streams, models)):
+            with torch.cuda.stream(stream):
+                got[n].append(D.train_step(*model, 0.05)[2])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for n in (0, 1) for grads in got[n] for a, b in zip(grads, want[n]))
+
+
+def test_other_default_types_and_devices():
+    """buffers and tables have the types that the calls are told, whatever torch makes by default"""
+    want = [t.clone() for t in D.train_step(*make(torch.bfloat16), 0.05)[2]]
+    model = make(torch.bfloat16)
+    torch.set_default_dtype(torch.bfloat16)
+    torch.set_default_device("cuda")
+    try:
+        loss, norm, grads = D.train_step(*model, 0.05)
+    finally:
+        torch.set_default_dtype(torch.float32)
+        torch.set_default_device("cpu")
+    assert loss.dtype == norm.dtype == torch.float32 and all(torch.equal(a, b) for a, b in zip(grads, want))
+
+
+def test_memory_that_is_listed_twice():
+    g = torch.ones(100, device="cuda")
+    with pytest.raises(ValueError, match="0 and 1 share memory"):
+        D.Gradients([g, g])
+    with pytest.raises(ValueError, match="0 and 2 share memory"):
+        D.Gradients([g[:51], torch.ones(3, device="cuda"), g[50:]])
+    assert float(D.Gradients([g[:50], g[50:], g[7:7]]).norm()) == 10.0
 
 
 def test_example_runs(capsys):

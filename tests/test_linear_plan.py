@@ -29,6 +29,12 @@ def test_the_gpu_tests_reach_every_kernel():
     assert {("kk", end, "few") for end in ("store", "gated", "scores")} <= taken
 
 
+def test_both_matrices_of_a_sum_are_read_on_every_tile():
+    """by the GPU test whose gate and up weights lie at different distances"""
+    got = choices([block(*c)[3] for c in ((1000, 1000, 2000), (2100, 4000, 520), (4000, 1500, 700), (1500, 2000, 1000))])
+    assert [g[0] for g in got] == ["64", "256", "128", "128 deep"]
+
+
 def test_slices_cover_the_sum_and_fit_their_room():
     rng = random.Random(1)
     asked = []
