@@ -195,34 +195,61 @@ hipError_t launch_zero_rows(void *X, int64_t rows, int64_t cols, int64_t ld, int
 #if defined(__HIPCC__)
 
 // e^x by the hardware's exponential of base two: relative error below 2^-23 (1 + |x|)
-__device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+constexpr float LOG2_E = 1.44269504088896340736f;
+__device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * LOG2_E); }
 template <bool PRECISE> __device__ inline float exp_of(float x)
 {
     if constexpr (PRECISE) return expf(x);
     else return exp_fast(x);
 }
+// 1 / x, PRECISE: rounded, otherwise off by a step (one instruction in the place of ten)
+template <bool PRECISE> __device__ inline float one_over(float x)
+{
+    if constexpr (PRECISE) return 1.f / x;
+    else return __builtin_amdgcn_rcpf(x);
+}
 
 // act(g) and its derivative (PRECISE: for results in FP32).  GELU_TANH: (1 + tanh(b)) / 2 = 1 / (1 + exp(-2 b)), which loses nothing for small results; GELU: the normal
-// distribution function as erfc(-g / sqrt 2) / 2, for the same reason.
+// distribution function as erfc(-g / sqrt 2) / 2, for the same reason.  That is exp(-g^2 / 2) times a function without poles, of which the 16-bit types take a
+// polynomial in t = 1 / (1 + 0.27 |g|), of degree 9 and without constant term, fitted to the least relative error (2^-25; evaluated in FP32 2^-21.3); the exponential is in the slope
+// too.  (erfcf: 16384 x 2048, hidden 8192: see linear_end.h.)
 template <int ACT, bool PRECISE = false> __device__ inline void activation_of(float g, float &a, float &slope)
 {
     if constexpr (ACT == MG_ACT_SILU) {
-        const float p = 1.f / (1.f + exp_of<PRECISE>(-g));
+        const float p = one_over<PRECISE>(1.f + exp_of<PRECISE>(-g));
         a = g * p;
-        slope = p * (1.f + g * (1.f - p));
+        slope = fmaf(a, 1.f - p, p);
     } else if constexpr (ACT == MG_ACT_RELU2) {
         const float v = g > 0.f ? g : g != g ? g : 0.f;
         a = v * v;
         slope = 2.f * v;
     } else if constexpr (ACT == MG_ACT_GELU) {
-        const float below = 0.5f * erfcf(-0.70710678118654752440f * g);
+        constexpr float DENSITY = 0.39894228040143267794f;               // 1 / sqrt(2 pi)
+        const float e = exp_of<PRECISE>(-0.5f * g * g);
+        float below;
+        if constexpr (PRECISE) {
+            below = 0.5f * erfcf(-0.70710678118654752440f * g);
+        } else {
+            const float t = one_over<false>(fmaf(fabsf(g), 0.27f, 1.f));
+            float s = 0.028915580362081528f;
+            s = fmaf(s, t, -0.1262567639350891f);
+            s = fmaf(s, t, 0.16929452121257782f);
+            s = fmaf(s, t, -0.06862454861402512f);
+            s = fmaf(s, t, 0.10740189999341965f);
+            s = fmaf(s, t, 0.07223924249410629f);
+            s = fmaf(s, t, 0.10175943374633789f);
+            s = fmaf(s, t, 0.1075504720211029f);
+            s = fmaf(s, t, 0.10772018134593964f);
+            const float tail = s * t * e;
+            below = g < 0.f ? tail : 1.f - tail;
+        }
         a = g * below;
-        slope = below + g * exp_of<PRECISE>(-0.5f * g * g) * 0.39894228040143267794f;
+        slope = fmaf(g * e, DENSITY, below);
     } else {
         constexpr float A = 1.59576912160573071176f, B = 0.044715f;       // 2 sqrt(2 / pi)
-        const float g2 = fminf(g * g, 1e30f), p = 1.f / (1.f + exp_of<PRECISE>(-A * g * (1.f + B * g2)));
+        const float g2 = fminf(g * g, 1e30f), p = one_over<PRECISE>(1.f + exp_of<PRECISE>(-g * fmaf(g2, A * B, A)));
         a = g * p;
-        slope = p + g * p * (1.f - p) * A * (1.f + 3.f * B * g2);
+        slope = fmaf(a * (1.f - p), fmaf(g2, 3.f * A * B, A), p);
     }
 }
 #endif

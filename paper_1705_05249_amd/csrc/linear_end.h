@@ -63,9 +63,12 @@ template <typename T> __device__ inline void keep(void *kept, int64_t block, int
         char *const at = static_cast<char *>(kept) + block * kept_block_bytes(MG_BF16);
         // the largest finite one of four goes to 2^14 .. 2^15 (infinities stay what they are)
         auto shift = [](const float (&v)[4]) {
-            float largest = 0.f;
+            float largest = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
+            if (__builtin_expect(__any(largest == __builtin_inff()), 0)) {
+                largest = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) largest = fmaxf(largest, fabsf(v[i]) < __builtin_inff() ? fabsf(v[i]) : 0.f);
+                for (int i = 0; i < 4; ++i) largest = fmaxf(largest, fabsf(v[i]) < __builtin_inff() ? fabsf(v[i]) : 0.f);
+            }
             const int e = __builtin_amdgcn_frexp_expf(largest);
             return 15 - e < 126 ? 15 - e : 126;
         };
@@ -85,31 +88,47 @@ template <typename T> __device__ inline void keep(void *kept, int64_t block, int
         *reinterpret_cast<end_floatx4 *>(at + 256) = end_floatx4{b[0], b[1], b[2], b[3]};
     }
 }
-template <typename T> __device__ inline void recall(const void *kept, int64_t block, int lane, float (&a)[4], float (&b)[4])
-{
-    if constexpr (std::is_same_v<T, bfloat>) {
-        const char *const at = static_cast<const char *>(kept) + block * kept_block_bytes(MG_BF16);
-        struct Both {
-            Four<_Float16> x, y;
-        };
-        const Both v = __builtin_bit_cast(Both, *reinterpret_cast<const end_floatx4 *>(at + 16 * lane));
-        const uint16_t k = *reinterpret_cast<const uint16_t *>(at + 1024 + 2 * lane);
-        const int ka = static_cast<int8_t>(k & 0xff), kb = static_cast<int8_t>(k >> 8);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            a[e] = ldexpf(static_cast<float>(v.x.v[e]), -ka);
-            b[e] = ldexpf(static_cast<float>(v.y.v[e]), -kb);
-        }
-    } else {
+// The way back: a block's load, which may be early, and what it holds
+template <typename T> struct Kept {
+    end_floatx4 x, y;
+    __device__ inline void load(const void *kept, int64_t block, int lane)
+    {
         const float *const at = reinterpret_cast<const float *>(static_cast<const char *>(kept) + block * kept_block_bytes(MG_F16)) + 4 * lane;
-        const end_floatx4 x = *reinterpret_cast<const end_floatx4 *>(at), y = *reinterpret_cast<const end_floatx4 *>(at + 256);
+        x = *reinterpret_cast<const end_floatx4 *>(at);
+        y = *reinterpret_cast<const end_floatx4 *>(at + 256);
+    }
+    __device__ inline void recall(float (&a)[4], float (&b)[4]) const
+    {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             a[e] = x[e];
             b[e] = y[e];
         }
     }
-}
+};
+template <> struct Kept<bfloat> {
+    end_floatx4 x;
+    uint16_t k;
+    __device__ inline void load(const void *kept, int64_t block, int lane)
+    {
+        const char *const at = static_cast<const char *>(kept) + block * kept_block_bytes(MG_BF16);
+        x = *reinterpret_cast<const end_floatx4 *>(at + 16 * lane);
+        k = *reinterpret_cast<const uint16_t *>(at + 1024 + 2 * lane);
+    }
+    __device__ inline void recall(float (&a)[4], float (&b)[4]) const
+    {
+        struct Both {
+            Four<_Float16> x, y;
+        };
+        const Both v = __builtin_bit_cast(Both, x);
+        const int ka = static_cast<int8_t>(k & 0xff), kb = static_cast<int8_t>(k >> 8);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a[e] = ldexpf(static_cast<float>(v.x.v[e]), -ka);
+            b[e] = ldexpf(static_cast<float>(v.y.v[e]), -kb);
+        }
+    }
+};
 
 // Columns of H, dG and dU that are written: zeros from `hidden` on
 __device__ inline int held_columns(int hidden) { return (hidden + 15) / 16 * 16; }
@@ -147,16 +166,31 @@ template <typename T, int FM, int FN> __device__ __forceinline__ void end_gated_
     const int held = held_columns(args.hidden);
     T *const C = static_cast<T *>(args.C0);
     const int64_t beside = args.ldc0 / 2;                   // dU's columns behind dG's
+    // what a row of blocks needs is asked for while the row before it is stored, as far as there are registers
+    constexpr int EARLY = std::is_same_v<T, bfloat> ? FM : FM / 4;
+    Kept<T> kept[2][FM];
+    auto ask = [&](int j, int from, int to) __attribute__((always_inline)) {
+        // (blocks outside are not there: a block that is, is read for them, and not used)
+        const int row = row0 + 16 * j < args.rows ? row0 + 16 * j : args.rows - 1;
+#pragma unroll
+        for (int i = from; i < to; ++i) {
+            const int col = col0 + 16 * i < held ? col0 + 16 * i : held - 1;
+            kept[j % 2][i].load(args.kept, kept_block(row, col, args.hidden), lane);
+        }
+    };
+    ask(0, 0, EARLY);
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
         const int row = row0 + 16 * j;
         Four<T> du[FM];
+        ask(j, EARLY, FM);
+        if (j + 1 < FN) ask(j + 1, 0, EARLY);
         end_fence();
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int col = col0 + 16 * i;
-            float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
-            if (row < args.rows && col < held) recall<T>(args.kept, kept_block(row, col, args.hidden), lane, a, b);
+            float a[4], b[4];
+            kept[j % 2][i].recall(a, b);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 // (columns behind the last one are sums of whatever lies behind the rows of WD)
@@ -175,6 +209,24 @@ template <typename T, int FM, int FN> __device__ __forceinline__ void end_gated_
         end_fence();
         end_drain<T, FM * 16>(region, ROWB, row, col0, args.rows, held, lane, [&](int r) { return C + beside + r * args.ldc0; });
     }
+}
+
+// A row's target among this lane's 4 FM columns (element e of block i is 4 i + e), -1: not there.  wanted: behind the wavefront's first column; left: columns from that on.
+// A vocabulary has many tiles and a row one target: what is done for it stands behind a branch that few wavefronts take.
+template <int FM> __device__ inline int wanted_column(int64_t wanted, int left, int lane)
+{
+    if (wanted < 0 || wanted >= 16 * FM || wanted >= left) return -1;
+    const int at = static_cast<int>(wanted);
+    return at % 16 / 4 == lane / 16 ? at / 16 * 4 + at % 4 : -1;
+}
+template <int FM> __device__ inline float wanted_of(const end_floatx4 (&row)[FM], int at)
+{
+    float z = 0.f;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z = at == 4 * i + e ? row[i][e] : z;
+    return z;
 }
 
 // (largest, sum of exp(z - largest)) of two sets of logits
@@ -232,25 +284,31 @@ __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
             const int row = row0 + 16 * j + lane % 16;
-            const int64_t wanted = row < args.rows ? args.targets[row] - args.first : -1;
-            float m = -__builtin_inff(), s = 0.f;
+            const int at = wanted_column<FM>(row < args.rows ? args.targets[row] - args.first - col0 : -1, args.cols - col0, lane);
+            if (col0 + 16 * FM > args.cols) {
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const int col = col0 + 16 * i + 4 * (lane / 16);
+                for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (col + e >= args.cols) acc[j][i][e] = -__builtin_inff();
-                    m = fmaxf(m, acc[j][i][e]);
-                    if (col + e == wanted && col + e < args.cols) args.target_score[row] = acc[j][i][e];
-                }
+                    for (int e = 0; e < 4; ++e)
+                        if (col0 + 16 * i + 4 * (lane / 16) + e >= args.cols) acc[j][i][e] = -__builtin_inff();
             }
-            m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(m, __shfl_xor(m, 32));
-            const float from = m == -__builtin_inff() ? 0.f : m;
+            if (__any(at >= 0)) {
+                const float z = wanted_of<FM>(acc[j], at);
+                if (at >= 0) args.target_score[row] = z;
+            }
+            float m = -__builtin_inff(), s = 0.f;
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s += exp_fast(acc[j][i][e] - from);
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[j][i][e]);
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            // exp(z - m) as 2 to the power of z log2(e) - (m log2(e)), the product in front rounded: off by half a step of m for all of a row's terms, as m itself is
+            const float from = m == -__builtin_inff() ? 0.f : -LOG2_E * m;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s += __builtin_amdgcn_exp2f(fmaf(acc[j][i][e], LOG2_E, from));
             s += __shfl_xor(s, 16);
             s += __shfl_xor(s, 32);
             if (lane < 16) shared[wc * (WR * FN * 16) + wr * FN * 16 + 16 * j + lane] = make_float2(m, s);
@@ -273,15 +331,17 @@ __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (
         for (int j = 0; j < FN; ++j) {
             const int row = row0 + 16 * j + lane % 16;
             int64_t wanted = -1;
-            float w = 0.f, lse = 0.f;
+            float w = 0.f, from = 0.f;
             if (row < args.rows) {
                 wanted = args.targets[row];
                 if (wanted >= 0 && wanted < args.vocab) {
                     w = (args.weights == nullptr ? 1.f : args.weights[row]) * weight_scale;
-                    lse = args.lse[row];
+                    from = -LOG2_E * args.lse[row];
                 }
-                wanted -= args.first;
+                wanted -= args.first + col0;
             }
+            const int at = wanted_column<FM>(wanted, args.cols - col0, lane);
+            const bool ends = col0 + 16 * FM > args.cols;
             end_fence();
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
@@ -289,10 +349,20 @@ __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (
                 float d[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = exp_fast(acc[j][i][e] - lse) - (col + e == wanted ? 1.f : 0.f);
-                    d[e] = w != 0.f && col + e < args.cols ? w * p : 0.f;           // (a token that adds nothing adds nothing, whatever its logits are)
+                    const float p = __builtin_amdgcn_exp2f(fmaf(acc[j][i][e], LOG2_E, from));
+                    d[e] = w != 0.f ? w * p : 0.f;                                  // (a token that adds nothing adds nothing, whatever its logits are)
+                }
+                if (ends) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e >= args.cols) d[e] = 0.f;
                 }
                 end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, d[0], d[1], d[2], d[3]);
+            }
+            if (__any(at >= 0)) {
+                // the target's own: w (p - 1), in the place of w p
+                const float p = __builtin_amdgcn_exp2f(fmaf(wanted_of<FM>(acc[j], at), LOG2_E, from)) - 1.f;
+                if (at >= 0) *reinterpret_cast<T *>(region + (lane % 16) * ROWB + (at / 4 * 16 + lane / 16 * 4 + at % 4) * 2) = static_cast<T>(w != 0.f ? w * p : 0.f);
             }
             end_fence();
             end_drain<T, FM * 16>(region, ROWB, row0 + 16 * j, col0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
