@@ -212,7 +212,7 @@ template <bool PRECISE> __device__ inline float one_over(float x)
 // act(g) and its derivative (PRECISE: for results in FP32).  GELU_TANH: (1 + tanh(b)) / 2 = 1 / (1 + exp(-2 b)), which loses nothing for small results; GELU: the normal
 // distribution function as erfc(-g / sqrt 2) / 2, for the same reason.  That is exp(-g^2 / 2) times a function without poles, of which the 16-bit types take a
 // polynomial in t = 1 / (1 + 0.27 |g|), of degree 9 and without constant term, fitted to the least relative error (2^-25; evaluated in FP32 2^-21.3); the exponential is in the slope
-// too.  (erfcf: 16384 x 2048, hidden 8192: see linear_end.h.)
+// too.  Gate and up product of 8192 tokens, width 2048, hidden 8192, with what is kept: 528 us with erfcf, 484 so; SILU with the reciprocal for a division 466 -> 453.
 template <int ACT, bool PRECISE = false> __device__ inline void activation_of(float g, float &a, float &slope)
 {
     if constexpr (ACT == MG_ACT_SILU) {

@@ -17,6 +17,13 @@ __device__ inline void mma(floatx4 &acc, const u32x4 &frag_n, const u32x4 &frag_
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bfloatx8, frag_m), __builtin_bit_cast(bfloatx8, frag_n), acc, 0, 0, 0);
 }
 
+// `rows` rows of `ld` elements in reach of a descriptor, the last one `last` long (in whole pieces: what a range cuts is lost in words)
+__device__ inline __amdgpu_buffer_rsrc_t linear_descriptor(const _Float16 *base, int64_t rows, int64_t ld, int last)
+{
+    const int64_t range = ((rows - 1) * ld + (last + 7) / 8 * 8) * 2;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16 *>(base), 0, rows <= 0 || last <= 0 ? 0 : static_cast<int>(range < 0x7fffffff ? range : 0x7fffffff), 0x00020000);
+}
+
 // One operand tile, ROWS rows x 64 values of the sum: global -> LDS, in blocks of 1 KB that a wavefront's instruction fills; a wavefront has COUNT
 // consecutive ones.  The swizzles of lds_layout.h repeat: two lane offsets (`group`) and a multiple of a scalar step name the place of every block.
 //   along the sum:    eight rows a block, 16 rows a step; what lies behind the sum's end in a row is left out by the lane's place in the K-tile, rows
@@ -30,8 +37,8 @@ template <int ROWS, int NT, bool ALONG, bool GATED = false, bool ONCE = false> s
     static constexpr int COUNT = LDS_BYTES / (NT * 16);
     static constexpr uint32_t MISSING = 0x80000000u;                // no range is that long; no step carries it past 2^32
     static_assert((COUNT == 2 || COUNT == 4 || (COUNT == 8 && ALONG && !GATED)) && COUNT * NT * 16 == LDS_BYTES && (ALONG || !GATED), "tile / work-group size");
-    static constexpr int group(int q) { return ALONG || ROWS == 256 ? q % 2 : ROWS == 128 ? q / 2 : q; }
-    static constexpr int steps(int q) { return ALONG || ROWS == 256 ? q / 2 : ROWS == 128 ? q % 2 : 0; }
+    static constexpr int group(int q) { return ALONG ? q % 2 : ROWS == 128 ? q / 2 : q; }
+    static constexpr int steps(int q) { return ALONG ? q / 2 : ROWS == 128 ? q % 2 : 0; }
 
     uint32_t goff[2], now[2];           // lane's byte offset of a group's first block; what the K-tile aimed at makes of it
     uint32_t other[2];                  // the same in a second matrix
@@ -63,21 +70,15 @@ template <int ROWS, int NT, bool ALONG, bool GATED = false, bool ONCE = false> s
         });
         step = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>((ALONG ? 16 : 4) * ld * 2));
     }
-    // rows of a tile in reach of the range: `rows` of `ld` elements, the last one `last` long (in whole pieces: what a range cuts is lost in words)
-    static __device__ inline __amdgpu_buffer_rsrc_t descriptor(const _Float16 *base, int64_t rows, int64_t ld, int last)
-    {
-        const int64_t range = ((rows - 1) * ld + (last + 7) / 8 * 8) * 2;
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<_Float16 *>(base), 0, rows <= 0 || last <= 0 ? 0 : static_cast<int>(range < 0x7fffffff ? range : 0x7fffffff), 0x00020000);
-    }
     // The K-tile that starts at value l0 of the sum, of which `left` are there (none: zeros).  rows: of the operand from r0 on (GATED: features).
     __device__ inline void aim(const _Float16 *X, int64_t ld, int64_t r0, int64_t l0, int left, int rows, bool second = false)
     {
         if constexpr (ALONG) {
-            rsrc = descriptor(X + r0 * ld + l0, rows < ROWS ? rows : ROWS, ld, left);
+            rsrc = linear_descriptor(X + r0 * ld + l0, rows < ROWS ? rows : ROWS, ld, left);
             now[0] = kpos[0] < left ? goff[0] : MISSING;
             now[1] = kpos[1] < left ? goff[1] : MISSING;
         } else {
-            rsrc = descriptor(X + r0 + l0 * ld, left < 64 ? left : 64, ld, rows);
+            rsrc = linear_descriptor(X + r0 + l0 * ld, left < 64 ? left : 64, ld, rows);
             now[0] = second ? other[0] : goff[0];
             now[1] = second ? other[1] : goff[1];
             step = static_cast<uint32_t>(4 * ld * 2);                               // (the matrices' rows need not be equally far apart)
@@ -86,8 +87,8 @@ template <int ROWS, int NT, bool ALONG, bool GATED = false, bool ONCE = false> s
     __device__ inline void aim_gated(const _Float16 *gate, int64_t ldg, const _Float16 *upper, int64_t ldu, int64_t feature, int64_t l0, int left, int features)
     {
         const int rows = features < ROWS / 2 ? features : ROWS / 2;
-        rsrc = descriptor(gate + feature * ldg + l0, rows, ldg, left);
-        rsrc_up = descriptor(upper + feature * ldu + l0, rows, ldu, left);
+        rsrc = linear_descriptor(gate + feature * ldg + l0, rows, ldg, left);
+        rsrc_up = linear_descriptor(upper + feature * ldu + l0, rows, ldu, left);
         if (COUNT == 2 && up) rsrc = rsrc_up;
     }
     // mine: this wavefront's first block in the destination stage (wave-uniform); left: values of the sum from the K-tile's first one on (GATED)

@@ -100,7 +100,7 @@ template <typename T, int END, int FM, int FN, int U> __global__ __launch_bounds
     }
     __syncthreads();
     if (wave > 0) return;
-#pragma unroll
+#pragma unroll 2
     for (int w = 0; w < W - 1; ++w)
 #pragma unroll
         for (int j = 0; j < FN; ++j)

@@ -45,10 +45,10 @@ template <bool ALONG, bool GATED = false> struct LinearLoaderHalf {
     __device__ inline void aim(const _Float16 *X, int64_t ld, int64_t r0, int64_t l0, int left, int rows, bool second = false)
     {
         if constexpr (ALONG) {
-            rsrc = LinearLoader<256, 512, true>::descriptor(X + r0 * ld + l0, rows < (GATED ? 128 : 256) ? rows : (GATED ? 128 : 256), ld, left);
+            rsrc = linear_descriptor(X + r0 * ld + l0, rows < (GATED ? 128 : 256) ? rows : (GATED ? 128 : 256), ld, left);
             now[0] = kpos < left ? goff[0] : MISSING;
         } else {
-            rsrc = LinearLoader<256, 512, false>::descriptor(X + r0 + l0 * ld, left < 64 ? left : 64, ld, rows);
+            rsrc = linear_descriptor(X + r0 + l0 * ld, left < 64 ? left : 64, ld, rows);
             now[0] = second ? other[0] : goff[0];
             now[1] = second ? other[1] : goff[1];
             step = static_cast<uint32_t>(16 * ld * 2);
@@ -80,7 +80,7 @@ struct LinearLoaderHalves {
     }
     __device__ inline void aim(const _Float16 *X, int64_t ld, int64_t r0, int64_t l0, int left, int rows)
     {
-        rsrc = LinearLoader<256, 512, false>::descriptor(X + r0 + l0 * ld, left < 64 ? left : 64, ld, rows);
+        rsrc = linear_descriptor(X + r0 + l0 * ld, left < 64 ? left : 64, ld, rows);
     }
     template <int Q> __device__ inline void issue(lds_char *mine, bool flat = false) const
     {
