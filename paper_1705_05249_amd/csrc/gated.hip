@@ -257,34 +257,32 @@ mg_status backward_16(const GatedProblem &p)
         a.C0 = d; a.ldc0 = 2 * half;
         if (const hipError_t e = launch_linear(p.dtype, FORM_KN, END_GATED_GRAD, a, nullptr, 0, p.stream)) return launched(e);
     }
+    LinearTogether last{};
     if (p.dX != nullptr) {
-        LinearArgs a{};
+        LinearArgs &a = last.of[0];
         left(a, both);
         gate(a, wg);
         a.Q1 = wu.at; a.ldq1 = wu.ld;
         a.segment = static_cast<int>(half); a.lines = hidden;
         a.rows = tokens; a.cols = width; a.k = static_cast<int>(2 * half);
         a.C0 = p.dX; a.ldc0 = p.lddx;
-        if (const hipError_t e = launch_linear(p.dtype, FORM_KN, END_STORE, a, room, room_bytes, p.stream)) return launched(e);
     }
     if (gates) {
-        LinearArgs a{};
+        LinearArgs &a = last.of[1];
         left(a, both);
         gate(a, x);
         a.rows = static_cast<int>(2 * half); a.cols = width; a.k = tokens;
         a.second = static_cast<int>(half); a.rows0 = hidden;
         a.C0 = p.dWG; a.ldc0 = p.lddwg; a.C1 = p.dWU; a.ldc1 = p.lddwu;
-        if (const hipError_t e = launch_linear(p.dtype, FORM_NN, END_STORE, a, room, room_bytes, p.stream)) return launched(e);
     }
     if (p.dWD != nullptr) {
-        LinearArgs a{};
+        LinearArgs &a = last.of[2];
         left(a, dy);
         gate(a, {static_cast<char *>(p.kept) + kept_front(p.dtype, p.tokens, p.hidden), half, true});
         a.rows = width; a.cols = hidden; a.k = tokens;
         a.C0 = p.dWD; a.ldc0 = p.lddwd;
-        if (const hipError_t e = launch_linear(p.dtype, FORM_NN, END_STORE, a, room, room_bytes, p.stream)) return launched(e);
     }
-    return MG_OK;
+    return launched(launch_linear_together(p.dtype, last, room, room_bytes, p.stream));
 }
 
 }  // namespace

@@ -63,6 +63,12 @@ __host__ __device__ inline int64_t kept_blocks(int64_t hidden) { return (hidden 
 __host__ __device__ inline int64_t kept_block(int64_t row, int64_t col, int64_t hidden) { return (row / 16) * kept_blocks(hidden) + col / 16; }
 constexpr int kept_block_bytes(int dtype) { return dtype == MG_BF16 ? 1024 + 128 : 2048; }
 
+// Products of END_STORE in one launch (linear_together.hip): the first of FORM_KN, the others of FORM_NN; none where rows is 0.  begin: first work-group
+struct LinearTogether {
+    LinearArgs of[3];
+    uint32_t begin[4];
+};
+
 // Which of P and Q lie along the sum
 enum LinearForm { FORM_KK = 0, FORM_KN = 1, FORM_NN = 2 };       // both; P along, Q across; both across
 
@@ -85,6 +91,11 @@ hipError_t launch_linear_dma_kk_scores_grad(int dtype, int tile, const LinearArg
 hipError_t launch_linear_dma_kn_store(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
 hipError_t launch_linear_dma_kn_gated_grad(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
 hipError_t launch_linear_dma_nn_store(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream);
+
+// All of them, in one launch or one by one (linear_plan.h); room: for slices of the first one's sum
+hipError_t launch_linear_together(int dtype, LinearTogether all, void *room, size_t room_bytes, hipStream_t stream);
+// tile: LINEAR_128 or LINEAR_64; slices: of the first product, whose k_per_slice and `partial` say so
+hipError_t launch_linear_together_on(int dtype, int tile, LinearTogether all, int slices, hipStream_t stream);
 
 // adds the slices of END_STORE and writes C in dtype
 hipError_t launch_linear_sum(int dtype, const LinearArgs &args, int slices, hipStream_t stream);

@@ -106,7 +106,7 @@ template <typename T, int FORM, int END> __global__ __launch_bounds__(256) void 
             __syncthreads();
         }
     }
-    linear_end<T, END, 2, 2, 2, 2>(args, acc, regions[wave], shared, row0, col0, wr, wc, lane);
+    linear_end<T, END, 2, 2, 2, 2>(args, acc, regions[wave], shared, row0, col0, wr, wc, lane, blockIdx.z);
 }
 
 template <typename T> hipError_t launch(int form, int end, const LinearArgs &args, int slices, hipStream_t stream)

@@ -125,8 +125,8 @@ template <bool ALONG, int ROWS, int F, int S, int STAGE> __device__ inline u32x4
     }
 }
 
-// BC x BR: columns and rows of a work-group's tile; WC x WR wavefronts.  FORM, END: LinearForm, LinearEnd.
-template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES> __global__ __launch_bounds__(WC *WR * 64) void linear_dma_kernel(const LinearArgs args)
+// BC x BR: columns and rows of a work-group's tile; WC x WR wavefronts.  FORM, END: LinearForm, LinearEnd.  group: among the tiles of a slice
+template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES> __device__ __forceinline__ void linear_dma_tile(const LinearArgs &args, int group, int slice)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool P_ALONG = FORM != FORM_NN, Q_ALONG = FORM == FORM_KK;
@@ -143,9 +143,9 @@ template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STA
     lds_char *const lds3 = (lds_char *)lds;
 
     int tile_c, tile_r;
-    tile_coords(blockIdx.x, args.tiles_c, args.tiles_r, 8, tile_c, tile_r);
+    tile_coords(group, args.tiles_c, args.tiles_r, 8, tile_c, tile_r);
     const int col0 = tile_c * BC, row0 = tile_r * BR;
-    const int kb = blockIdx.z * args.k_per_slice, ke = kb + args.k_per_slice < args.k ? kb + args.k_per_slice : args.k;
+    const int kb = slice * args.k_per_slice, ke = kb + args.k_per_slice < args.k ? kb + args.k_per_slice : args.k;
     const int ktiles = (ke - kb + BK - 1) / BK;
 
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -280,10 +280,15 @@ template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STA
     hold_registers(fp[0]);
     __syncthreads();        // all loads have landed and all fragment reads are done
     constexpr int REGION = end_region<WTC>();
-    linear_end<T, END, FM, FN, WR, WC>(args, acc, lds + wave * REGION, reinterpret_cast<float2 *>(lds + WC * WR * REGION), row0, col0, wr, wc, lane);
+    linear_end<T, END, FM, FN, WR, WC>(args, acc, lds + wave * REGION, reinterpret_cast<float2 *>(lds + WC * WR * REGION), row0, col0, wr, wc, lane, slice);
 #else
-    (void)args;
+    (void)args, (void)group, (void)slice;
 #endif
+}
+
+template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES> __global__ __launch_bounds__(WC *WR * 64) void linear_dma_kernel(const LinearArgs args)
+{
+    linear_dma_tile<T, FORM, END, BC, BR, WC, WR, STAGES>(args, blockIdx.x, blockIdx.z);
 }
 
 template <int BC, int BR, int WC, int WR, int STAGES> constexpr int linear_dma_lds()

@@ -239,13 +239,13 @@ __device__ inline float2 join_scores(float2 a, float2 b)
 // All WR x WC wavefronts that share a tile come here, and nobody uses the LDS any more.  The wavefront's tile starts at (row0, col0) and is wavefront
 // (wr, wc) of WR x WC; region: its own; shared: WR * FN * 16 * WC float2 that no region overlaps (END_SCORES).
 template <typename T, int END, int FM, int FN, int WR, int WC>
-__device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (&acc)[FN][FM], char *region, float2 *shared, int tile_row, int tile_col, int wr, int wc, int lane)
+__device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (&acc)[FN][FM], char *region, float2 *shared, int tile_row, int tile_col, int wr, int wc, int lane, int slice = 0)
 {
     const int row0 = tile_row + wr * FN * 16, col0 = tile_col + wc * FM * 16;
     if constexpr (END == END_STORE) {
         if (args.partial != nullptr) {
             constexpr int ROWB = FM * 64 + 16;
-            float *const to = args.partial + blockIdx.z * args.partial_stride;
+            float *const to = args.partial + slice * args.partial_stride;
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 end_fence();

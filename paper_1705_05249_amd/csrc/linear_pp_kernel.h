@@ -292,7 +292,7 @@ template <typename T, int FORM, int END> __global__ __launch_bounds__(512) void 
     // anything reads them.
     asm volatile("s_nop 15\n\ts_nop 15");
     fence();
-    linear_end<T, END, FM, FN, WR, WC>(args, acc, lds + wave * REGION, reinterpret_cast<float2 *>(lds + WC * WR * REGION), row0, col0, wr, wc, lane);
+    linear_end<T, END, FM, FN, WR, WC>(args, acc, lds + wave * REGION, reinterpret_cast<float2 *>(lds + WC * WR * REGION), row0, col0, wr, wc, lane, blockIdx.z);
     __builtin_amdgcn_s_waitcnt(0x0F70);
 #else
     (void)args;

@@ -287,6 +287,7 @@ mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
     if (const hipError_t e = launch_linear_copies(list, p.stream)) return launched(e);
     const int64_t columns = piece_columns(p.dtype, p.tokens, p.vocab), lead = padded(columns);
     const int count = static_cast<int>(ceil_div(p.vocab, columns));
+    LinearTogether both{};
     LinearArgs x{};                                        // dX
     x.P = m.dz; x.ldp = lead; x.p_padded = true; x.ldq0 = o.ldw;
     x.rows = static_cast<int>(p.tokens); x.cols = static_cast<int>(p.width);
@@ -304,16 +305,16 @@ mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
             x.Q0 = z.Q0;
             x.k = static_cast<int>(some);
             x.partial = count > 1 ? m.slices + n * m.slice : nullptr;
-            if (const hipError_t e = launch_linear(p.dtype, FORM_KN, END_STORE, x, m.room, m.room_bytes, p.stream)) return launched(e);
+            both.of[0] = x;
         }
         if (p.dW != nullptr) {
-            LinearArgs w{};
+            LinearArgs &w = both.of[1];
             w.P = m.dz; w.ldp = lead; w.Q0 = o.X; w.ldq0 = o.ldx;
             w.rows = static_cast<int>(some); w.cols = static_cast<int>(p.width); w.k = static_cast<int>(p.tokens);
             w.C0 = static_cast<uint16_t *>(p.dW) + first * p.lddw; w.ldc0 = p.lddw;
             w.scale = x.scale;
-            if (const hipError_t e = launch_linear(p.dtype, FORM_NN, END_STORE, w, m.room, m.room_bytes, p.stream)) return launched(e);
         }
+        if (const hipError_t e = launch_linear_together(p.dtype, both, m.room, m.room_bytes, p.stream)) return launched(e);
     }
     if (p.dX != nullptr && count > 1) {
         x.partial = m.slices;

@@ -202,6 +202,18 @@ def test_gradients_that_are_wanted(wanted, dtype):
     run_block((70, 72, 90), "gelu", KINDS[dtype], wanted=wanted)
 
 
+# sizes at which one gradient alone is made on each of the tiles (tests/test_linear_plan.py)
+ONE_GRADIENT = [(1500, 2000, 1000), (4000, 1500, 700), (2100, 4000, 520), (70, 72, 90), (1000, 1000, 2000), (700, 3000, 3000)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("case", ONE_GRADIENT, ids=lambda c: "x".join(map(str, c)))
+def test_each_gradient_by_itself(case, dtype):
+    say("one gradient", case, dtype)
+    for wanted in ((True, False, False, False), (False, True, True, False), (False, False, False, True)):
+        run_block(case, "silu", KINDS[dtype], wanted=wanted)
+
+
 @pytest.mark.parametrize("dtype", KINDS)
 def test_blocks_without_work(dtype):
     kind, code = KINDS[dtype], CODES[KINDS[dtype]]
@@ -358,7 +370,7 @@ def test_tokens_that_do_not_count_may_hold_anything():
 
 
 # sizes at which the large tiles are taken (tests/test_linear_plan.py says which by which product)
-LARGE_BLOCKS = [(3999, 520, 4000), (4000, 4008, 520), (520, 4000, 2000), (3970, 515, 4001), (1500, 1032, 1000), (1000, 1000, 9992), (2500, 2600, 300), (2100, 520, 2500)]
+LARGE_BLOCKS = [(3999, 520, 4000), (4000, 4008, 520), (520, 4000, 2000), (3970, 515, 4001), (1500, 1032, 1000), (1000, 1000, 9992), (2500, 2600, 300), (2100, 520, 2500), (2100, 2048, 4100)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
@@ -368,7 +380,7 @@ def test_large_blocks(case, dtype):
     run_block(case, R.ACTS[sum(case) % 4], KINDS[dtype])
 
 
-LARGE_LOSSES = [(4000, 520, 4000), (3970, 515, 4061), (1111, 1032, 2100), (2600, 264, 2600)]
+LARGE_LOSSES = [(4000, 520, 4000), (3970, 515, 4061), (1111, 1032, 2100), (2600, 264, 2600), (4000, 2000, 4000), (200, 512, 9000)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])

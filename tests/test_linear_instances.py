@@ -58,9 +58,15 @@ def few():
     return {(kind, *kernel, once) for kind in (False, True) for kernel in kernels for once in (0, 1)}
 
 
-@pytest.mark.parametrize("start,wanted", [("_ZN2mg17linear_dma_kernelI", dma), ("_ZN2mg16linear_pp_kernelI", pp), ("_ZN2mg12_GLOBAL__N_121linear_few_dma_kernelI", few)])
+def together():
+    """bfloat16, tile, stages"""
+    return {(kind, *kernel) for kind in (False, True) for kernel in ((128, 2), (64, 4))}
+
+
+@pytest.mark.parametrize("start,wanted", [("_ZN2mg17linear_dma_kernelI", dma), ("_ZN2mg16linear_pp_kernelI", pp), ("_ZN2mg12_GLOBAL__N_121linear_few_dma_kernelI", few),
+                                          ("_ZN2mg12_GLOBAL__N_122linear_together_kernelI", together)])
 def test_every_hand_waited_kernel_is_looked_over(tmp_path, monkeypatch, start, wanted):
-    monkeypatch.setattr(T, "KERNEL", re.compile(r"^[0-9a-f]+ <(" + start + r"\w+E+vNS\w*?10LinearArgsE)>:$"))
+    monkeypatch.setattr(T, "KERNEL", re.compile(r"^[0-9a-f]+ <(" + start + r"\w+E+vNS\w*?1[04]Linear(?:Args|Together)E)>:$"))
     seen, wrong = set(), {}
     for n, code in enumerate(code_objects()):
         if start.encode() not in code:

@@ -1,7 +1,7 @@
 """The choice of the kernel for a product of 16-bit matrices, on the host: every kernel is taken somewhere in the GPU tests, slices fit their room and cover the sum."""
 import random
 
-from tests.linear_choice import choices
+from tests.linear_choice import choices, together
 
 
 def padded(v):
@@ -18,9 +18,20 @@ def loss(tokens, width, vocab):
     return [("kk", "scores", tokens, vocab, width), ("kk", "scores_grad", tokens, vocab, width), ("kn", "store", tokens, width, vocab), ("nn", "store", vocab, width, tokens)]
 
 
+def ends(products):
+    """the products of a call that go together where that pays: (rows, cols, k) of the one with its operand across the sum, and of those with both"""
+    sizes = [p[2:] for p in products if p[:2] == ("kn", "store")] + [p[2:] for p in products if p[0] == "nn"]
+    return (*(sizes + [(0, 0, 0)])[:3], 1 << 40)
+
+
 def test_the_gpu_tests_reach_every_kernel():
+    """gradients wanted one by one too, whose products are not asked to go together"""
     from tests import test_gpu_layers as G
-    asked = [p for c in G.BLOCKS + G.LARGE_BLOCKS for p in block(*c)] + [p for c in G.LOSSES + G.LARGE_LOSSES for p in loss(*c)]
+    calls = [block(*c) for c in G.BLOCKS + G.LARGE_BLOCKS] + [loss(*c) for c in G.LOSSES + G.LARGE_LOSSES]
+    joined = together([ends(c) for c in calls])
+    assert {(j[0], j[1] > 1) for j in joined} == {("any", False), ("128", False), ("128", True), ("64", False), ("64", True)}
+    asked = [p for c, j in zip(calls, joined) for p in c if j[0] == "any" or p[0] == "kk" or p[1] != "store"]
+    asked += [p for c in G.ONE_GRADIENT for p in block(*c)]
     taken = {(form, end, kernel) for (form, end, *_), (kernel, _, _) in zip(asked, choices(asked))}
     pairs = {(form, end) for form, end, *_ in asked}
     missing = {(*pair, tile) for pair in pairs for tile in ("256", "128", "64")} - taken
@@ -33,6 +44,24 @@ def test_both_matrices_of_a_sum_are_read_on_every_tile():
     """by the GPU test whose gate and up weights lie at different distances"""
     got = choices([block(*c)[3] for c in ((1000, 1000, 2000), (2100, 4000, 520), (4000, 1500, 700), (1500, 2000, 1000))])
     assert [g[0] for g in got] == ["64", "256", "128", "128 deep"]
+
+
+def test_products_that_go_together():
+    """both sides were measured (csrc/linear_plan.h); slices cover the sum and fit their room"""
+    got = together([((333, 1001, 4096), (4096, 1001, 333), (1001, 1999, 333), 1 << 30), ((64, 512, 2048), (2048, 512, 64), (512, 1024, 64), 1 << 30),
+                    ((1024, 1024, 4096), (4096, 1024, 1024), (1024, 2048, 1024), 1 << 30), ((4096, 1024, 4096), (4096, 1024, 4096), (1024, 2048, 4096), 1 << 30),
+                    ((333, 1001, 4096), (0, 0, 0), (0, 0, 0), 1 << 30), ((8192, 2048, 16384), (16384, 2048, 8192), (2048, 8192, 8192), 1 << 40)])
+    assert [g[0] for g in got] == ["128", "64", "128", "any", "any", "any"] and [g[1] for g in got[:3]] == [4, 8, 2]
+    rng = random.Random(2)
+    size = lambda most: int(round(most ** rng.random()))  # noqa: E731
+    asked = [(tuple(size(9000) for _ in range(3)), (size(20000), size(3000), size(3000)), (0, 0, 0), rng.choice((0, 1 << 16, 1 << 20, 1 << 30))) for _ in range(1000)]
+    taken = 0
+    for (first, _, _, room), (kernel, slices, each) in zip(asked, together(asked)):
+        if kernel == "any":
+            continue
+        taken += slices > 1
+        assert each % 64 == 0 and (slices - 1) * each < first[2] <= slices * each and (slices == 1 or slices * first[0] * padded(first[1]) * 4 <= room)
+    assert taken > 20
 
 
 def test_slices_cover_the_sum_and_fit_their_room():
