@@ -73,8 +73,9 @@ struct LinearTogether {
 enum LinearForm { FORM_KK = 0, FORM_KN = 1, FORM_NN = 2 };       // both; P along, Q across; both across
 
 // Tiles of C, square; ANY: the kernel for operands at any address.  128_DEEP: four K-tiles in LDS instead of two, for launches that leave a compute unit one
-// work-group (2048^3: 30.2 -> 21.7 us; with two work-groups to a compute unit the other one is ahead, 4096 x 4096 x 2048: 72 against 82).
-enum LinearTile { LINEAR_256 = 0, LINEAR_128 = 1, LINEAR_64 = 2, LINEAR_128_DEEP = 3, LINEAR_FEW = 4, LINEAR_ANY = -1, LINEAR_ANY_FEW = -2 };
+// work-group (2048^3: 30.2 -> 21.7 us; with two work-groups to a compute unit the other one is ahead, 4096 x 4096 x 2048: 72 against 82).  64_TWICE: two sets of
+// wavefronts for such launches (512 x 1024 x 2048: 10.6 -> 9.0 us, 1024 x 1024 x 1024 7.3 -> 6.9).
+enum LinearTile { LINEAR_256 = 0, LINEAR_128 = 1, LINEAR_64 = 2, LINEAR_128_DEEP = 3, LINEAR_FEW = 4, LINEAR_64_TWICE = 5, LINEAR_ANY = -1, LINEAR_ANY_FEW = -2 };
 constexpr int linear_tile_size(int tile) { return tile == LINEAR_256 ? 256 : tile == LINEAR_128 || tile == LINEAR_128_DEEP ? 128 : 64; }
 // slices: of the sum, each from z * k_per_slice on
 hipError_t launch_linear_any(int dtype, int form, int end, LinearArgs args, int slices, hipStream_t stream);

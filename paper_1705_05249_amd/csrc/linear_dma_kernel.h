@@ -125,8 +125,10 @@ template <bool ALONG, int ROWS, int F, int S, int STAGE> __device__ inline u32x4
     }
 }
 
-// BC x BR: columns and rows of a work-group's tile; WC x WR wavefronts.  FORM, END: LinearForm, LinearEnd.  group: among the tiles of a slice
-template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES> __device__ __forceinline__ void linear_dma_tile(const LinearArgs &args, int group, int slice)
+// BC x BR: columns and rows of a work-group's tile; WC x WR wavefronts.  FORM, END: LinearForm, LinearEnd.  group: among the tiles of a slice.
+// HALVES 2: twice the wavefronts, two sets that take K-tiles in turn, each with LDS of its own, and share the end.  For launches that leave a compute unit one tile of 64: alone, a K-tile there waits
+// for itself from load to matrix instruction (0.3 us), and two at a time take hardly longer.
+template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES, int HALVES> __device__ __forceinline__ void linear_dma_tile(const LinearArgs &args, int group, int slice)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool P_ALONG = FORM != FORM_NN, Q_ALONG = FORM == FORM_KK;
@@ -139,16 +141,18 @@ template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STA
     constexpr int Q_BYTES = LoadQ::LDS_BYTES, P_BYTES = LoadP::LDS_BYTES;        // LDS: [Q stage 0][Q stage 1] ... [P stage 0] ...
     constexpr int SLOTS = FM * FN, FRAGS = FM + FN, PIECES = LoadQ::COUNT + LoadP::COUNT;
 
+    constexpr int HALF_BYTES = STAGES * (Q_BYTES + P_BYTES);
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    lds_char *const lds3 = (lds_char *)lds;
+    const int half = HALVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
+    lds_char *const lds3 = (lds_char *)lds + half * HALF_BYTES;
 
     int tile_c, tile_r;
     tile_coords(group, args.tiles_c, args.tiles_r, 8, tile_c, tile_r);
     const int col0 = tile_c * BC, row0 = tile_r * BR;
     const int kb = slice * args.k_per_slice, ke = kb + args.k_per_slice < args.k ? kb + args.k_per_slice : args.k;
-    const int ktiles = (ke - kb + BK - 1) / BK;
+    const int ktiles = (ke - kb + BK * HALVES - 1) / (BK * HALVES);
 
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x % NT / 64;
     const int wc = wave % WC, wr = wave / WC;
     const int wave_u = __builtin_amdgcn_readfirstlane(wave);
 
@@ -171,7 +175,7 @@ template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STA
     lp.prepare(args.ldp, args.ldp, wave, lane, args.rows - row0);
     int left = 0;                               // values of the sum from the K-tile aimed at on
     auto aim_tile = [&](int t) {
-        int l0 = kb + t * BK;
+        int l0 = kb + (t * HALVES + half) * BK;
         left = ke - l0;                         // (behind the end nothing is fetched)
         if (left <= 0) l0 = kb;
         if constexpr (GATED) {
@@ -280,15 +284,33 @@ template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STA
     hold_registers(fp[0]);
     __syncthreads();        // all loads have landed and all fragment reads are done
     constexpr int REGION = end_region<WTC>();
-    linear_end<T, END, FM, FN, WR, WC>(args, acc, lds + wave * REGION, reinterpret_cast<float2 *>(lds + WC * WR * REGION), row0, col0, wr, wc, lane, slice);
+    if constexpr (HALVES == 1) {
+        linear_end<T, END, FM, FN, WR, WC>(args, acc, lds + wave * REGION, reinterpret_cast<float2 *>(lds + WC * WR * REGION), row0, col0, wr, wc, lane, slice);
+    } else {
+        // each set leaves the other one its sums of a half of the rows
+        static_assert(HALVES == 2 && FN == 2, "a row of blocks for each");
+        end_floatx4 *const sums = reinterpret_cast<end_floatx4 *>(lds);
+        end_floatx4 mine[1][FM];
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            sums[((half * WC * WR + wave) * FM + i) * 64 + lane] = half == 0 ? acc[1][i] : acc[0][i];
+            mine[0][i] = half == 0 ? acc[0][i] : acc[1][i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < FM; ++i) mine[0][i] += sums[(((1 - half) * WC * WR + wave) * FM + i) * 64 + lane];
+        constexpr int SUMS = HALVES * WC * WR * FM * 1024;
+        linear_end<T, END, FM, 1, WR * 2, WC>(args, mine, lds + SUMS + (half * WC * WR + wave) * REGION, reinterpret_cast<float2 *>(lds + SUMS + 2 * WC * WR * REGION), row0, col0,
+                                              wr * 2 + half, wc, lane, slice);
+    }
 #else
     (void)args, (void)group, (void)slice;
 #endif
 }
 
-template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES> __global__ __launch_bounds__(WC *WR * 64) void linear_dma_kernel(const LinearArgs args)
+template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES, int HALVES> __global__ __launch_bounds__(WC *WR *HALVES * 64) void linear_dma_kernel(const LinearArgs args)
 {
-    linear_dma_tile<T, FORM, END, BC, BR, WC, WR, STAGES>(args, blockIdx.x, blockIdx.z);
+    linear_dma_tile<T, FORM, END, BC, BR, WC, WR, STAGES, HALVES>(args, blockIdx.x, blockIdx.z);
 }
 
 template <int BC, int BR, int WC, int WR, int STAGES> constexpr int linear_dma_lds()
@@ -297,16 +319,16 @@ template <int BC, int BR, int WC, int WR, int STAGES> constexpr int linear_dma_l
     return stages > end ? stages : end;
 }
 
-template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES> hipError_t launch_linear_dma_as(LinearArgs args, int slices, hipStream_t stream)
+template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STAGES, int HALVES> hipError_t launch_linear_dma_as(LinearArgs args, int slices, hipStream_t stream)
 {
-    constexpr int LDS = linear_dma_lds<BC, BR, WC, WR, STAGES>();
+    constexpr int LDS = HALVES * linear_dma_lds<BC, BR, WC, WR, STAGES>();
     static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
     static RaisedLds raised;
-    auto kernel = linear_dma_kernel<T, FORM, END, BC, BR, WC, WR, STAGES>;
+    auto kernel = linear_dma_kernel<T, FORM, END, BC, BR, WC, WR, STAGES, HALVES>;
     if (const hipError_t e = raised(reinterpret_cast<const void *>(kernel), LDS)) return e;
     args.tiles_c = (args.cols + BC - 1) / BC;
     args.tiles_r = (args.rows + BR - 1) / BR;
-    kernel<<<dim3(static_cast<uint32_t>(args.tiles_c) * args.tiles_r, 1, slices), WC * WR * 64, LDS, stream>>>(args);
+    kernel<<<dim3(static_cast<uint32_t>(args.tiles_c) * args.tiles_r, 1, slices), WC * WR * HALVES * 64, LDS, stream>>>(args);
     return hipGetLastError();
 }
 
@@ -318,9 +340,10 @@ template <int FORM, int END> hipError_t launch_linear_dma(int dtype, int tile, c
     auto with = [&](auto type) {
         using T = decltype(type);
         if (tile == LINEAR_256) return launch_linear_pp<T, FORM, END>(args, slices, stream);
-        if (tile == LINEAR_128) return launch_linear_dma_as<T, FORM, END, 128, 128, 2, 2, 2>(args, slices, stream);
-        if (tile == LINEAR_128_DEEP) return launch_linear_dma_as<T, FORM, END, 128, 128, 2, 2, 4>(args, slices, stream);
-        return launch_linear_dma_as<T, FORM, END, 64, 64, 2, 2, 4>(args, slices, stream);
+        if (tile == LINEAR_128) return launch_linear_dma_as<T, FORM, END, 128, 128, 2, 2, 2, 1>(args, slices, stream);
+        if (tile == LINEAR_128_DEEP) return launch_linear_dma_as<T, FORM, END, 128, 128, 2, 2, 4, 1>(args, slices, stream);
+        if (tile == LINEAR_64_TWICE) return launch_linear_dma_as<T, FORM, END, 64, 64, 2, 2, 4, 2>(args, slices, stream);
+        return launch_linear_dma_as<T, FORM, END, 64, 64, 2, 2, 4, 1>(args, slices, stream);
     };
     return dtype == MG_F16 ? with(_Float16{}) : with(bfloat{});
 }

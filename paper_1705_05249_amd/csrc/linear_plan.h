@@ -15,23 +15,24 @@ struct LinearPlan {
 // What a tile takes, in us, measured with random bfloat16 operands: `alone` for 64 values of the sum while a compute unit has one of its tiles, `pair` while it has two
 // at a time (LDS has room for two of 128 or 64); around the sum `start`, and `more` for every tile of a compute unit (C leaves).  Operands across the sum cost more
 // reads of LDS (`form`).  Estimated and measured: 2048^3 on 128_DEEP 23 and 21.7, 4096 x 4096 x 2048 on 256 55 and 57, on 128 74 and 72, 8192 x 8192 x 512 on 256
-// 75 and 89, 1000 x 9999 x 1001 on 128 37 and 36, on 256 33 and 31, 8192 x 1024 x 1024 on 128 22 and 21.5, 512 x 2048 x 2048 on 64 11.6 and 10.9,
-// 333 x 1001 x 1999 on 64 11.6 and 10.5.
+// 75 and 89, 1000 x 9999 x 1001 on 128 37 and 36, on 256 33 and 31, 8192 x 1024 x 1024 on 128 22 and 21.5, 512 x 2048 x 2048 on 64 10.6 and 10.7,
+// with two sets of wavefronts 9.5 and 9.3; 1024^3 7.1 and 7.3, with two sets 7.0 and 6.9; 64 x 2048 x 8192 31.2 and 30.9, with two sets 24.3 and 23.7.
 struct LinearCost {
     double alone, pair, start, more;
 };
 inline LinearCost linear_cost(int tile, int form)
 {
     LinearCost c{};
-    double across = 1;                     // FORM_NN; half as much more for FORM_KN
+    double one = 1, both = 1;              // FORM_KN, FORM_NN
     switch (tile) {
-        case LINEAR_256: c = {1.4, 2.8, 4, 6.5}; across = 1.08; break;
-        case LINEAR_128: c = {0.82, 1.0, 3, 1.6}; across = 1.08; break;
-        case LINEAR_128_DEEP: c = {0.57, 1.14, 2.5, 2}; across = 1.08; break;
-        case LINEAR_64: c = {0.3, 0.42, 1.5, 0.5}; across = 1.2; break;
-        default: c = {0.5, 0.7, 3, 1.5}; across = 1.5; break;
+        case LINEAR_256: c = {1.4, 2.8, 4, 6.5}; one = 1.04; both = 1.08; break;
+        case LINEAR_128: c = {0.82, 1.0, 3, 1.6}; one = 1.04; both = 1.08; break;
+        case LINEAR_128_DEEP: c = {0.57, 1.14, 2.5, 2}; one = 1.04; both = 1.08; break;
+        case LINEAR_64: c = {0.215, 0.4, 3.2, 0.5}; one = 1.42; both = 1.35; break;
+        case LINEAR_64_TWICE: c = {0.155, 0.31, 2.5, 2}; one = 1.42; both = 1.35; break;
+        default: c = {0.5, 0.7, 3, 1.5}; one = 1.25; both = 1.5; break;
     }
-    const double factor = form == FORM_NN ? across : form == FORM_KN ? (1 + across) / 2 : 1;
+    const double factor = form == FORM_NN ? both : form == FORM_KN ? one : 1;
     c.alone *= factor;
     c.pair *= factor;
     return c;
@@ -49,12 +50,13 @@ inline LinearPlan linear_plan(int form, int end, int64_t rows, int64_t cols, int
         best.tile = aligned ? LINEAR_FEW : LINEAR_ANY_FEW;
         return best;
     }
-    for (const int tile : {int(LINEAR_256), int(LINEAR_128), int(LINEAR_128_DEEP), int(LINEAR_64), int(LINEAR_ANY)}) {
+    for (const int tile : {int(LINEAR_256), int(LINEAR_128), int(LINEAR_128_DEEP), int(LINEAR_64), int(LINEAR_64_TWICE), int(LINEAR_ANY)}) {
         if (aligned != (tile != LINEAR_ANY)) continue;
         const int64_t size = linear_tile_size(tile), tiles = ceil_div(rows, size) * ceil_div(cols, size);
         const LinearCost c = linear_cost(tile, form);
         for (int s = 1; s <= 64; s *= 2) {
             if (s > 1 && (end != END_STORE || pieces / s < 4 || one * s > static_cast<double>(room) || tiles * s > 1024)) break;
+            if (tile == LINEAR_64_TWICE && tiles * s > 256) break;      // (two of them do not share a compute unit: 700 x 1536 x 1536, 264 tiles, 11.8 and 14.6 us)
             const double per_unit = static_cast<double>(ceil_div(tiles * s, 256));
             const double pairs = static_cast<double>(ceil_div(tiles * s, 256) / 2), piece = pairs * c.pair + (per_unit - 2 * pairs) * c.alone;
             const double us = c.start + c.more * per_unit + pieces / s * piece + (s > 1 ? 6 + one * (s + 1) / 4e6 : 0);
@@ -111,7 +113,7 @@ inline LinearPlan linear_plan_together(const LinearSize (&sizes)[3], size_t room
             for (int n = 0; n < 3; ++n) as_long += 2 * pieces[n] >= longest ? tiles[n] : 0;
             const double length = static_cast<double>(longest), last = as_long <= 256 ? length * alone : static_cast<double>(ceil_div(as_long, 512)) * length * 2 * half;
             const double body = work / 256 * half + length * alone * tail;
-            const double us = start + more * static_cast<double>(groups) / 256 + (body > last ? body : last) + (s > 1 ? 2 + one * (2 * s + 1) / 1.2e7 : 0);
+            const double us = start + more * static_cast<double>(groups) / 256 + (body > last ? body : last) + (s > 1 ? 2 + one * (2 * s + 1) / 8e6 : 0);
             if (us < 0.97 * least) {                     // (what is not clearly ahead is not taken)
                 least = us;
                 best = {tile, static_cast<int>(ceil_div(k, each)), static_cast<int>(each), us};

@@ -14,10 +14,10 @@ template <typename T, int SIZE, int STAGES> __global__ __launch_bounds__(256) vo
     if (group < all.begin[1]) {
         const LinearArgs &args = all.of[0];
         const uint32_t tiles = static_cast<uint32_t>(args.tiles_c) * args.tiles_r, slice = group / tiles;
-        linear_dma_tile<T, FORM_KN, END_STORE, SIZE, SIZE, 2, 2, STAGES>(args, group - slice * tiles, slice);
+        linear_dma_tile<T, FORM_KN, END_STORE, SIZE, SIZE, 2, 2, STAGES, 1>(args, group - slice * tiles, slice);
     } else {
         const int n = group < all.begin[2] ? 1 : 2;
-        linear_dma_tile<T, FORM_NN, END_STORE, SIZE, SIZE, 2, 2, STAGES>(all.of[n], group - all.begin[n], 0);
+        linear_dma_tile<T, FORM_NN, END_STORE, SIZE, SIZE, 2, 2, STAGES, 1>(all.of[n], group - all.begin[n], 0);
     }
 }
 

@@ -4,7 +4,7 @@ import subprocess
 import tempfile
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-KERNELS = {0: "256", 1: "128", 2: "64", 3: "128 deep", 4: "few", -1: "any", -2: "any few"}
+KERNELS = {0: "256", 1: "128", 2: "64", 3: "128 deep", 4: "few", 5: "64 twice", -1: "any", -2: "any few"}
 FORMS = {"kk": 0, "kn": 1, "nn": 2}
 ENDS = {"store": 0, "gated": 1, "gated_grad": 2, "scores": 3, "scores_grad": 4}
 

@@ -37,7 +37,7 @@ def built(kind):
 
 
 def dma():
-    tiles = {(128, 128, 2, 2, 2), (128, 128, 2, 2, 4), (64, 64, 2, 2, 4)}
+    tiles = {(128, 128, 2, 2, 2, 1), (128, 128, 2, 2, 4, 1), (64, 64, 2, 2, 4, 1), (64, 64, 2, 2, 4, 2)}
     return {(kind, *pair, *tile) for kind in (False, True) for pair in PAIRS for tile in tiles}
 
 
