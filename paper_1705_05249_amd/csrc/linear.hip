@@ -48,11 +48,13 @@ __global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
     }
     int m = 0;
     while (m + 1 < c.count && group >= c.begin[m + 1]) ++m;
-    const int64_t piece = (group - c.begin[m]) * int64_t(256) + threadIdx.x;
-    const int cols = c.cols[m], per_row = static_cast<int>(padded(cols) / 8);
-    const int64_t row = piece / per_row;
+    // (a matrix of 2^34 elements and the columns that it is padded with are fewer than 2^32 pieces)
+    const uint32_t piece = (group - c.begin[m]) * 256 + threadIdx.x;
+    const int cols = c.cols[m];
+    const uint32_t per_row = static_cast<uint32_t>(padded(cols) / 8), in_column = piece / per_row;
+    const int64_t row = in_column;
     if (row >= c.rows[m]) return;
-    const int col = static_cast<int>(piece - row * per_row) * 8;
+    const int col = static_cast<int>(piece - in_column * per_row) * 8;
     int left = cols - col;
     if (m == 0 && c.targets != nullptr) {
         // nothing times an infinity is no number: a token that does not count must not reach the sums over tokens
