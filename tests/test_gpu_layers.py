@@ -1,6 +1,7 @@
 """Gated blocks, the loss over a vocabulary and clipping on the GPU against 64 bits (layer_reference.py), within bounds element by element."""
 import functools
 import math
+import threading
 
 import pytest
 import torch
@@ -607,6 +608,29 @@ def test_two_streams_at_once():
                 got[n].append(D.train_step(*model, 0.05)[2])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for n in (0, 1) for grads in got[n] for a, b in zip(grads, want[n]))
+
+
+def test_calls_from_several_threads():
+    """the interpreter's lock is released in a call: every thread has a stream and workspaces of its own"""
+    block, head, x, targets = make(torch.float16, tokens=300)
+    want = [t.clone() for t in D.train_step(block, head, x, targets, 0.05)[2]]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work():
+        with torch.cuda.stream(torch.cuda.Stream()):
+            model = D.GatedBlock(block.gate, block.up, block.down), D.VocabLoss(head.weights)
+            for _ in range(10):
+                grads = D.train_step(*model, x, targets, 0.05)[2]
+            torch.cuda.current_stream().synchronize()
+            wrong.extend(not torch.equal(a, b) for a, b in zip(grads, want))
+
+    threads = [threading.Thread(target=work) for _ in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(wrong) == 16 and not any(wrong)
 
 
 def test_other_default_types_and_devices():
