@@ -3,7 +3,8 @@
 // Forward, 16 bits: one product with gate and up weights as one matrix, 16 rows of each in turn, so that a lane holds g and u of the same element and
 // H leaves the kernel (6 tokens width hidden operations in two launches); then Y.  Backward: dH never exists in memory, dG and dU leave its product, made of what
 // the forward pass kept without another look at the activation;
-// dX is one sum over 2 hidden, dG's half and dU's; the gradients of gate and up weights are one product with twice the rows.
+// dX is one sum over 2 hidden, dG's half and dU's; the gradients of gate and up weights are one product with twice the rows; these and the down weights' go in one
+// launch where that pays (linear_together.hip).
 // FP32: products as mg_sgemm makes them, with G and U in memory.
 #include "linear_end.h"
 #include "internal.h"
