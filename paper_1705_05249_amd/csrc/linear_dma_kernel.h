@@ -332,7 +332,7 @@ template <typename T, int FORM, int END, int BC, int BR, int WC, int WR, int STA
     return hipGetLastError();
 }
 
-template <typename T, int FORM, int END> hipError_t launch_linear_pp(LinearArgs args, int slices, hipStream_t stream);      // linear_pp_kernel.h
+template <typename T, int FORM, int END> hipError_t launch_linear_pp(const LinearArgs &args, int slices, hipStream_t stream);      // linear_pp_kernel.h
 
 // the kernels of one form and end, all tiles
 template <int FORM, int END> hipError_t launch_linear_dma(int dtype, int tile, const LinearArgs &args, int slices, hipStream_t stream)

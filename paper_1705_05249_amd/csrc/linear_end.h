@@ -57,7 +57,18 @@ template <typename T> __device__ inline void end_stage(char *at, float a, float 
 }
 
 // A block of a and b of what is kept (kept_block), this lane's four of each.  bfloat16: 16 bytes a lane, then the lanes' exponents.
-template <typename T> __device__ inline void keep(void *kept, int64_t block, int lane, const float (&a)[4], const float (&b)[4])
+// PAST: by the caches
+template <bool PAST, typename V> __device__ inline void put_kept(V v, void *at)
+{
+    if constexpr (PAST) __builtin_nontemporal_store(v, static_cast<V *>(at));
+    else *static_cast<V *>(at) = v;
+}
+template <bool PAST, typename V> __device__ inline V get_kept(const void *at)
+{
+    if constexpr (PAST) return __builtin_nontemporal_load(static_cast<const V *>(at));
+    else return *static_cast<const V *>(at);
+}
+template <typename T, bool PAST> __device__ inline void keep(void *kept, int64_t block, int lane, const float (&a)[4], const float (&b)[4])
 {
     if constexpr (std::is_same_v<T, bfloat>) {
         char *const at = static_cast<char *>(kept) + block * kept_block_bytes(MG_BF16);
@@ -80,22 +91,22 @@ template <typename T> __device__ inline void keep(void *kept, int64_t block, int
             y.v[e] = static_cast<_Float16>(ldexpf(b[e], kb));
         }
         const uint64_t both[2] = {__builtin_bit_cast(uint64_t, x), __builtin_bit_cast(uint64_t, y)};
-        *reinterpret_cast<end_floatx4 *>(at + 16 * lane) = __builtin_bit_cast(end_floatx4, both);
-        *reinterpret_cast<uint16_t *>(at + 1024 + 2 * lane) = static_cast<uint16_t>((ka & 0xff) | (kb & 0xff) << 8);
+        put_kept<PAST>(__builtin_bit_cast(end_floatx4, both), at + 16 * lane);
+        put_kept<PAST>(static_cast<uint16_t>((ka & 0xff) | (kb & 0xff) << 8), at + 1024 + 2 * lane);
     } else {
         float *const at = reinterpret_cast<float *>(static_cast<char *>(kept) + block * kept_block_bytes(MG_F16)) + 4 * lane;
-        *reinterpret_cast<end_floatx4 *>(at) = end_floatx4{a[0], a[1], a[2], a[3]};
-        *reinterpret_cast<end_floatx4 *>(at + 256) = end_floatx4{b[0], b[1], b[2], b[3]};
+        put_kept<PAST>(end_floatx4{a[0], a[1], a[2], a[3]}, at);
+        put_kept<PAST>(end_floatx4{b[0], b[1], b[2], b[3]}, at + 256);
     }
 }
 // The way back: a block's load, which may be early, and what it holds
 template <typename T> struct Kept {
     end_floatx4 x, y;
-    __device__ inline void load(const void *kept, int64_t block, int lane)
+    template <bool PAST> __device__ inline void load(const void *kept, int64_t block, int lane)
     {
         const float *const at = reinterpret_cast<const float *>(static_cast<const char *>(kept) + block * kept_block_bytes(MG_F16)) + 4 * lane;
-        x = *reinterpret_cast<const end_floatx4 *>(at);
-        y = *reinterpret_cast<const end_floatx4 *>(at + 256);
+        x = get_kept<PAST, end_floatx4>(at);
+        y = get_kept<PAST, end_floatx4>(at + 256);
     }
     __device__ inline void recall(float (&a)[4], float (&b)[4]) const
     {
@@ -109,11 +120,11 @@ template <typename T> struct Kept {
 template <> struct Kept<bfloat> {
     end_floatx4 x;
     uint16_t k;
-    __device__ inline void load(const void *kept, int64_t block, int lane)
+    template <bool PAST> __device__ inline void load(const void *kept, int64_t block, int lane)
     {
         const char *const at = static_cast<const char *>(kept) + block * kept_block_bytes(MG_BF16);
-        x = *reinterpret_cast<const end_floatx4 *>(at + 16 * lane);
-        k = *reinterpret_cast<const uint16_t *>(at + 1024 + 2 * lane);
+        x = get_kept<PAST, end_floatx4>(at + 16 * lane);
+        k = get_kept<PAST, uint16_t>(at + 1024 + 2 * lane);
     }
     __device__ inline void recall(float (&a)[4], float (&b)[4]) const
     {
@@ -133,7 +144,7 @@ template <> struct Kept<bfloat> {
 // Columns of H, dG and dU that are written: zeros from `hidden` on
 __device__ inline int held_columns(int hidden) { return (hidden + 15) / 16 * 16; }
 
-template <int ACT, typename T, int FM, int FN> __device__ __forceinline__ void end_gated(const LinearArgs &args, const end_floatx4 (&acc)[FN][FM], char *region, int row0, int col0, int lane)
+template <int ACT, typename T, bool PAST, int FM, int FN> __device__ __forceinline__ void end_gated(const LinearArgs &args, const end_floatx4 (&acc)[FN][FM], char *region, int row0, int col0, int lane)
 {
     constexpr int HALF = FM / 2, ROWB = HALF * 32 + 16;
     const int out0 = col0 / 2, held = held_columns(args.hidden);
@@ -152,7 +163,7 @@ template <int ACT, typename T, int FM, int FN> __device__ __forceinline__ void e
                 activation_of<ACT>(g[e], a[e], slope);
                 b[e] = u[e] * slope;
             }
-            if (args.kept != nullptr && row < args.rows && out0 + 16 * i < held) keep<T>(args.kept, kept_block(row, out0 + 16 * i, args.hidden), lane, a, b);
+            if (args.kept != nullptr && row < args.rows && out0 + 16 * i < held) keep<T, PAST>(args.kept, kept_block(row, out0 + 16 * i, args.hidden), lane, a, b);
             end_stage<T>(region + (lane % 16) * ROWB + i * 32 + (lane / 16) * 8, a[0] * u[0], a[1] * u[1], a[2] * u[2], a[3] * u[3]);
         }
         end_fence();
@@ -160,7 +171,7 @@ template <int ACT, typename T, int FM, int FN> __device__ __forceinline__ void e
     }
 }
 
-template <typename T, int FM, int FN> __device__ __forceinline__ void end_gated_grad(const LinearArgs &args, const end_floatx4 (&acc)[FN][FM], char *region, int row0, int col0, int lane)
+template <typename T, bool PAST, int FM, int FN> __device__ __forceinline__ void end_gated_grad(const LinearArgs &args, const end_floatx4 (&acc)[FN][FM], char *region, int row0, int col0, int lane)
 {
     constexpr int ROWB = FM * 32 + 16;
     const int held = held_columns(args.hidden);
@@ -175,7 +186,7 @@ template <typename T, int FM, int FN> __device__ __forceinline__ void end_gated_
 #pragma unroll
         for (int i = from; i < to; ++i) {
             const int col = col0 + 16 * i < held ? col0 + 16 * i : held - 1;
-            kept[j % 2][i].load(args.kept, kept_block(row, col, args.hidden), lane);
+            kept[j % 2][i].template load<PAST>(args.kept, kept_block(row, col, args.hidden), lane);
         }
     };
     ask(0, 0, EARLY);
@@ -238,7 +249,7 @@ __device__ inline float2 join_scores(float2 a, float2 b)
 
 // All WR x WC wavefronts that share a tile come here, and nobody uses the LDS any more.  The wavefront's tile starts at (row0, col0) and is wavefront
 // (wr, wc) of WR x WC; region: its own; shared: WR * FN * 16 * WC float2 that no region overlaps (END_SCORES).
-template <typename T, int END, int FM, int FN, int WR, int WC>
+template <typename T, int END, int FM, int FN, int WR, int WC, bool PAST = false>
 __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (&acc)[FN][FM], char *region, float2 *shared, int tile_row, int tile_col, int wr, int wc, int lane, int slice = 0)
 {
     const int row0 = tile_row + wr * FN * 16, col0 = tile_col + wc * FM * 16;
@@ -274,12 +285,12 @@ __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (
             }
         }
     } else if constexpr (END == END_GATED) {
-        if (args.activation == MG_ACT_SILU) end_gated<MG_ACT_SILU, T>(args, acc, region, row0, col0, lane);
-        else if (args.activation == MG_ACT_GELU) end_gated<MG_ACT_GELU, T>(args, acc, region, row0, col0, lane);
-        else if (args.activation == MG_ACT_GELU_TANH) end_gated<MG_ACT_GELU_TANH, T>(args, acc, region, row0, col0, lane);
-        else end_gated<MG_ACT_RELU2, T>(args, acc, region, row0, col0, lane);
+        if (args.activation == MG_ACT_SILU) end_gated<MG_ACT_SILU, T, PAST>(args, acc, region, row0, col0, lane);
+        else if (args.activation == MG_ACT_GELU) end_gated<MG_ACT_GELU, T, PAST>(args, acc, region, row0, col0, lane);
+        else if (args.activation == MG_ACT_GELU_TANH) end_gated<MG_ACT_GELU_TANH, T, PAST>(args, acc, region, row0, col0, lane);
+        else end_gated<MG_ACT_RELU2, T, PAST>(args, acc, region, row0, col0, lane);
     } else if constexpr (END == END_GATED_GRAD) {
-        end_gated_grad<T>(args, acc, region, row0, col0, lane);
+        end_gated_grad<T, PAST>(args, acc, region, row0, col0, lane);
     } else if constexpr (END == END_SCORES) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) {

@@ -371,7 +371,7 @@ def test_tokens_that_do_not_count_may_hold_anything():
 
 
 # sizes at which the large tiles are taken (tests/test_linear_plan.py says which by which product)
-LARGE_BLOCKS = [(3999, 520, 4000), (4000, 4008, 520), (520, 4000, 2000), (3970, 515, 4001), (1500, 1032, 1000), (1000, 1000, 9992), (2500, 2600, 300), (2100, 520, 2500), (2100, 2048, 4100)]
+LARGE_BLOCKS = [(3999, 520, 4000), (4000, 4008, 520), (520, 4000, 2000), (3970, 515, 4001), (1500, 1032, 1000), (1000, 1000, 9992), (2500, 2600, 300), (2100, 520, 2500), (2100, 2048, 4100), (5500, 264, 5600)]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])

@@ -32,7 +32,7 @@ def built(kind):
     for code in code_objects():
         for name, arguments in NAME.findall(code):
             if name.decode() == kind:
-                found.add((arguments.startswith(b"DF16b"), *(int(v) for v in re.findall(rb"Li(\d+)E?", arguments))))
+                found.add((arguments.startswith(b"DF16b"), *(int(v) for v in re.findall(rb"L[ib](\d+)E?", arguments))))
     return found
 
 
@@ -42,8 +42,8 @@ def dma():
 
 
 def pp():
-    """the 256 x 256 tile"""
-    return {(kind, *pair) for kind in (False, True) for pair in PAIRS}
+    """the 256 x 256 tile; what a block keeps passes the caches by or does not"""
+    return {(kind, *pair, past) for kind in (False, True) for pair in PAIRS for past in (0, 1) if not past or pair in ((KK, GATED), (KN, GATED_GRAD))}
 
 
 def test_kernels_that_are_built():

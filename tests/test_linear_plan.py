@@ -33,6 +33,9 @@ def test_the_gpu_tests_reach_every_kernel():
     asked = [p for c, j in zip(calls, joined) for p in c if j[0] == "any" or p[0] == "kk" or p[1] != "store"]
     asked += [p for c in G.ONE_GRADIENT for p in block(*c)]
     taken = {(form, end, kernel) for (form, end, *_), (kernel, _, _) in zip(asked, choices(asked))}
+    # what a block keeps passes the caches by from 128 MB on, on the largest tiles
+    tokens, width, hidden = G.LARGE_BLOCKS[-1]
+    assert tokens // 16 * (hidden // 16) * 1152 >= 1 << 27 and [c[0] for c in choices([block(tokens, width, hidden)[i] for i in (0, 2)])] == ["256", "256"]
     pairs = {(form, end) for form, end, *_ in asked}
     missing = {(*pair, tile) for pair in pairs for tile in ("256", "128", "64", "64 twice")} - taken
     assert not missing, missing
