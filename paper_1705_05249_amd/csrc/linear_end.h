@@ -12,6 +12,7 @@ namespace mg {
 #if defined(__HIPCC__)
 
 typedef float end_floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t end_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
 
 // LDS bytes of a wavefront's region: 16 rows of its columns in FP32 or two matrices of 16 bits, 16 bytes apart from each other's banks
 template <int WTM> constexpr int end_region() { return 16 * (WTM * 4 + 16); }
@@ -28,7 +29,7 @@ template <typename T> struct __attribute__((packed, aligned(8))) Four {
 };
 
 // COLS columns of 16 rows, U elements, in the wavefront's region -> base(row) + col; rows below `rows`, columns below `cols`
-template <typename U, int COLS, typename Row> __device__ inline void end_drain(const char *region, int row_bytes, int row, int col, int rows, int cols, int lane, Row &&at)
+template <typename U, int COLS, bool PAST = false, typename Row> __device__ inline void end_drain(const char *region, int row_bytes, int row, int col, int rows, int cols, int lane, Row &&at)
 {
     constexpr int PER = 16 / static_cast<int>(sizeof(U)), CH = COLS / PER;
     static_assert(COLS % PER == 0, "whole pieces");
@@ -41,7 +42,8 @@ template <typename U, int COLS, typename Row> __device__ inline void end_drain(c
         const Piece<U, PER> x = __builtin_bit_cast(Piece<U, PER>, *reinterpret_cast<const end_floatx4 *>(region + r * row_bytes + c * 16));
         U *to = at(row + r) + col + c * PER;
         if (left >= PER) {
-            *reinterpret_cast<Piece<U, PER> *>(to) = x;
+            if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(end_u32x4, x), reinterpret_cast<end_u32x4 *>(to));
+            else *reinterpret_cast<Piece<U, PER> *>(to) = x;
         } else {
 #pragma unroll
             for (int e = 0; e < PER; ++e)
@@ -376,7 +378,7 @@ __device__ __forceinline__ void linear_end(const LinearArgs &args, end_floatx4 (
                 if (at >= 0) *reinterpret_cast<T *>(region + (lane % 16) * ROWB + (at / 4 * 16 + lane / 16 * 4 + at % 4) * 2) = static_cast<T>(w != 0.f ? w * p : 0.f);
             }
             end_fence();
-            end_drain<T, FM * 16>(region, ROWB, row0 + 16 * j, col0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
+            end_drain<T, FM * 16, PAST>(region, ROWB, row0 + 16 * j, col0, args.rows, held, lane, [&](int r) { return C + r * args.ldc0; });
         }
     }
 }

@@ -97,7 +97,7 @@ template <typename T> __device__ inline void multiply_in_place(floatx4 &acc, con
 
 constexpr int LINEAR_PP_LDS = 4 * 32768 + 1024;
 
-// PAST (END_GATED, END_GATED_GRAD): what a block keeps passes the caches by
+// PAST: what a block keeps (END_GATED, END_GATED_GRAD) or dz (END_SCORES_GRAD) passes the caches by
 template <typename T, int FORM, int END, bool PAST> __global__ __launch_bounds__(512) void linear_pp_kernel(const LinearArgs args)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -312,12 +312,15 @@ template <typename T, int FORM, int END, bool PAST> hipError_t launch_linear_pp_
 }
 
 // What does not stay in the last-level cache (256 MB) until the backward pass comes for it leaves it to what does.  302 MB (8192 x 8192 elements in bfloat16): the forward product of
-// width 2048 453 -> 438 us, the backward one 294 -> 279; 52 MB: backward 39.7 through the caches and 42.3 past them.
+// width 2048 453 -> 438 us, the backward one 294 -> 279; 52 MB: backward 39.7 through the caches and 42.3 past them.  dz of 256 MB and more: the step of the loss of
+// 8192 x 2048 x 65536, 537 MB a piece, 6633 -> 6545 us.
 template <typename T, int FORM, int END> hipError_t launch_linear_pp(const LinearArgs &args, int slices, hipStream_t stream)
 {
     if constexpr (END == END_GATED || END == END_GATED_GRAD)
         if (args.kept != nullptr && kept_blocks(args.hidden) * ((args.rows + 15) / 16) * kept_block_bytes(std::is_same_v<T, bfloat> ? MG_BF16 : MG_F16) >= int64_t(128) << 20)
             return launch_linear_pp_as<T, FORM, END, true>(args, slices, stream);
+    if constexpr (END == END_SCORES_GRAD)
+        if (static_cast<int64_t>(args.rows) * args.cols >= int64_t(1) << 27) return launch_linear_pp_as<T, FORM, END, true>(args, slices, stream);
     return launch_linear_pp_as<T, FORM, END, false>(args, slices, stream);
 }
 

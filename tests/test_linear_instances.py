@@ -42,8 +42,8 @@ def dma():
 
 
 def pp():
-    """the 256 x 256 tile; what a block keeps passes the caches by or does not"""
-    return {(kind, *pair, past) for kind in (False, True) for pair in PAIRS for past in (0, 1) if not past or pair in ((KK, GATED), (KN, GATED_GRAD))}
+    """the 256 x 256 tile; what a block keeps, or dz, passes the caches by or does not"""
+    return {(kind, *pair, past) for kind in (False, True) for pair in PAIRS for past in (0, 1) if not past or pair in ((KK, GATED), (KN, GATED_GRAD), (KK, SCORES_GRAD))}
 
 
 def test_kernels_that_are_built():
