@@ -19,6 +19,11 @@ TYPES = {torch.float32: L.MG_F32, torch.float16: L.MG_F16, torch.bfloat16: L.MG_
 ACTIVATIONS = {"silu": L.MG_ACT_SILU, "gelu": L.MG_ACT_GELU, "gelu_tanh": L.MG_ACT_GELU_TANH, "relu2": L.MG_ACT_RELU2}
 
 
+def _check_current(name, device):
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
 def _checked(name, tensor, shape, device, types):
     """the tensor with dense rows: the library's calls take addresses and believe what they are told of the memory behind them"""
     if tensor.dtype not in types:
@@ -27,8 +32,7 @@ def _checked(name, tensor, shape, device, types):
         raise ValueError(f"{name}: shape {tuple(tensor.shape)}, expected {tuple(shape)}")
     if tensor.device != device or not tensor.is_cuda:
         raise ValueError(f"{name}: on {tensor.device}, expected on {device if device.type == 'cuda' else 'the GPU'}")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {device}, but the current device is cuda:{torch.cuda.current_device()}")
+    _check_current(name, device)
     tensor = tensor.detach()
     if tensor.dim() == 2 and tensor.numel() and (tensor.stride(1) != 1 or tensor.stride(0) < tensor.shape[1]):
         return tensor.contiguous()
@@ -132,6 +136,7 @@ class Gradients:
                 raise TypeError(f"tensor {i}: {t.dtype} is none of {', '.join(str(k) for k in TYPES)}")
             if not t.is_cuda or t.device != self.tensors[0].device:
                 raise ValueError(f"tensor {i}: on {t.device}, expected on {self.tensors[0].device if self.tensors[0].is_cuda else 'the GPU'}")
+            _check_current(f"tensor {i}", t.device)
             if not t.is_contiguous():
                 raise ValueError(f"tensor {i}: not dense")
         # (scaled in place, a number that is listed twice would be scaled twice)

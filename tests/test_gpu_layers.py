@@ -647,6 +647,18 @@ def test_other_default_types_and_devices():
     assert loss.dtype == norm.dtype == torch.float32 and all(torch.equal(a, b) for a, b in zip(grads, want))
 
 
+def test_other_devices_are_refused(monkeypatch):
+    """the calls would go to the current device's stream"""
+    block, head, x, targets = make(torch.float16)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device is cuda:1"):
+        block.forward(x)
+    with pytest.raises(ValueError, match="current device is cuda:1"):
+        head.forward(x, targets)
+    with pytest.raises(ValueError, match="current device is cuda:1"):
+        D.Gradients([x])
+
+
 def test_memory_that_is_listed_twice():
     g = torch.ones(100, device="cuda")
     with pytest.raises(ValueError, match="0 and 1 share memory"):
