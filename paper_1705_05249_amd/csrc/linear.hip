@@ -106,6 +106,7 @@ hipError_t launch_linear_copies(LinearCopies c, hipStream_t stream)
     c.begin[0] = 0;
     for (int m = 0; m < c.count; ++m) c.begin[m + 1] = c.begin[m] + static_cast<uint32_t>(ceil_div(c.rows[m] * (padded(c.cols[m]) / 8), 256));
     const uint32_t groups = c.begin[c.count] + (c.scale != nullptr ? 1 : 0), wide = groups < COPY_GROUPS ? groups : COPY_GROUPS;
+    if (groups == 0) return hipSuccess;               // matrices without rows or columns
     copy_kernel<<<dim3(wide, (groups + wide - 1) / wide), 256, 0, stream>>>(c);
     return hipGetLastError();
 }

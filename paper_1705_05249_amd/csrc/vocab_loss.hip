@@ -206,7 +206,7 @@ struct LossOperands {
 bool copy_of(LinearCopies &list, Arena &ws, const void *&at, int64_t &ld, int64_t rows, int64_t width)
 {
     const size_t bytes = static_cast<size_t>(rows * padded(width)) * 2;
-    if ((width % 8 == 0 && reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 8 == 0) || ws.left() < bytes) return false;
+    if (bytes == 0 || (width % 8 == 0 && reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 8 == 0) || ws.left() < bytes) return false;
     const int m = list.count++;
     list.from[m] = at; list.to[m] = ws.take(bytes); list.ld[m] = ld; list.rows[m] = rows; list.cols[m] = static_cast<int>(width);
     at = list.to[m];

@@ -347,6 +347,26 @@ def test_losses_without_work(dtype):
     assert not bool(dx.x.any()) and not bool(dw.x.any()) and dw.untouched() and dx.untouched()
 
 
+@pytest.mark.parametrize("dtype", KINDS)
+@pytest.mark.parametrize("tokens", [191, 192, 300, 5000])
+def test_losses_without_width(tokens, dtype):
+    """all logits are zero, on every kernel that many tokens take, wherever the empty rows start"""
+    kind, code, targets = KINDS[dtype], CODES[KINDS[dtype]], torch.arange(tokens, device="cuda") % 8
+    for vocab, ldx, ldw in ((7, 1, 1), (7, 8, 8), (2000, 3, 8)):
+        loss, lse = (result(1, tokens, torch.float32) for _ in range(2))
+        ws = scratch(L.mg_vocab_loss_workspace_bytes(code, tokens, 0, vocab))[1]
+        L.mg_vocab_loss(code, tokens, 0, vocab, None, ldx, None, ldw, targets, loss.at()[0], lse.at()[0], ws)
+        torch.cuda.synchronize()
+        # a sum of `vocab` ones is exact, a logarithm off by a step
+        assert bool(((lse.x[0].double() - math.log(vocab)).abs() <= R.STEP * math.log(vocab)).all()) and loss.untouched() and lse.untouched()
+        assert torch.equal(loss.x[0], torch.where(targets < vocab, lse.x[0], 0.0))
+    head = D.VocabLoss(torch.zeros(7, 0, dtype=kind, device="cuda"))
+    loss = head.forward(torch.zeros(tokens, 0, dtype=kind, device="cuda"), targets)
+    assert bool(((loss.double() - math.log(7)).abs() <= R.STEP * math.log(7))[targets < 7].all()) and not bool(loss[targets == 7].any())
+    dx, dw = head.backward()
+    assert dx.shape == (tokens, 0) and dw.shape == (7, 0)
+
+
 def test_tokens_that_do_not_count_may_hold_anything():
     """infinities and NaN in ignored tokens and in tokens of weight zero stay where they are"""
     for kind in KINDS.values():

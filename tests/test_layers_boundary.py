@@ -3,6 +3,8 @@ import ctypes
 import math
 import os
 import re
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -184,3 +186,19 @@ def test_layers_refuse_what_the_calls_would_believe():
         D.Gradients([w])
     with pytest.raises(TypeError, match="int64"):
         D.Gradients([torch.zeros(3, dtype=torch.int64)])
+
+
+def test_copies_of_matrices_without_columns():
+    """width 0, with tokens from which copies of operands off 16 bytes start: nothing to copy.  In a process of its own, which sees no GPU: its launches fail"""
+    program = """
+import sys
+from paper_1705_05249_amd import layers as L
+for dtype in (L.MG_F16, L.MG_BF16, L.MG_F32):
+    for tokens in (191, 192, 300, 5000):
+        for ldx, ldw in ((1, 1), (8, 1), (1, 8), (8, 8), (3, 5)):
+            st = L.mg_vocab_loss(dtype, tokens, 0, 7, None, ldx, None, ldw, 1 << 16, 1 << 16, 1 << 16, type("M", (), dict(data_ptr=lambda s: 1 << 16, numel=lambda s: 1 << 40, element_size=lambda s: 1))(), stream=0, check=False)
+            assert st < 0, st
+print("done")
+"""
+    run = subprocess.run([sys.executable, "-c", program], cwd=ROOT, env={**os.environ, "HIP_VISIBLE_DEVICES": "-1"}, capture_output=True, text=True)
+    assert run.returncode == 0 and run.stdout.split()[-1] == "done", (run.returncode, run.stderr[-500:])
