@@ -123,6 +123,21 @@ struct LinearCopies {
     float most, *scale;
 };
 hipError_t launch_linear_copies(LinearCopies copies, hipStream_t stream);
+// Rows of `cols` units whose pieces of eight a launch counts in 32 bits.  Matrices of 16 bits (2^34 elements, fewer than 2^24 rows) have no more pieces than that; X of FP32, two
+// units an element, may have: 16 760 000 x 1025 has 4.4e9.  It is alone in its list and goes in parts.
+inline int64_t copy_rows(int64_t cols) { return cols == 0 ? INT64_MAX : (int64_t(1) << 32) / (padded(cols) / 8); }
+// the first rows of a list's only matrix leave the list
+inline LinearCopies take_copy_rows(LinearCopies &c, int64_t rows)
+{
+    LinearCopies first = c;
+    first.rows[0] = rows;
+    c.rows[0] -= rows;
+    c.from[0] = static_cast<const uint16_t *>(c.from[0]) + rows * c.ld[0];
+    c.to[0] = static_cast<uint16_t *>(c.to[0]) + rows * padded(c.cols[0]);
+    if (c.targets != nullptr) c.targets += rows;
+    if (c.weights != nullptr) c.weights += rows;
+    return first;
+}
 
 // Memory of a workspace, handed out on 256 bytes; without a base it only counts
 struct Arena {

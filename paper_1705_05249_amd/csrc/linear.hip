@@ -36,7 +36,7 @@ __device__ inline void weight_scale(const float *weights, int64_t tokens, float 
     scale[1] = largest == 0 ? 1.f : w / most;
 }
 
-constexpr uint32_t COPY_GROUPS = uint32_t(1) << 22;           // along x: a launch has fewer than 2^32 threads there, five matrices of 2^34 elements more pieces
+constexpr uint32_t COPY_GROUPS = uint32_t(1) << 22;           // along x: a launch has fewer than 2^32 threads there, five large matrices more pieces
 
 // A thread moves a piece of eight elements; the work-group behind the last matrix makes the scale.
 __global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
     }
     int m = 0;
     while (m + 1 < c.count && group >= c.begin[m + 1]) ++m;
-    // (a matrix of 2^34 elements and the columns that it is padded with are fewer than 2^32 pieces)
+    // (copy_rows: a launch has at most 2^32 of them in a matrix)
     const uint32_t piece = (group - c.begin[m]) * 256 + threadIdx.x;
     const int cols = c.cols[m];
     const uint32_t per_row = static_cast<uint32_t>(padded(cols) / 8), in_column = piece / per_row;
@@ -103,6 +103,11 @@ template <typename T> __global__ __launch_bounds__(256) void linear_sum_kernel(c
 hipError_t launch_linear_copies(LinearCopies c, hipStream_t stream)
 {
     if (c.count == 0) return hipSuccess;
+    if (c.count == 1 && c.scale == nullptr)
+        for (const int64_t most = copy_rows(c.cols[0]); c.rows[0] > most;)
+            if (const hipError_t e = launch_linear_copies(take_copy_rows(c, most), stream)) return e;
+    for (int m = 0; m < c.count; ++m)
+        if (c.rows[m] > copy_rows(c.cols[m])) return hipErrorInvalidValue;
     c.begin[0] = 0;
     for (int m = 0; m < c.count; ++m) c.begin[m + 1] = c.begin[m] + static_cast<uint32_t>(ceil_div(c.rows[m] * (padded(c.cols[m]) / 8), 256));
     const uint32_t groups = c.begin[c.count] + (c.scale != nullptr ? 1 : 0), wide = groups < COPY_GROUPS ? groups : COPY_GROUPS;
