@@ -98,7 +98,7 @@ hipError_t launch_linear_together(int dtype, LinearTogether all, void *room, siz
 // tile: LINEAR_128 or LINEAR_64; slices: of the first product, whose k_per_slice and `partial` say so
 hipError_t launch_linear_together_on(int dtype, int tile, LinearTogether all, int slices, hipStream_t stream);
 
-// adds the slices of END_STORE and writes C in dtype
+// adds the slices of END_STORE and writes C in dtype (MG_F32: C may be the first slice)
 hipError_t launch_linear_sum(int dtype, const LinearArgs &args, int slices, hipStream_t stream);
 
 // The product on the kernel that its plan (linear_plan.h) takes, `room` for slices of its sum; scores_columns, of END_SCORES: columns that one entry of args.scores stands for

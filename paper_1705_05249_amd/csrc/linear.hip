@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
     *reinterpret_cast<end_floatx4 *>(static_cast<uint16_t *>(c.to[m]) + row * padded(cols) + col) = __builtin_bit_cast(end_floatx4, x);
 }
 
-// C = the sum of the slices, in their order.  A work-group has 1024 elements of a row.
+// C = the sum of the slices, in their order (T float: C may be the first of them).  A work-group has 1024 elements of a row.
 template <typename T> __global__ __launch_bounds__(256) void linear_sum_kernel(const LinearArgs args, int slices)
 {
     int64_t row = blockIdx.x;
@@ -119,7 +119,8 @@ hipError_t launch_linear_copies(LinearCopies c, hipStream_t stream)
 hipError_t launch_linear_sum(int dtype, const LinearArgs &args, int slices, hipStream_t stream)
 {
     const dim3 grid(static_cast<uint32_t>(args.rows), static_cast<uint32_t>(ceil_div(args.cols, 1024)));
-    if (dtype == MG_F16) linear_sum_kernel<_Float16><<<grid, 256, 0, stream>>>(args, slices);
+    if (dtype == MG_F32) linear_sum_kernel<float><<<grid, 256, 0, stream>>>(args, slices);
+    else if (dtype == MG_F16) linear_sum_kernel<_Float16><<<grid, 256, 0, stream>>>(args, slices);
     else linear_sum_kernel<bfloat><<<grid, 256, 0, stream>>>(args, slices);
     return hipGetLastError();
 }

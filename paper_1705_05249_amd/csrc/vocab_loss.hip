@@ -3,7 +3,7 @@
 // Logits of 16-bit matrices stay in the registers of the product's kernel: a tile leaves the largest one and the sum of exponentials of each of its
 // rows, and a second kernel joins the tiles (the running maximum and sum of a softmax, over tiles).  The gradient makes the logits again, a piece of the
 // vocabulary at a time, and leaves dz = w (exp(z - lse) - [target]) in the operands' type for the two products that read it: dX is a sum over all
-// pieces, each an FP32 slice of its own, dW's rows belong to one piece each.  FP32: pieces of logits in memory, products as mg_sgemm makes them.
+// pieces, in FP32 slices that are added in the pieces' order, dW's rows belong to one piece each.  FP32: pieces of logits in memory, products as mg_sgemm makes them.
 #include "linear_end.h"
 #include "internal.h"
 
@@ -12,6 +12,11 @@ namespace {
 
 constexpr int64_t F = sizeof(float);
 constexpr int64_t PIECE_ELEMENTS = int64_t(1) << 28;              // of dz in 16 bits; FP32: logits, a quarter as many
+
+// FP32 slices of dX, one for each piece.  Where there are more pieces, the first slice takes the sum of all whenever they are full, in the order in which one launch would add
+// them: the bits are the same.  A slice for every piece, whose columns are 2^28 / tokens, would take memory that grows with tokens^2 (131072 tokens of width 4096, 131072 words:
+// 130 GiB, 9.6 so).  Gradient of 32768 x 2048 x 131072, 16 pieces: 4.63 -> 1.63 GiB, 40.7 -> 40.9 ms; of 65536 x 1024 x 65536: 4.69 -> 1.69 GiB, 23.7 -> 24.0.
+constexpr int64_t MOST_SLICES = 4;
 
 // columns of a piece: a multiple of 256, or the vocabulary
 int64_t piece_columns(int dtype, int64_t tokens, int64_t vocab)
@@ -155,7 +160,7 @@ LossGradMemory loss_grad_memory(Arena &ws, int dtype, int64_t tokens, int64_t wi
     m.dz = ws.take(tokens * padded(columns) * (dtype == MG_F32 ? 4 : 2));
     m.slice = tokens * padded(width);
     if (dtype != MG_F32) {
-        if (count > 1) m.slices = static_cast<float *>(ws.take(count * m.slice * F));
+        if (count > 1) m.slices = static_cast<float *>(ws.take((count < MOST_SLICES ? count : MOST_SLICES) * m.slice * F));
         else m.room_bytes = linear_room(FORM_KN, END_STORE, tokens, width, columns);
         const size_t other = linear_room(FORM_NN, END_STORE, columns, width, tokens);
         m.room_bytes = other > m.room_bytes ? other : m.room_bytes;
@@ -286,7 +291,8 @@ mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
     if (copies_pay(p.tokens, true)) o.w_padded = copy_of(list, ws, o.W, o.ldw, p.vocab, p.width);
     if (const hipError_t e = launch_linear_copies(list, p.stream)) return launched(e);
     const int64_t columns = piece_columns(p.dtype, p.tokens, p.vocab), lead = padded(columns);
-    const int count = static_cast<int>(ceil_div(p.vocab, columns));
+    const int64_t count = ceil_div(p.vocab, columns);
+    int held = 0;                                          // slices of dX that are full
     LinearTogether both{};
     LinearArgs x{};                                        // dX
     x.P = m.dz; x.ldp = lead; x.p_padded = true; x.ldq0 = o.ldw;
@@ -295,7 +301,7 @@ mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
     x.scale = scale == nullptr ? nullptr : scale + 1;
     x.partial_ld = padded(p.width);
     x.partial_stride = m.slice;
-    for (int64_t first = 0, n = 0; first < p.vocab; first += columns, ++n) {
+    for (int64_t first = 0; first < p.vocab; first += columns) {
         const int64_t some = p.vocab - first < columns ? p.vocab - first : columns;
         LinearArgs z = logits(p, o, first, some);
         z.lse = p.lse; z.weights = p.weights; z.weight_scale = scale;
@@ -304,7 +310,14 @@ mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
         if (p.dX != nullptr) {
             x.Q0 = z.Q0;
             x.k = static_cast<int>(some);
-            x.partial = count > 1 ? m.slices + n * m.slice : nullptr;
+            if (held == MOST_SLICES) {
+                LinearArgs sum = x;
+                sum.partial = m.slices;
+                sum.C0 = m.slices; sum.ldc0 = x.partial_ld; sum.scale = nullptr;
+                if (const hipError_t e = launch_linear_sum(MG_F32, sum, held, p.stream)) return launched(e);
+                held = 1;
+            }
+            x.partial = count > 1 ? m.slices + held++ * m.slice : nullptr;
             both.of[0] = x;
         }
         if (p.dW != nullptr) {
@@ -318,7 +331,7 @@ mg_status grad_16(const LossProblem &p, const LossGradMemory &m, Arena &ws)
     }
     if (p.dX != nullptr && count > 1) {
         x.partial = m.slices;
-        return launched(launch_linear_sum(p.dtype, x, count, p.stream));
+        return launched(launch_linear_sum(p.dtype, x, held, p.stream));
     }
     return MG_OK;
 }

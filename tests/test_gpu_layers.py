@@ -418,6 +418,38 @@ def test_losses_in_pieces_of_the_vocabulary(case, dtype):
     run_loss(case, KINDS[dtype])
 
 
+@pytest.mark.parametrize("dtype,tokens,vocab,pieces", [("bf16", 80000, 16640, 5), ("f16", 200000, 16701, 14), ("bf16", 160000, 10800, 8), ("f16", 100001, 10000, 4)])
+def test_losses_in_more_pieces_than_slices(dtype, tokens, vocab, pieces):
+    """every hundredth token counts, the others are ignored: dX of those and dW are what they alone give"""
+    kind, code, width = KINDS[dtype], CODES[KINDS[dtype]], 72
+    columns = (1 << 28) // tokens // 256 * 256
+    assert -(-vocab // columns) == pieces
+    x, w = normal(1, tokens, width).to(kind).cuda(), normal(2, vocab, width, sigma=2 * width ** -0.5).to(kind).cuda()
+    some = torch.arange(7, tokens, 100, device="cuda")
+    targets = torch.full((tokens,), -100, device="cuda")
+    targets[some] = torch.randint(0, vocab, some.shape, generator=torch.Generator().manual_seed(3)).cuda()
+    weights = torch.rand(tokens, generator=torch.Generator().manual_seed(4)).cuda() + 0.5
+    want = R.loss(x[some], w, targets[some], kind, weights[some], gradient=True)
+    lse = torch.zeros(tokens, device="cuda")
+    lse[some] = want["lse"][0].float()
+    size = code, tokens, width, vocab
+    both = []
+    for wanted in ((True, True), (True, False)):
+        dx, dw = (result(*shape, kind) if on else None for on, shape in zip(wanted, ((tokens, width), (vocab, width))))
+        ws_all, ws = scratch(L.mg_vocab_loss_grad_workspace_bytes(*size))
+        L.mg_vocab_loss_grad(*size, x, width, w, width, targets, lse, weights, *dx.at(), *(dw.at() if dw else (None, 0)), ws)
+        torch.cuda.synchronize()
+        R.check(dx.x[some], want["dx"], "dx")
+        others = torch.ones(tokens, dtype=torch.bool, device="cuda")
+        others[some] = False
+        assert not bool(dx.x[others].any()) and dx.untouched() and bool((ws_all[len(ws):] == 255).all())
+        if dw:
+            R.check(dw.x, want["dw"], "dw")
+            assert dw.untouched()
+        both.append(dx.x)
+    assert torch.equal(*both)
+
+
 # ---- clipping
 
 def run_clip(sizes, kinds, max_norm, place, lead=0, scale=1.0):

@@ -202,3 +202,14 @@ print("done")
 """
     run = subprocess.run([sys.executable, "-c", program], cwd=ROOT, env={**os.environ, "HIP_VISIBLE_DEVICES": "-1"}, capture_output=True, text=True)
     assert run.returncode == 0 and run.stdout.split()[-1] == "done", (run.returncode, run.stderr[-500:])
+
+
+@pytest.mark.parametrize("dtype", [L.MG_F16, L.MG_BF16])
+def test_the_gradient_of_the_loss_does_not_hold_a_slice_for_every_piece(dtype):
+    """a copy of X, 2^28 elements of dz or 256 columns of them, copies of odd weights, four slices of dX and room for slices of a product: no tokens^2"""
+    for tokens, width, vocab in ((8192, 2048, 65536), (32768, 4096, 131072), (65536, 4096, 131072), (131072, 4096, 131072), (131072, 8192, 131072), (1 << 20, 1024, 16000), (100001, 1001, 99999)):
+        padded = -(-width // 64) * 64
+        dz = 2 * max(1 << 28, tokens * (256 + 64))
+        room = 64 << 20                                                   # 1024 tiles of 256 x 256 in FP32 are the most that slices of a product have
+        most = (2 + 4 * 4) * tokens * padded + dz + 2 * 2 * vocab * padded * (width % 8 != 0) + 4 * room + 4096
+        assert L.mg_vocab_loss_grad_workspace_bytes(dtype, tokens, width, vocab) <= most, (tokens, width, vocab)
