@@ -98,7 +98,7 @@ size_t mg_vocab_loss_grad_workspace_bytes(int dtype, int64_t tokens, int64_t wid
  * mg_gradient_clip also writes every tensor, multiplied by max_norm / norm where max_norm < norm (formed in 64 bits and rounded to FP32, as each
  * product is to the tensor's type) and as it is otherwise, to results[i]
  * (the same type and size; the same address is fine, any other overlap of results with sources is not; results NULL: all in place).  Where
- * the norm is infinite or no number, tensors stay as they are: the caller sees it in norm[0].  max_norm infinite: nothing is ever clipped.
+ * norm[0] is infinite (also of finite elements whose norm FP32 does not hold) or no number, tensors stay as they are.  max_norm infinite: nothing is ever clipped.
  * Errors: MG_ERR_DIM (count outside 0 .. 2^16, a negative size, more than 2^40 elements in all), MG_ERR_NULL (an array, or an address of a tensor with elements),
  * MG_ERR_WORKSPACE, MG_ERR_TYPE, MG_ERR_LIMIT.  count == 0: norm[0] = 0. */
 mg_status mg_gradient_norm(int64_t count, const int32_t *types, const void *const *sources, const int64_t *sizes, float *norm,

@@ -141,13 +141,13 @@ template <typename T, bool PASS> __device__ inline void scale_chunk(const T *fro
     }
 }
 
-// factor 1 does not touch what is scaled in place and copies what is not, infinities and NaN among it
+// factor 1 does not touch what is scaled in place and copies what is not, infinities and NaN among it.  Whether the norm is finite goes by what the caller is told, in FP32.
 template <bool PASS> __global__ __launch_bounds__(256) void clip_kernel(const ClipTable t, const double *sums, int count, double max_norm, float *norm)
 {
     __shared__ double parts[4];
     const double n = norm_of(sums, count, parts);
     if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = static_cast<float>(n);
-    const float factor = n > max_norm && n < __builtin_inf() ? static_cast<float>(max_norm / n) : 1.f;
+    const float factor = n > max_norm && static_cast<float>(n) < __builtin_inff() ? static_cast<float>(max_norm / n) : 1.f;
     for_chunks<true>(t, [&](int tensor, int type, int64_t first, int some) {
         if (factor == 1.f && t.source[tensor] == t.result[tensor]) return;
         if (type == MG_F32) scale_chunk<float, PASS>(static_cast<const float *>(t.source[tensor]) + first, static_cast<float *>(t.result[tensor]) + first, some, factor);

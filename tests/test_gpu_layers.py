@@ -505,6 +505,25 @@ def test_squares_beyond_fp32():
     run_clip((5000, 600), ("f32", "bf16"), 0.5, "beside", scale=1e-30)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_norms_beyond_fp32(kind):
+    """finite numbers whose norm is told as infinity: they stay as they are, in place and beside"""
+    for numbers in ([3e38, 3e38, -1.0], [2.5e38] * 2 + [1e-3] * 5000):
+        g = torch.tensor(numbers).to(KINDS[kind])
+        held, beside = g.cuda(), torch.full(g.shape, MARK, dtype=g.dtype, device="cuda")
+        assert bool(held.isfinite().all()) and float(held.double().norm()) > torch.finfo(torch.float32).max
+        norm, ws = torch.empty(1, device="cuda"), scratch(L.mg_gradient_workspace_bytes(1))[1]
+        args = 1, torch.tensor([CODES[g.dtype]], dtype=torch.int32), torch.tensor([held.data_ptr()])
+        for results in (torch.tensor([beside.data_ptr()]), None):
+            for limit in (1.0, 3e38, 0.0):
+                norm.fill_(MARK)
+                L.mg_gradient_clip(*args, results, torch.tensor([g.numel()]), limit, norm, ws)
+                assert float(norm) == math.inf and torch.equal(held.cpu(), g) and (results is None or torch.equal(beside.cpu(), g)), (numbers[:3], limit)
+    # just within the range: clipped, by a factor and with products that are off by half a step each
+    g = torch.tensor([3e38, 1e38]).to(KINDS[kind]).cuda()
+    assert math.isfinite(float(D.Gradients([g]).clip(2.0 ** 100))) and abs(float(g.double().norm()) / 2.0 ** 100 - 1.0) <= 2 * R.HALF[KINDS[kind]]
+
+
 def test_limits_of_clipping():
     g = torch.tensor([3.0, 4.0, 0.0], device="cuda")
     grads = D.Gradients([g])
