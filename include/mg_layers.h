@@ -84,7 +84,7 @@ size_t mg_vocab_loss_workspace_bytes(int dtype, int64_t tokens, int64_t width, i
  * weights: FP32 device array of tokens (a mean over `count` tokens has 1/count in it, and a loss scale), NULL: 1.  A token that is ignored or has weight zero adds
  * nothing, whatever its row of X holds, infinities and NaN among it; its row of dX is zero.
  * dz exists for a piece of the vocabulary at a time, in the workspace.  dX or dW may be NULL.  No tokens: dW becomes zero; vocab == 0: dX.
- * 16 bits: dz is rounded in units of the largest weight (MG_F16: of 2^-13 of it), so that equal weights cost no bits and small probabilities keep theirs.
+ * 16 bits: dz is rounded in units of the largest weight of a token that counts (MG_F16: of 2^-13 of it), so that equal weights cost no bits and small probabilities keep theirs.
  * Errors: as above, MG_ERR_LDC (lddx, lddw). */
 mg_status mg_vocab_loss_grad(int dtype, int64_t tokens, int64_t width, int64_t vocab, const void *X, int64_t ldx, const void *W, int64_t ldw,
                              const int64_t *targets, const float *lse, const float *weights, void *dX, int64_t lddx, void *dW, int64_t lddw,

@@ -5,10 +5,10 @@
 namespace mg {
 namespace {
 
-// scale[0] = most / (the largest weight), scale[1] its inverse: what dz is multiplied with while it is an operand in 16 bits, and its products with afterwards.
+// scale[0] = most / (the largest weight of the tokens that count), scale[1] its inverse: what dz is multiplied with while it is an operand in 16 bits, and its products with afterwards.
 // Where all weights are alike, as in a mean, dz then is p - [target] itself, whose -1 of an unlikely target is exact (1 / count is not: off by up to half a
 // step in every token, where it is the largest part of dz).  FP16: most = 2^13, an eighth of the largest number; probabilities down to 2^-27 stay normal.
-__device__ inline void weight_scale(const float *weights, int64_t tokens, float most, float *scale)
+__device__ inline void weight_scale(const float *weights, const int64_t *targets, int64_t vocab, int64_t tokens, float most, float *scale)
 {
     __shared__ uint32_t parts[4];
     uint32_t largest = weights == nullptr ? 0x3f800000u : 0u;
@@ -16,10 +16,15 @@ __device__ inline void weight_scale(const float *weights, int64_t tokens, float 
         // (eight at a time: a load behind the other would be 0.5 us each)
         for (int64_t t = threadIdx.x; t < tokens; t += 8 * 256) {
             uint32_t w[8];
+            int64_t target[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = t + 256 * e < tokens ? __builtin_bit_cast(uint32_t, weights[t + 256 * e]) & 0x7fffffffu : 0u;
+            for (int e = 0; e < 8; ++e) {
+                const bool there = t + 256 * e < tokens;
+                w[e] = there ? __builtin_bit_cast(uint32_t, weights[t + 256 * e]) & 0x7fffffffu : 0u;
+                target[e] = there ? targets[t + 256 * e] : -1;
+            }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) largest = w[e] < 0x7f800000u && w[e] > largest ? w[e] : largest;
+            for (int e = 0; e < 8; ++e) largest = target[e] >= 0 && target[e] < vocab && w[e] < 0x7f800000u && w[e] > largest ? w[e] : largest;
         }
     }
     for (int d = 32; d > 0; d /= 2) {
@@ -43,7 +48,7 @@ __global__ __launch_bounds__(256) void copy_kernel(const LinearCopies c)
 {
     const uint32_t group = blockIdx.y * gridDim.x + blockIdx.x;
     if (group >= c.begin[c.count]) {
-        if (group == c.begin[c.count] && c.scale != nullptr) weight_scale(c.weights, c.rows[0], c.most, c.scale);
+        if (group == c.begin[c.count] && c.scale != nullptr) weight_scale(c.weights, c.targets, c.vocab, c.rows[0], c.most, c.scale);
         return;
     }
     int m = 0;

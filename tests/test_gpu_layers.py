@@ -318,6 +318,28 @@ def test_weights_of_all_sizes(dtype):
 
 
 @pytest.mark.parametrize("dtype", KINDS)
+def test_weights_of_ignored_tokens(dtype):
+    """they may be anything: what the gradient is rounded in goes by the tokens that count"""
+    kind, vocab = KINDS[dtype], 90
+    x, w = normal(1, 600, 40).to(kind).cuda(), normal(2, vocab, 40, sigma=0.2).to(kind).cuda()
+    targets = torch.randint(0, vocab, (600,), generator=torch.Generator().manual_seed(3))
+    ignored = torch.arange(600) % 3 == 1
+    targets[ignored] = torch.tensor([-100, -1, vocab, 1 << 40, -(1 << 63)])[torch.arange(600) % 5][ignored]
+    weights = torch.rand(600, generator=torch.Generator().manual_seed(4)) * 0.01
+    head = D.VocabLoss(w)
+    head.forward(x, targets.cuda())
+    weights[ignored] = 0.0
+    want = head.backward(weights.cuda())
+    for other in (0.005, 1.0, 1e6, -1e30, 3e38, math.inf, -math.inf, math.nan):
+        weights[ignored] = other
+        got = head.backward(weights.cuda())
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), other
+    # none counts: exactly nothing
+    head.forward(x, torch.full((600,), -1, device="cuda"))
+    assert not any(bool(t.any()) for t in head.backward(torch.full((600,), 1e6, device="cuda")))
+
+
+@pytest.mark.parametrize("dtype", KINDS)
 @pytest.mark.parametrize("wanted", [(True, False), (False, True)])
 def test_gradients_of_the_loss_that_are_wanted(wanted, dtype):
     run_loss((40, 72, 333), KINDS[dtype], wanted=wanted)
