@@ -117,6 +117,7 @@ class VocabLoss:
         if self.kept is None:
             raise RuntimeError("backward without a forward pass that kept its inputs")
         w = self.weights
+        _check_current("weights", w.device)
         x, targets, lse = self.kept
         if token_weights is not None:
             token_weights = _checked("token_weights", token_weights, x.shape[:1], w.device, (torch.float32,))
@@ -154,11 +155,13 @@ class Gradients:
 
     def norm(self):
         """the norm of all of them, FP32, one element"""
+        _check_current("tensors", self.value.device)
         L.mg_gradient_norm(self.count, self.types, self.addresses, self.sizes, self.value, self.workspace)
         return self.value
 
     def clip(self, max_norm):
         """scales them in place where their norm is larger; the norm in front of that"""
+        _check_current("tensors", self.value.device)
         L.mg_gradient_clip(self.count, self.types, self.addresses, None, self.sizes, float(max_norm), self.value, self.workspace)
         return self.value
 

@@ -752,6 +752,18 @@ def test_other_devices_are_refused(monkeypatch):
         D.Gradients([x])
 
 
+def test_other_devices_are_refused_in_every_call(monkeypatch):
+    """also by calls that take no tensor of their own"""
+    block, head, x, targets = make(torch.float16)
+    grads = D.Gradients([x])
+    head.forward(x, targets)
+    block.forward(x)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (head.backward, grads.norm, lambda: grads.clip(1.0), lambda: block.backward(x)):
+        with pytest.raises(ValueError, match="current device is cuda:1"):
+            call()
+
+
 def test_memory_that_is_listed_twice():
     g = torch.ones(100, device="cuda")
     with pytest.raises(ValueError, match="0 and 1 share memory"):
