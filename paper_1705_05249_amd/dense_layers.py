@@ -128,7 +128,8 @@ class VocabLoss:
 
 
 class Gradients:
-    """dense tensors whose norm is taken together; listed once, for as long as they stay where they are"""
+    """dense tensors whose norm is taken together; listed once, for as long as they stay where they are.  Every call has a result and a workspace of its own; `value` is the last one's
+    result"""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -146,24 +147,31 @@ class Gradients:
             if start < end:
                 raise ValueError(f"tensors {min(i, j)} and {max(i, j)} share memory")
         self.count = len(self.tensors)
-        device = self.tensors[0].device if self.tensors else "cuda"
+        self.device = self.tensors[0].device if self.tensors else torch.device("cuda", torch.cuda.current_device())
         self.types = torch.tensor([TYPES[t.dtype] for t in self.tensors], dtype=torch.int32, device="cpu")
         self.addresses = torch.tensor([t.data_ptr() for t in self.tensors], dtype=torch.int64, device="cpu")
         self.sizes = torch.tensor([t.numel() for t in self.tensors], dtype=torch.int64, device="cpu")
-        self.value = torch.empty(1, dtype=torch.float32, device=device)
-        self.workspace = _scratch(L.mg_gradient_workspace_bytes(self.count), device)
+        self.value = self._result()
+
+    def _result(self):
+        return torch.empty(1, dtype=torch.float32, device=self.device)
+
+    def _workspace(self):
+        return _scratch(L.mg_gradient_workspace_bytes(self.count), self.device)
 
     def norm(self):
         """the norm of all of them, FP32, one element"""
-        _check_current("tensors", self.value.device)
-        L.mg_gradient_norm(self.count, self.types, self.addresses, self.sizes, self.value, self.workspace)
-        return self.value
+        _check_current("tensors", self.device)
+        value = self.value = self._result()
+        L.mg_gradient_norm(self.count, self.types, self.addresses, self.sizes, value, self._workspace())
+        return value
 
     def clip(self, max_norm):
         """scales them in place where their norm is larger; the norm in front of that"""
-        _check_current("tensors", self.value.device)
-        L.mg_gradient_clip(self.count, self.types, self.addresses, None, self.sizes, float(max_norm), self.value, self.workspace)
-        return self.value
+        _check_current("tensors", self.device)
+        value = self.value = self._result()
+        L.mg_gradient_clip(self.count, self.types, self.addresses, None, self.sizes, float(max_norm), value, self._workspace())
+        return value
 
 
 def train_step(block, head, x, targets, max_norm):

@@ -764,6 +764,38 @@ def test_other_devices_are_refused_in_every_call(monkeypatch):
             call()
 
 
+def test_norms_of_one_list_on_two_streams(monkeypatch):
+    """every call has a result and a workspace of its own"""
+    g = torch.tensor([3.0, 4.0], device="cuda")
+    grads = D.Gradients([g])
+    first = grads.norm()
+    g.mul_(2.0)
+    second = grads.clip(5.0)
+    third = grads.norm()
+    assert [float(t) for t in (first, second, third)] == [5.0, 10.0, 5.0] and g.tolist() == [3.0, 4.0]
+    places = []
+    for name in ("mg_gradient_norm", "mg_gradient_clip"):
+        real = getattr(L, name)
+        monkeypatch.setattr(L, name, lambda *a, real=real: places.append({t.data_ptr() for t in a[-2:]}) or real(*a))
+    torch.cuda.synchronize()
+    streams, norms = [torch.cuda.Stream() for _ in range(2)], []
+    for stream in streams:
+        with torch.cuda.stream(stream):
+            norms.append(grads.norm())
+            norms.append(grads.clip(100.0))
+    torch.cuda.synchronize()
+    assert [float(t) for t in norms] == [5.0] * 4
+    assert not (places[0] | places[1]) & (places[2] | places[3])
+    # two captured graphs and an eager call between their replays
+    graphs = [graph_of(grads.norm) for _ in range(2)]
+    for turn in range(4):
+        for n, (graph, out) in enumerate(graphs):
+            g.copy_(torch.tensor([3.0, 4.0], device="cuda") * (turn + n + 1))
+            graph.replay()
+            g.copy_(torch.tensor([6.0, 8.0], device="cuda"))
+            assert float(grads.norm()) == 10.0 and float(out) == 5.0 * (turn + n + 1)
+
+
 def test_memory_that_is_listed_twice():
     g = torch.ones(100, device="cuda")
     with pytest.raises(ValueError, match="0 and 1 share memory"):
