@@ -11,13 +11,16 @@
  *
  * Sums are in FP32 (MG_F32: as mg_sgemm's).  With 16-bit types a number is rounded to dtype where it becomes an operand of the next product
  * (H, dG and dU of a block, dz of the loss) and where it is a result; activations and exponentials are in FP32, and so is what a block keeps for its
- * backward pass, but for MG_BF16, where that has 11 bits and exponents of its own.
+ * backward pass, but for MG_BF16, where that has 11 bits and an exponent for four neighbouring features (numbers below 2^-28 of the largest of the four may
+ * have fewer, below 2^-40 none).  MG_F16: an element of H, dG or dU beyond 65504 is an infinity, as it is in any program that stores it in that type; dG and dU are
+ * not scaled as dz is, so that gradients in that range are the caller's (a loss scale).
  *
  * Workspaces: 256-byte aligned, at least the bytes that the query of the call answers (MG_ERR_WORKSPACE otherwise), which is 0 for sizes that
  * the call refuses.  With 16-bit types, operands whose rows start on 16 bytes (pointer and leading dimension) and are whole 16-byte pieces
  * along a sum take the fastest kernels as they are.  Others are copied into the workspace first where it has room: the queries count that
- * room where `width` or `hidden` is no multiple of eight; without it the products run on a slower kernel, with the same result up to the order
- * of sums.  Two calls that may run at the same time need a workspace each.
+ * room where `width` or `hidden` is no multiple of eight; without it the products run on a slower kernel (large calls take 2.7 to 4.5 times as long), with the
+ * same result up to the order of sums.  So do matrices of whole widths whose rows lie off 16 bytes in a workspace of the query's size: room for a copy of
+ * each, rows x (columns up to a multiple of 64) x 2 bytes, beyond it is used.  Two calls that may run at the same time need a workspace each.
  *
  * A kernel may read an aligned 16-byte piece of memory whole when at least one of its bytes belongs to an operand.
  *
@@ -82,7 +85,7 @@ size_t mg_vocab_loss_workspace_bytes(int dtype, int64_t tokens, int64_t width, i
  *     dz(t, v) = weights[t] * (exp(z(t, v) - lse[t]) - (v == targets[t])),  0 for ignored targets
  *     dX = dz W,  dW = dz^T X
  * weights: FP32 device array of tokens (a mean over `count` tokens has 1/count in it, and a loss scale), NULL: 1.  A token that is ignored or has weight zero adds
- * nothing, whatever its row of X holds, infinities and NaN among it; its row of dX is zero.
+ * nothing, whatever its row of X holds, infinities and NaN among it; its row of dX is zero (a product of zeros with W: no number where W is not finite).
  * dz exists for a piece of the vocabulary at a time, in the workspace.  dX or dW may be NULL.  No tokens: dW becomes zero; vocab == 0: dX.
  * 16 bits: dz is rounded in units of the largest weight of a token that counts (MG_F16: of 2^-13 of it), so that equal weights cost no bits and small probabilities keep theirs.
  * Errors: as above, MG_ERR_LDC (lddx, lddw). */

@@ -57,8 +57,8 @@ struct LinearArgs {
 
 // What a block keeps of 16-bit types for its backward pass: a = act(G) and b = U act'(G), of which dU = dH a and dG = dH b, in blocks of 16 x 16 in the order in which a
 // matrix instruction leaves them (lane l: row l % 16, columns 4 (l / 16) .. + 3): a wavefront moves a block on end.  FP16: FP32 numbers.  bfloat16: FP16
-// numbers with a power of two for every four of a row, which have 11 bits, three more than dG and dU are rounded to afterwards, whatever the range (bfloat16 would
-// add as much error as that rounding), in 1152 bytes instead of 2048.
+// numbers with a power of two for every four of a row, which puts the largest into 2^14 .. 2^15: 11 bits, three more than dG and dU are rounded to afterwards, whatever the range
+// (bfloat16 would add as much error as that rounding), down to 2^-28 of the largest of the four, fewer below, in 1152 bytes instead of 2048.
 __host__ __device__ inline int64_t kept_blocks(int64_t hidden) { return (hidden + 15) / 16; }
 __host__ __device__ inline int64_t kept_block(int64_t row, int64_t col, int64_t hidden) { return (row / 16) * kept_blocks(hidden) + col / 16; }
 constexpr int kept_block_bytes(int dtype) { return dtype == MG_BF16 ? 1024 + 128 : 2048; }

@@ -7,7 +7,8 @@
 trains a block under a loss on tokens that another model has labelled, with clipped gradients, and prints loss, norm and the time of a step.  In the
 manner of expert_layer.py: outside autograd, `backward` gives the gradients; PyTorch holds the memory and makes the update, everything else runs in the
 library's kernels.  All buffers are allocated by the layers, on their weights' device, none by the library; the calls go to torch's current stream, so
-that device has to be the current one.  What `forward` keeps (its inputs as they are, not copies of them) belongs to its stream: `backward` goes to the same one.
+that device has to be the current one.  Views are used where they are; 16-bit ones whose rows lie off 16 bytes (wide[:, 1:4097]) make large calls 2.7 to 4.5
+times as long as their .contiguous() does.  What `forward` keeps (its inputs as they are, not copies of them) belongs to its stream: `backward` goes to the same one.
 """
 import sys
 
@@ -49,7 +50,8 @@ def _scratch(size, device):
 
 
 class GatedBlock:
-    """weights: gate and up, hidden x width, and down, width x hidden, of one type (views with dense rows are used where they are, so that an update of them is seen)"""
+    """weights: gate and up, hidden x width, and down, width x hidden, of one type (views with dense rows are used where they are, so that an update of them is seen; of others
+    a copy is made once)"""
 
     def __init__(self, gate, up, down, activation="silu"):
         if gate.dim() != 2 or up.shape != gate.shape or tuple(down.shape) != (gate.shape[1], gate.shape[0]):
