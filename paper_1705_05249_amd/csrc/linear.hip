@@ -19,9 +19,9 @@ __device__ inline void weight_scale(const float *weights, const int64_t *targets
             int64_t target[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool there = t + 256 * e < tokens;
-                w[e] = there ? __builtin_bit_cast(uint32_t, weights[t + 256 * e]) & 0x7fffffffu : 0u;
-                target[e] = there ? targets[t + 256 * e] : -1;
+                const int64_t at = t + 256 * e < tokens ? t + 256 * e : tokens - 1;      // (the last one again)
+                w[e] = __builtin_bit_cast(uint32_t, weights[at]) & 0x7fffffffu;
+                target[e] = targets[at];
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) largest = target[e] >= 0 && target[e] < vocab && w[e] < 0x7f800000u && w[e] > largest ? w[e] : largest;
